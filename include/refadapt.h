@@ -2,7 +2,9 @@
  * refadapt.h - C ABI of the MI355X (gfx950) hot path of RefAdapt-DiT
  * (arxiv 2609.32415): joint attention over a [reference; target] token
  * sequence with fresh or cached reference K/V and per-query reference mass,
- * the consecutive target-Q change, the reuse gate and the cache commit.
+ * the consecutive target-Q change, the reuse gate and the cache commit; the
+ * rotary positions of Q and K, and a reference cache in 8 or 4 bits with the
+ * attention over it.
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -337,6 +339,119 @@ ra_status refadapt_cache_commit(int32_t batch, int32_t heads, int32_t n_ref, int
                                 ra_tensor k_ref, ra_tensor v_ref, ra_tensor q_ref, ra_tensor k_cache,
                                 ra_tensor v_cache, ra_tensor q_cache, const int32_t* decision, int32_t* age,
                                 int32_t step, void* stream);
+
+/* ---- Rotary positions ------------------------------------------------------ */
+
+/* Most axes (time, height, width, ...) and most pairs of one call. */
+#define RA_ROPE_MAX_AXES 8
+#define RA_ROPE_MAX_PAIRS 128
+typedef enum { RA_POS_I32 = 0, RA_POS_F32 = 1 } ra_pos_dtype;
+/* Elements of pair i: 2i and 2i + 1, or i and i + n_pairs. */
+typedef enum { RA_ROPE_INTERLEAVED = 0, RA_ROPE_HALF = 1 } ra_rope_pairing;
+
+typedef struct {
+  int32_t batch, heads, rows, head_dim; /* rows >= 0 */
+  int32_t dtype;     /* ra_dtype */
+  int32_t n_pairs;   /* 1..head_dim / 2; elements past 2 n_pairs are copied */
+  int32_t pairing;   /* ra_rope_pairing */
+  int32_t n_axes;    /* 1..RA_ROPE_MAX_AXES */
+  int32_t inverse;   /* 0, or not 0: turn back (the gradient of the turn) */
+  int32_t pos_dtype; /* ra_pos_dtype */
+  int64_t pos_stride_b, pos_stride_s; /* elements; 0 for positions shared by the batch; axes contiguous */
+  const double* freq;  /* HOST [n_pairs]: radians a position */
+  const int32_t* axis; /* HOST [n_pairs]: axis of each pair, 0..n_axes - 1 */
+} ra_rope_desc;
+
+/*
+ * refadapt_rope - rotary positions of Q, or of Q and K, with several axes.
+ *
+ * For row s of batch entry b, every head and every pair i of elements (x, y):
+ *   phi = pos[b, s, axis[i]] * freq[i]   (inverse: -phi)
+ *   (x, y) -> (x cos phi - y sin phi, x sin phi + y cos phi).
+ * The post-rotation Q and K are what refadapt_joint_attn, refadapt_q_change and
+ * the cache commits take. The map is orthogonal: called with `inverse` on the
+ * gradient of its output, it gives the gradient of its input.
+ * q [B, H, rows, d] -> q_out and, with non-NULL data, k -> k_out, in one launch
+ * that forms each angle once. An output may be its own input (same data and
+ * strides); otherwise outputs overlap nothing. `pos` [B, rows, n_axes] is on the
+ * device. phi is reduced in fp64 (off by at most 2^-52 |phi| + 2^-24 radians),
+ * the rest is fp32, rounded once to dtype. Infinite or NaN positions give NaN.
+ * Errors: RA_EINVAL (null pointers, sizes, unknown enums, freq not finite, axis
+ * out of range, one of k and k_out NULL); RA_EUNSUPPORTED (head_dim not in whole
+ * 16-byte units, RA_ROPE_HALF with n_pairs not in whole 16-byte units, n_pairs
+ * above RA_ROPE_MAX_PAIRS, alignment, 2^31 or more 16-byte pieces of q).
+ */
+ra_status refadapt_rope(const ra_rope_desc* desc, ra_tensor q, ra_tensor k, ra_tensor q_out, ra_tensor k_out,
+                        const void* pos, void* stream);
+
+/* ---- Reference cache in 8 or 4 bits ---------------------------------------- */
+
+/* Codes of a quantised cache: e2m1 (0, .5, 1, 1.5, 2, 3, 4, 6 and their
+ * negatives; two a byte, the first in the low half) and e4m3 (largest 448). */
+typedef enum { RA_MXFP4 = 0, RA_MXFP8 = 1 } ra_mx_format;
+
+/* A quantised [B, H, S, d] tensor: d / 2 (RA_MXFP4) or d (RA_MXFP8) bytes of
+ * codes and d / 32 scale bytes a row, each row contiguous, with BYTE strides.
+ * Codes: 16-byte aligned, strides in multiples of 16; scales: base and strides in
+ * multiples of the largest power of two, at most 4, that divides d / 32. Elements 32 j .. 32 j + 31 of a row share scale byte j:
+ * value = code * 2^(byte - 127); byte 255 makes them all NaN. */
+typedef struct {
+  void* codes;
+  int64_t stride_b, stride_h, stride_s;
+  void* scales;
+  int64_t scale_stride_b, scale_stride_h, scale_stride_s;
+} ra_mx_tensor;
+
+/*
+ * refadapt_mx_commit - refadapt_cache_commit into a quantised cache.
+ *
+ * As refadapt_cache_commit (decision, age, step and the optional V and Q pairs),
+ * but quantises the rows. Of a block of 32 elements with largest magnitude m the
+ * scale is 2^e, e = floor(log2 m) - emax (emax 2 for RA_MXFP4, 8 for RA_MXFP8),
+ * plus 1 where m's significand exceeds 1.75 (1.8125), held to -127 (-124) ..
+ * 127 - emax; an element's code is the nearest to x * 2^-e, ties to the even
+ * code, saturating. A block of zeros has the lowest scale, a block that holds a
+ * NaN or an infinity byte 255 and codes 0. Every value is a finite bf16.
+ * Errors: RA_EINVAL (null K tensors, a pair with one NULL side, sizes, enums),
+ * RA_EUNSUPPORTED (head_dim not a multiple of 32, alignment, batch * heads >
+ * 65535).
+ */
+ra_status refadapt_mx_commit(int32_t batch, int32_t heads, int32_t n_ref, int32_t head_dim, int32_t dtype,
+                             int32_t format, ra_tensor k_ref, ra_tensor v_ref, ra_tensor q_ref, ra_mx_tensor k_mx,
+                             ra_mx_tensor v_mx, ra_mx_tensor q_mx, const int32_t* decision, int32_t* age, int32_t step,
+                             void* stream);
+
+/*
+ * refadapt_mx_read - the values that a quantised cache stands for, exactly, in
+ * dtype. K is required; V and Q are read when both sides are non-NULL.
+ * Errors: as refadapt_mx_commit.
+ */
+ra_status refadapt_mx_read(int32_t batch, int32_t heads, int32_t n_ref, int32_t head_dim, int32_t dtype, int32_t format,
+                           ra_mx_tensor k_mx, ra_mx_tensor v_mx, ra_mx_tensor q_mx, ra_tensor k_out, ra_tensor v_out,
+                           ra_tensor q_out, void* stream);
+
+/* The quantised reference cache of a block: K, V and, with non-NULL codes, the reference queries. */
+typedef struct {
+  int32_t format; /* ra_mx_format */
+  ra_mx_tensor k, v, q; /* [B, H, n_ref, d] */
+} ra_mx_cache;
+
+/*
+ * refadapt_joint_attn_mx - refadapt_joint_attn over a quantised reference cache.
+ *
+ * refadapt_joint_attn under RA_KV_CACHE or RA_KV_DEVICE, with the cached
+ * reference K, V and queries taken from `cache` (args->k_cache, v_cache and
+ * q_cache are ignored): the attention over the values that the cache stands for.
+ * args->workspace must hold refadapt_joint_attn_mx_workspace_size(desc, format,
+ * with_q) bytes, 16-byte aligned (with_q: cache->q is given); it needs no
+ * initialisation and must not be used by another call that runs concurrently.
+ * Errors: as refadapt_joint_attn; RA_EUNSUPPORTED for other K/V sources,
+ * seg_mass, and as refadapt_mx_commit for the cache; RA_EWORKSPACE for a missing
+ * or smaller workspace.
+ */
+size_t refadapt_joint_attn_mx_workspace_size(const ra_attn_desc* desc, int32_t format, int32_t with_q);
+ra_status refadapt_joint_attn_mx(const ra_attn_desc* desc, const ra_attn_args* args, const ra_mx_cache* cache,
+                                 void* stream);
 
 /* ---- Diagnostics sidecar --------------------------------------------------
  *

@@ -35,6 +35,9 @@ diagnostics          The analysis quantities of Secs. 3.1-3.3 and App. A.2:
                      exposure (fresh or with anchor reference keys), the
                      reference-query mass on target keys and the adjacent
                      reference-mass change.
+rope                 Rotary positions with several axes.
+mx                   The reference cache in blocks of 32 elements that share
+                     a power-of-two scale: codes, scales and their values.
 
 Every function is pinned by ``-m "not gpu"`` tests in ``tests/`` against
 closed forms, library routines (torch SDPA in fp64, scipy logsumexp),
@@ -45,7 +48,8 @@ the paper.
 from .joint_attention import joint_attention, joint_attention_loops, segment_masses
 from .stats import q_change, head_exposure, gate, GateResult, REUSE, REACTIVATE, COMPUTE
 from .controller import run_controller, local_impact, ControllerTrace
-from . import diagnostics
+from .rope import rope
+from . import diagnostics, mx
 
 __all__ = [
     "joint_attention",
@@ -62,4 +66,6 @@ __all__ = [
     "local_impact",
     "ControllerTrace",
     "diagnostics",
+    "rope",
+    "mx",
 ]

@@ -33,6 +33,12 @@ RA_MAX_SEG = 16
 RA_REUSE, RA_REACTIVATE, RA_COMPUTE = 0, 1, 2
 # ra_gate_mode
 RA_GATE_PRODUCT, RA_GATE_Q_ONLY, RA_GATE_MASS_ONLY, RA_GATE_AND = 0, 1, 2, 3
+# rotary positions
+RA_POS_I32, RA_POS_F32 = 0, 1
+RA_ROPE_INTERLEAVED, RA_ROPE_HALF = 0, 1
+RA_ROPE_MAX_AXES, RA_ROPE_MAX_PAIRS = 8, 128
+# ra_mx_format
+RA_MXFP4, RA_MXFP8 = 0, 1
 # matrix-core rate probe
 RA_PROBE_DENSE, RA_PROBE_MIX = 0, 1
 RA_PROBE_OPERAND_BYTES = 65536
@@ -48,6 +54,11 @@ EXPORTED = (
     "refadapt_q_change_gate",
     "refadapt_q_change_gate_noalloc",
     "refadapt_cache_commit",
+    "refadapt_rope",
+    "refadapt_mx_commit",
+    "refadapt_mx_read",
+    "refadapt_joint_attn_mx_workspace_size",
+    "refadapt_joint_attn_mx",
     "refadapt_kv_drift_workspace_size",
     "refadapt_kv_drift",
     "refadapt_drift_log_ratio_workspace_size",
@@ -69,6 +80,33 @@ class ra_tensor(ctypes.Structure):
         ("stride_h", ctypes.c_int64),
         ("stride_s", ctypes.c_int64),
     ]
+
+
+class ra_rope_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "heads", "rows", "head_dim", "dtype", "n_pairs", "pairing",
+                                              "n_axes", "inverse", "pos_dtype")] + [
+        ("pos_stride_b", ctypes.c_int64),
+        ("pos_stride_s", ctypes.c_int64),
+        ("freq", ctypes.c_void_p),
+        ("axis", ctypes.c_void_p),
+    ]
+
+
+class ra_mx_tensor(ctypes.Structure):
+    _fields_ = [
+        ("codes", ctypes.c_void_p),
+        ("stride_b", ctypes.c_int64),
+        ("stride_h", ctypes.c_int64),
+        ("stride_s", ctypes.c_int64),
+        ("scales", ctypes.c_void_p),
+        ("scale_stride_b", ctypes.c_int64),
+        ("scale_stride_h", ctypes.c_int64),
+        ("scale_stride_s", ctypes.c_int64),
+    ]
+
+
+class ra_mx_cache(ctypes.Structure):
+    _fields_ = [("format", ctypes.c_int32), ("k", ra_mx_tensor), ("v", ra_mx_tensor), ("q", ra_mx_tensor)]
 
 
 class ra_attn_desc(ctypes.Structure):
@@ -158,6 +196,17 @@ def _load():
     lib.refadapt_cache_commit.argtypes = [i32, i32, i32, i32, i32, ra_tensor, ra_tensor, ra_tensor, ra_tensor,
                                           ra_tensor, ra_tensor, vp, vp, i32, vp]
     lib.refadapt_cache_commit.restype = i32
+    lib.refadapt_rope.argtypes = [ctypes.POINTER(ra_rope_desc), ra_tensor, ra_tensor, ra_tensor, ra_tensor, vp, vp]
+    lib.refadapt_rope.restype = i32
+    lib.refadapt_mx_commit.argtypes = [i32] * 6 + [ra_tensor] * 3 + [ra_mx_tensor] * 3 + [vp, vp, i32, vp]
+    lib.refadapt_mx_commit.restype = i32
+    lib.refadapt_mx_read.argtypes = [i32] * 6 + [ra_mx_tensor] * 3 + [ra_tensor] * 3 + [vp]
+    lib.refadapt_mx_read.restype = i32
+    lib.refadapt_joint_attn_mx_workspace_size.argtypes = [ctypes.POINTER(ra_attn_desc), i32, i32]
+    lib.refadapt_joint_attn_mx_workspace_size.restype = ctypes.c_size_t
+    lib.refadapt_joint_attn_mx.argtypes = [ctypes.POINTER(ra_attn_desc), ctypes.POINTER(ra_attn_args),
+                                           ctypes.POINTER(ra_mx_cache), vp]
+    lib.refadapt_joint_attn_mx.restype = i32
     lib.refadapt_kv_drift_workspace_size.argtypes = [i32, i32, i32, i32]
     lib.refadapt_kv_drift_workspace_size.restype = ctypes.c_size_t
     lib.refadapt_kv_drift.argtypes = [i32, i32, i32, i32, i32, ra_tensor, ra_tensor, ra_tensor, ra_tensor, f32,
@@ -195,6 +244,16 @@ ARGS_PACK = struct.Struct("=32qq8q5q18iq4qq")  # ra_attn_args, field by field
 assert DESC_PACK.size == ctypes.sizeof(ra_attn_desc) and ARGS_PACK.size == ctypes.sizeof(ra_attn_args)
 _joint_attn_packed = ctypes.CFUNCTYPE(ctypes.c_int32, ctypes.c_char_p, ctypes.c_char_p, ctypes.c_void_p)(
     ("refadapt_joint_attn", LIB))
+
+
+# The rope and quantised-cache calls on packed blocks too: tensors as 4 or 8 words each.
+ROPE_PACK = struct.Struct("=10i4q")  # ra_rope_desc
+MX_CACHE_PACK = struct.Struct("=i4x24q")  # ra_mx_cache
+assert ROPE_PACK.size == ctypes.sizeof(ra_rope_desc) and MX_CACHE_PACK.size == ctypes.sizeof(ra_mx_cache)
+_joint_attn_mx_packed = ctypes.CFUNCTYPE(ctypes.c_int32, ctypes.c_char_p, ctypes.c_char_p, ctypes.c_char_p,
+                                         ctypes.c_void_p)(("refadapt_joint_attn_mx", LIB))
+_rope_packed = ctypes.CFUNCTYPE(ctypes.c_int32, ctypes.c_char_p, ra_tensor, ra_tensor, ra_tensor, ra_tensor,
+                                ctypes.c_void_p, ctypes.c_void_p)(("refadapt_rope", LIB))
 
 
 def _check(status):
@@ -255,6 +314,31 @@ def refadapt_cache_commit(batch, heads, n_ref, head_dim, dtype, k_ref, v_ref, q_
                           decision, age, step, stream):
     return _check(LIB.refadapt_cache_commit(batch, heads, n_ref, head_dim, dtype, k_ref, v_ref, q_ref, k_cache,
                                             v_cache, q_cache, decision, age, step, stream))
+
+
+def refadapt_rope(desc, q, k, q_out, k_out, pos, stream):
+    """``desc``: bytes of ROPE_PACK."""
+    return _check(_rope_packed(desc, q, k, q_out, k_out, pos, stream))
+
+
+def refadapt_mx_commit(batch, heads, n_ref, head_dim, dtype, fmt, k_ref, v_ref, q_ref, k_mx, v_mx, q_mx, decision, age,
+                       step, stream):
+    return _check(LIB.refadapt_mx_commit(batch, heads, n_ref, head_dim, dtype, fmt, k_ref, v_ref, q_ref, k_mx, v_mx,
+                                         q_mx, decision, age, step, stream))
+
+
+def refadapt_mx_read(batch, heads, n_ref, head_dim, dtype, fmt, k_mx, v_mx, q_mx, k_out, v_out, q_out, stream):
+    return _check(LIB.refadapt_mx_read(batch, heads, n_ref, head_dim, dtype, fmt, k_mx, v_mx, q_mx, k_out, v_out,
+                                       q_out, stream))
+
+
+def refadapt_joint_attn_mx_workspace_size(desc, fmt, with_q):
+    return int(LIB.refadapt_joint_attn_mx_workspace_size(ctypes.byref(desc), fmt, with_q))
+
+
+def refadapt_joint_attn_mx_packed(desc, args, cache, stream):
+    """``refadapt_joint_attn_mx`` on bytes of DESC_PACK, ARGS_PACK and MX_CACHE_PACK."""
+    return _check(_joint_attn_mx_packed(desc, args, cache, stream))
 
 
 def refadapt_kv_drift_workspace_size(batch, heads, n_rows, head_dim):

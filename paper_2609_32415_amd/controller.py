@@ -22,6 +22,10 @@ cue="anchor" the Q-change is taken against the target Q of the block's last
 COMPUTE step (copied on the device by a K-only commit), the paper's
 Anchor-Q x Exposure ablation.
 
+With ``rope`` the inputs' Q and K are those before the rotary positions, and every block
+turns them first (refadapt_rope); with ``cache_format`` the cached K, V and Q are kept in 8 or
+4 bits (refadapt_mx_commit on COMPUTE, refadapt_joint_attn_mx otherwise the same).
+
 The block inputs are exogenous here: the caller supplies each block's fresh
 Q/K/V per step (the diffusion transformer whose hidden states would produce
 them is outside this library).
@@ -34,6 +38,7 @@ trajectory through the same harness.
 from __future__ import annotations
 
 import math
+from dataclasses import dataclass
 
 import torch
 
@@ -41,12 +46,31 @@ from . import ops, synth
 from .ops import COMPUTE, REACTIVATE, REUSE
 
 
+@dataclass
+class Rope:
+    """Rotary positions of a trajectory's tokens: ``ops.rope``'s tables and the positions of its
+    reference and target rows."""
+
+    freq: torch.Tensor
+    axis: torch.Tensor
+    pos_ref: torch.Tensor
+    pos_tgt: torch.Tensor
+    pairing: str = "interleaved"
+
+    def turned(self, x):
+        """The block inputs ``x`` with their Q and K turned (new tensors)."""
+        kw = dict(freq=self.freq, axis=self.axis, pairing=self.pairing)
+        q_tgt, k_tgt = ops.rope(x["q_tgt"], x["k_tgt"], pos=self.pos_tgt, **kw)
+        q_ref, k_ref = ops.rope(x["q_ref"], x["k_ref"], pos=self.pos_ref, **kw)
+        return {**x, "q_tgt": q_tgt, "k_tgt": k_tgt, "q_ref": q_ref, "k_ref": k_ref}
+
+
 class Controller:
     """Device-resident controller state and per-block buffers of one trajectory."""
 
     def __init__(self, n_blocks, n_steps, batch, heads, n_ref, n_tgt, head_dim, theta, delta_max=None,
                  mode="product", theta_m=None, dtype=torch.bfloat16, device="cuda:0", eps=1e-8, fused=True,
-                 cue="consecutive", sidecar=None):
+                 cue="consecutive", sidecar=None, rope=None, cache_format=None):
         self.nb, self.n_steps = n_blocks, n_steps
         self.shape_r = (batch, heads, n_ref, head_dim)
         self.shape_t = (batch, heads, n_tgt, head_dim)
@@ -59,11 +83,15 @@ class Controller:
             th = tq
         self.theta = th.to(torch.float32).contiguous().to(device)
         self.state = ops.new_gate_state(device, delta_max or 0)
-        self.k_cache = [torch.empty(self.shape_r, dtype=dtype, device=device) for _ in range(n_blocks)]
-        self.v_cache = [torch.empty(self.shape_r, dtype=dtype, device=device) for _ in range(n_blocks)]
+        self.rope, self.cache_format = rope, cache_format
+        if cache_format is None:
+            new = lambda: [torch.empty(self.shape_r, dtype=dtype, device=device) for _ in range(n_blocks)]
+        else:
+            new = lambda: [ops.mx_tensor(self.shape_r, cache_format, device) for _ in range(n_blocks)]
+        self.k_cache, self.v_cache = new(), new()
         # reference queries of each block's cached state: the boundary restores that state, so
         # its reference rows attend with them (Alg. 1 boundary branch)
-        self.q_cache = [torch.empty(self.shape_r, dtype=dtype, device=device) for _ in range(n_blocks)]
+        self.q_cache = new()
         self.mass = [[torch.zeros((batch, heads, n_tgt), dtype=torch.float32, device=device) for _ in range(2)]
                      for _ in range(n_blocks)]
         self.parity = [0] * n_blocks
@@ -83,15 +111,20 @@ class Controller:
         q_like = torch.empty(self.shape_t, dtype=dtype, device=device)
         self.fused = fused
         self.ws = ops.q_change_gate_workspace(q_like) if fused else ops.q_change_workspace(q_like)
-        self.attn_ws = ops.attn_workspace(q_like, n_ref, kvsrc="device")
+        self.attn_ws = (ops.attn_workspace(q_like, n_ref, kvsrc="device") if cache_format is None else
+                        ops.attn_mx_workspace(q_like, n_ref, cache_format, kvsrc="device", q_cached=True))
         self.sidecar = sidecar
 
     def block(self, t, b, x, mark=None, clock_probe=None):
         """Enqueue Alg. 1's work for block ``b`` at step ``t`` on fresh inputs ``x``.
 
-        ``mark(name)`` (optional) is called after each enqueued phase ("gate", "attn",
-        "commit"), e.g. to record timing events; ``clock_probe`` is passed to the attention
-        launch (see ``ops.joint_attn``)."""
+        ``mark(name)`` (optional) is called after each enqueued phase ("rope" where the
+        controller has it, "gate", "attn", "commit"), e.g. to record timing events;
+        ``clock_probe`` is passed to the attention launch (see ``ops.joint_attn``)."""
+        if self.rope is not None:
+            x = self.rope.turned(x)
+            if mark:
+                mark("rope")
         if self.cue == "anchor":
             q_prev = self.q_anchor[b] if t > 0 else x["q_tgt"]
         else:
@@ -119,18 +152,25 @@ class Controller:
         if mark:
             mark("gate")
         nxt = 1 - self.parity[b]
-        ops.joint_attn(
-            x["q_tgt"], x["k_tgt"], x["v_tgt"], q_ref=x["q_ref"], k_ref=x["k_ref"], v_ref=x["v_ref"],
-            k_cache=self.k_cache[b], v_cache=self.v_cache[b], q_cache=self.q_cache[b], kvsrc="device", decision=dec,
-            o_tgt=self.o_tgt[b], o_ref=self.o_ref[b], ref_mass=self.mass[b][nxt], workspace=self.attn_ws,
-            clock_probe=clock_probe,
+        if self.cache_format is None:
+            attn, caches = ops.joint_attn, dict(k_cache=self.k_cache[b], v_cache=self.v_cache[b], q_cache=self.q_cache[b])
+        else:
+            attn, caches = ops.joint_attn_mx, dict(k_mx=self.k_cache[b], v_mx=self.v_cache[b], q_mx=self.q_cache[b])
+        attn(
+            x["q_tgt"], x["k_tgt"], x["v_tgt"], q_ref=x["q_ref"], k_ref=x["k_ref"], v_ref=x["v_ref"], **caches,
+            kvsrc="device", decision=dec, o_tgt=self.o_tgt[b], o_ref=self.o_ref[b], ref_mass=self.mass[b][nxt],
+            workspace=self.attn_ws, clock_probe=clock_probe,
         )
         if mark:
             mark("attn")
         if self.sidecar is not None:  # read-only probes; the block's cache still holds its anchor K/V
             self.sidecar.block(t, b, x, self)
-        ops.cache_commit(x["k_ref"], x["v_ref"], self.k_cache[b], self.v_cache[b], decision=dec,
-                         age=age, step=t, q_ref=x["q_ref"], q_cache=self.q_cache[b])
+        if self.cache_format is None:
+            ops.cache_commit(x["k_ref"], x["v_ref"], self.k_cache[b], self.v_cache[b], decision=dec,
+                             age=age, step=t, q_ref=x["q_ref"], q_cache=self.q_cache[b])
+        else:
+            ops.mx_commit(x["k_ref"], x["v_ref"], self.k_cache[b], self.v_cache[b], decision=dec, age=age, step=t,
+                          q_ref=x["q_ref"], q_mx=self.q_cache[b])
         if self.cue == "anchor":
             ops.cache_commit(x["q_tgt"], None, self.q_anchor[b], None, decision=dec)
         if mark:
@@ -207,9 +247,12 @@ class Sidecar:
         ops.mass_mean(self.mass_refq, complement=True, out=self.m_refq_tgt[t, b])
         ops.output_impact(ctl.o_tgt[b], self.o_fresh, eps, out=self.impact[t, b], workspace=self.ws_impact)
         if t > 0:
-            ops.kv_drift(x["k_ref"], ctl.k_cache[b], x["v_ref"], ctl.v_cache[b], eps, d_k=self.d_k[t, b],
+            k_cache, v_cache = ctl.k_cache[b], ctl.v_cache[b]
+            if ctl.cache_format is not None:  # the anchor as the controller's attention reads it
+                k_cache, v_cache = ops.mx_read(k_cache, v_cache, dtype=x["k_ref"].dtype)
+            ops.kv_drift(x["k_ref"], k_cache, x["v_ref"], v_cache, eps, d_k=self.d_k[t, b],
                          d_v=self.d_v[t, b], e_kv=self.e_kv[t, b], workspace=self.ws_kv)
-            ops.joint_attn(x["q_tgt"], x["k_tgt"], x["v_tgt"], k_cache=ctl.k_cache[b], v_cache=ctl.v_cache[b],
+            ops.joint_attn(x["q_tgt"], x["k_tgt"], x["v_tgt"], k_cache=k_cache, v_cache=v_cache,
                            qset="target", kvsrc="cache", o_tgt=self.o_cached, ref_mass=self.mass_cached,
                            workspace=self.ws_cached)
             ops.mass_mean(self.mass_cached, out=self.m_cached[t, b])

@@ -114,7 +114,13 @@ size_t refadapt_joint_attn_seg_workspace_size(const ra_attn_desc* desc, int32_t 
   return launch_seg_ws_bytes(plan_launch(plan_shape(d), true), launch_mode(d, true), d.head_dim, n_seg);
 }
 
-ra_status refadapt_joint_attn(const ra_attn_desc* desc, const ra_attn_args* args, void* stream) {
+}  // extern "C"
+
+namespace {
+
+// refadapt_joint_attn; `before` enqueues what the launch needs first, once every check has passed.
+template <typename Before>
+ra_status joint_attn(const ra_attn_desc* desc, const ra_attn_args* args, void* stream, Before&& before) {
   ra_status s;
   if ((s = check_attn_desc(desc, "joint_attn")) != RA_OK) return s;
   if (!args) return fail(RA_EINVAL, "joint_attn: null args");
@@ -240,6 +246,7 @@ ra_status refadapt_joint_attn(const ra_attn_desc* desc, const ra_attn_args* args
     if ((reinterpret_cast<uintptr_t>(a.workspace) & 15) != 0)
       return fail(RA_EUNSUPPORTED, "joint_attn: workspace must be 16-byte aligned");
     p.qt_ref = ref_queries ? 1 : 0;
+    if (const hipError_t e = before(); e != hipSuccess) return launch_status(e, "joint_attn");
     return launch_status(launch_attn_f32(p, d.head_dim, st), "joint_attn");
   }
 
@@ -274,7 +281,16 @@ ra_status refadapt_joint_attn(const ra_attn_desc* desc, const ra_attn_args* args
   p.part_st = ws ? reinterpret_cast<float4*>(ws + part_o_bytes(items, q.bm, d.head_dim)) : nullptr;
   p.part_lo = ws ? reinterpret_cast<float*>(p.part_st + items * q.bm) : nullptr;
   p.part_seg = ws && a.seg_mass ? reinterpret_cast<float*>(ws + items_ws_bytes(items, q.bm, d.head_dim)) : nullptr;
+  if (const hipError_t e = before(); e != hipSuccess) return launch_status(e, "joint_attn");
   return launch_status(launch_attn_bf16(p, d.head_dim, st), "joint_attn");
+}
+
+}  // namespace
+
+extern "C" {
+
+ra_status refadapt_joint_attn(const ra_attn_desc* desc, const ra_attn_args* args, void* stream) {
+  return joint_attn(desc, args, stream, [] { return hipSuccess; });
 }
 
 size_t refadapt_q_change_workspace_size(int32_t batch, int32_t heads, int32_t n_tgt, int32_t head_dim) {
@@ -466,6 +482,243 @@ ra_status refadapt_cache_commit(int32_t batch, int32_t heads, int32_t n_ref, int
   const hipError_t e = launch_cache_commit(dtype, batch, heads, n_ref, head_dim, cs, decision, age, step,
                                            static_cast<hipStream_t>(stream));
   return launch_status(e, "cache_commit");
+}
+
+}  // extern "C"
+
+// ---- rotary positions
+
+extern "C" {
+
+ra_status refadapt_rope(const ra_rope_desc* desc, ra_tensor q, ra_tensor k, ra_tensor q_out, ra_tensor k_out,
+                        const void* pos, void* stream) {
+  if (!desc) return fail(RA_EINVAL, "rope: null desc");
+  const ra_rope_desc& d = *desc;
+  if (d.batch < 1 || d.heads < 1 || d.rows < 0) return fail(RA_EINVAL, "rope: bad sizes");
+  if (d.dtype != RA_BF16 && d.dtype != RA_F32) return fail(RA_EINVAL, "rope: unknown dtype %d", d.dtype);
+  if (d.pos_dtype != RA_POS_I32 && d.pos_dtype != RA_POS_F32)
+    return fail(RA_EINVAL, "rope: unknown pos_dtype %d", d.pos_dtype);
+  if (d.pairing != RA_ROPE_INTERLEAVED && d.pairing != RA_ROPE_HALF)
+    return fail(RA_EINVAL, "rope: unknown pairing %d", d.pairing);
+  const int n = d.dtype == RA_BF16 ? 8 : 4;
+  if (d.head_dim < n || d.head_dim % n != 0)
+    return fail(RA_EUNSUPPORTED, "rope: head_dim %d must be a positive multiple of %d", d.head_dim, n);
+  if (d.n_pairs < 1 || d.n_pairs > d.head_dim / 2)
+    return fail(RA_EINVAL, "rope: n_pairs %d outside 1..%d", d.n_pairs, d.head_dim / 2);
+  if (d.n_pairs > kRopeMaxPairs) return fail(RA_EUNSUPPORTED, "rope: n_pairs %d above %d", d.n_pairs, kRopeMaxPairs);
+  if (d.pairing == RA_ROPE_HALF && d.n_pairs % n != 0)
+    return fail(RA_EUNSUPPORTED, "rope: RA_ROPE_HALF needs n_pairs in multiples of %d (got %d)", n, d.n_pairs);
+  if (d.n_axes < 1 || d.n_axes > RA_ROPE_MAX_AXES)
+    return fail(RA_EINVAL, "rope: n_axes %d outside 1..%d", d.n_axes, RA_ROPE_MAX_AXES);
+  if (!d.freq || !d.axis) return fail(RA_EINVAL, "rope: null freq or axis table");
+  if (d.pos_stride_b < 0 || d.pos_stride_s < 0) return fail(RA_EINVAL, "rope: negative position stride");
+  RopeParams p{};
+  for (int i = 0; i < d.n_pairs; ++i) {
+    if (!std::isfinite(d.freq[i])) return fail(RA_EINVAL, "rope: freq[%d] is not finite", i);
+    if (d.axis[i] < 0 || d.axis[i] >= d.n_axes)
+      return fail(RA_EINVAL, "rope: axis[%d] = %d outside 0..%d", i, d.axis[i], d.n_axes - 1);
+    p.freq[i] = (d.inverse ? -d.freq[i] : d.freq[i]) * 0.63661977236758134308;  // quarter turns: 2 / pi
+    p.axis[i] = (uint8_t)d.axis[i];
+  }
+  if (d.rows == 0) return ok();
+  if ((int64_t)d.batch * d.rows * (d.head_dim / n) > 0x7fffffff)
+    return fail(RA_EUNSUPPORTED, "rope: problem too large for one launch");
+  if (!pos) return fail(RA_EINVAL, "rope: null pos");
+  if ((reinterpret_cast<uintptr_t>(pos) & 3) != 0) return fail(RA_EUNSUPPORTED, "rope: pos must be 4-byte aligned");
+  ra_status s;
+  if ((s = check_tensor("q", q, d.dtype, d.rows, d.head_dim)) != RA_OK) return s;
+  if ((s = check_tensor("q_out", q_out, d.dtype, d.rows, d.head_dim)) != RA_OK) return s;
+  p.x[0] = view(q);
+  p.y[0] = view(q_out);
+  p.n = 1;
+  if (k.data != nullptr || k_out.data != nullptr) {
+    if ((s = check_tensor("k", k, d.dtype, d.rows, d.head_dim)) != RA_OK) return s;
+    if ((s = check_tensor("k_out", k_out, d.dtype, d.rows, d.head_dim)) != RA_OK) return s;
+    p.x[1] = view(k);
+    p.y[1] = view(k_out);
+    p.n = 2;
+  }
+  p.pos = pos;
+  p.pos_sb = d.pos_stride_b;
+  p.pos_ss = d.pos_stride_s;
+  p.pos_f32 = d.pos_dtype == RA_POS_F32 ? 1 : 0;
+  p.B = d.batch;
+  p.H = d.heads;
+  p.S = d.rows;
+  p.n_pairs = d.n_pairs;
+  return launch_status(launch_rope(d.dtype, d.pairing == RA_ROPE_HALF, d.head_dim, p, static_cast<hipStream_t>(stream)),
+                       "rope");
+}
+
+}  // extern "C"
+
+// ---- the quantised reference cache
+
+namespace {
+
+MxView mx_view(const ra_mx_tensor& t) {
+  return MxView{static_cast<uint8_t*>(t.codes), t.stride_b, t.stride_h, t.stride_s,
+                static_cast<uint8_t*>(t.scales), t.scale_stride_b, t.scale_stride_h, t.scale_stride_s};
+}
+
+ra_status check_mx_sizes(const char* who, int32_t batch, int32_t heads, int32_t n_ref, int32_t head_dim, int32_t dtype,
+                         int32_t format) {
+  if (batch < 1 || heads < 1 || n_ref < 0) return fail(RA_EINVAL, "%s: bad sizes", who);
+  if (dtype != RA_BF16 && dtype != RA_F32) return fail(RA_EINVAL, "%s: unknown dtype %d", who, dtype);
+  if (format != RA_MXFP4 && format != RA_MXFP8) return fail(RA_EINVAL, "%s: unknown format %d", who, format);
+  if (head_dim < 32 || head_dim % 32 != 0)
+    return fail(RA_EUNSUPPORTED, "%s: head_dim %d must be a positive multiple of 32", who, head_dim);
+  if ((int64_t)batch * heads > 65535) return fail(RA_EUNSUPPORTED, "%s: batch*heads must be <= 65535", who);
+  return RA_OK;
+}
+
+// Rows of codes in whole 16-byte units, rows of scales at multiples of 4 bytes as far as their length is one.
+ra_status check_mx(const char* name, const ra_mx_tensor& t, int32_t format, int32_t rows, int32_t head_dim) {
+  const int64_t row = format == RA_MXFP4 ? head_dim / 2 : head_dim, erow = head_dim / 32;
+  if (t.codes == nullptr || t.scales == nullptr) return fail(RA_EINVAL, "%s: null codes or scales", name);
+  if (t.stride_b < 0 || t.stride_h < 0 || t.stride_s < 0 || t.scale_stride_b < 0 || t.scale_stride_h < 0 ||
+      t.scale_stride_s < 0)
+    return fail(RA_EINVAL, "%s: negative stride", name);
+  if (rows > 1 && (t.stride_s < row || t.scale_stride_s < erow))
+    return fail(RA_EINVAL, "%s: row strides %lld and %lld are smaller than a row's %lld codes and %lld scales", name,
+                (long long)t.stride_s, (long long)t.scale_stride_s, (long long)row, (long long)erow);
+  if ((reinterpret_cast<uintptr_t>(t.codes) & 15) != 0 || ((t.stride_b | t.stride_h | t.stride_s) & 15) != 0)
+    return fail(RA_EUNSUPPORTED, "%s: codes must be 16-byte aligned with strides in multiples of 16 bytes", name);
+  const int64_t unit = std::min<int64_t>(erow & -erow, 4);
+  if (reinterpret_cast<uintptr_t>(t.scales) % unit != 0 ||
+      ((t.scale_stride_b | t.scale_stride_h | t.scale_stride_s) & (unit - 1)) != 0)
+    return fail(RA_EUNSUPPORTED, "%s: scales and their strides must be multiples of %lld bytes", name, (long long)unit);
+  return RA_OK;
+}
+
+// The (plain, quantised) pairs of a commit or a read: K is required, V and Q are given on both sides or on neither.
+ra_status mx_set(MxSet* ms, const ra_tensor* const plain[3], const char* const plain_name[3],
+                 const ra_mx_tensor* const mx[3], const char* const mx_name[3], int32_t format, int32_t n_ref,
+                 int32_t head_dim, int32_t dtype) {
+  ra_status s;
+  for (int i = 0; i < 3; ++i) {
+    if (i > 0 && plain[i]->data == nullptr && mx[i]->codes == nullptr && mx[i]->scales == nullptr) continue;
+    if ((s = check_tensor(plain_name[i], *plain[i], dtype, n_ref, head_dim)) != RA_OK) return s;
+    if ((s = check_mx(mx_name[i], *mx[i], format, n_ref, head_dim)) != RA_OK) return s;
+    ms->plain[ms->n] = view(*plain[i]);
+    ms->mx[ms->n] = mx_view(*mx[i]);
+    ++ms->n;
+  }
+  return RA_OK;
+}
+
+// Workspace of the attention over a quantised cache: its K, V (and Q) in the run dtype, then the workspace of
+// refadapt_joint_attn.
+struct MxAttnSpace {
+  size_t tensor;  // bytes of one tensor, in whole 256-byte units
+  int tensors;
+  size_t inner;
+  size_t total() const { return tensor * tensors + inner; }
+};
+
+MxAttnSpace mx_attn_space(const ra_attn_desc& d, bool with_q) {
+  MxAttnSpace s{};
+  if (d.n_ref > 0) {
+    const size_t bytes = (size_t)d.batch * d.heads * d.n_ref * d.head_dim * (d.dtype == RA_BF16 ? 2 : 4);
+    s.tensor = (bytes + 255) & ~size_t(255);
+    s.tensors = 2 + (with_q && launch_mode(d, false).all ? 1 : 0);
+  }
+  s.inner = refadapt_joint_attn_workspace_size(&d);
+  return s;
+}
+
+ra_status check_mx_attn(const char* who, const ra_attn_desc* desc, int32_t format) {
+  ra_status s;
+  if ((s = check_attn_desc(desc, who)) != RA_OK) return s;
+  if (desc->kvsrc != RA_KV_CACHE && desc->kvsrc != RA_KV_DEVICE)
+    return fail(RA_EUNSUPPORTED, "%s: a quantised cache needs RA_KV_CACHE or RA_KV_DEVICE", who);
+  return check_mx_sizes(who, desc->batch, desc->heads, desc->n_ref, desc->head_dim, desc->dtype, format);
+}
+
+}  // namespace
+
+extern "C" {
+
+ra_status refadapt_mx_commit(int32_t batch, int32_t heads, int32_t n_ref, int32_t head_dim, int32_t dtype,
+                             int32_t format, ra_tensor k_ref, ra_tensor v_ref, ra_tensor q_ref, ra_mx_tensor k_mx,
+                             ra_mx_tensor v_mx, ra_mx_tensor q_mx, const int32_t* decision, int32_t* age, int32_t step,
+                             void* stream) {
+  ra_status s;
+  if ((s = check_mx_sizes("mx_commit", batch, heads, n_ref, head_dim, dtype, format)) != RA_OK) return s;
+  if (n_ref == 0) return ok();
+  MxSet ms{};
+  const ra_tensor* const plain[3] = {&k_ref, &v_ref, &q_ref};
+  const ra_mx_tensor* const mx[3] = {&k_mx, &v_mx, &q_mx};
+  const char* const plain_name[3] = {"k_ref", "v_ref", "q_ref"};
+  const char* const mx_name[3] = {"k_mx", "v_mx", "q_mx"};
+  if ((s = mx_set(&ms, plain, plain_name, mx, mx_name, format, n_ref, head_dim, dtype)) != RA_OK) return s;
+  return launch_status(launch_mx_commit(dtype, format, batch, heads, n_ref, head_dim, ms, decision, age, step,
+                                        static_cast<hipStream_t>(stream)),
+                       "mx_commit");
+}
+
+ra_status refadapt_mx_read(int32_t batch, int32_t heads, int32_t n_ref, int32_t head_dim, int32_t dtype, int32_t format,
+                           ra_mx_tensor k_mx, ra_mx_tensor v_mx, ra_mx_tensor q_mx, ra_tensor k_out, ra_tensor v_out,
+                           ra_tensor q_out, void* stream) {
+  ra_status s;
+  if ((s = check_mx_sizes("mx_read", batch, heads, n_ref, head_dim, dtype, format)) != RA_OK) return s;
+  if (n_ref == 0) return ok();
+  MxSet ms{};
+  const ra_tensor* const plain[3] = {&k_out, &v_out, &q_out};
+  const ra_mx_tensor* const mx[3] = {&k_mx, &v_mx, &q_mx};
+  const char* const plain_name[3] = {"k_out", "v_out", "q_out"};
+  const char* const mx_name[3] = {"k_mx", "v_mx", "q_mx"};
+  if ((s = mx_set(&ms, plain, plain_name, mx, mx_name, format, n_ref, head_dim, dtype)) != RA_OK) return s;
+  return launch_status(launch_mx_read(dtype, format, batch, heads, n_ref, head_dim, ms, nullptr, 3,
+                                      static_cast<hipStream_t>(stream)),
+                       "mx_read");
+}
+
+size_t refadapt_joint_attn_mx_workspace_size(const ra_attn_desc* desc, int32_t format, int32_t with_q) {
+  if (check_mx_attn("joint_attn_mx_workspace_size", desc, format) != RA_OK) return 0;
+  return mx_attn_space(*desc, with_q != 0).total();
+}
+
+ra_status refadapt_joint_attn_mx(const ra_attn_desc* desc, const ra_attn_args* args, const ra_mx_cache* cache,
+                                 void* stream) {
+  if (!cache) return fail(RA_EINVAL, "joint_attn_mx: null cache");
+  const ra_mx_cache& c = *cache;
+  ra_status s;
+  if ((s = check_mx_attn("joint_attn_mx", desc, c.format)) != RA_OK) return s;
+  if (!args) return fail(RA_EINVAL, "joint_attn_mx: null args");
+  const ra_attn_desc& d = *desc;
+  ra_attn_args a = *args;
+  if (a.seg_mass != nullptr) return fail(RA_EUNSUPPORTED, "joint_attn_mx: reference segments are not available");
+  a.k_cache = a.v_cache = a.q_cache = ra_tensor{nullptr, 0, 0, 0};
+  if (d.n_ref == 0) return refadapt_joint_attn(&d, &a, stream);
+  const bool with_q = launch_mode(d, false).all && (c.q.codes != nullptr || c.q.scales != nullptr);
+  const ra_mx_tensor* const mx[3] = {&c.k, &c.v, &c.q};
+  const char* const mx_name[3] = {"k_mx", "v_mx", "q_mx"};
+  const int n = with_q ? 3 : 2;
+  for (int i = 0; i < n; ++i)
+    if ((s = check_mx(mx_name[i], *mx[i], c.format, d.n_ref, d.head_dim)) != RA_OK) return s;
+  const MxAttnSpace space = mx_attn_space(d, with_q);
+  if (a.workspace == nullptr || a.workspace_bytes < space.total())
+    return fail(RA_EWORKSPACE, "joint_attn_mx: workspace needs %zu bytes (got %zu)", space.total(),
+                a.workspace ? a.workspace_bytes : 0);
+  if ((reinterpret_cast<uintptr_t>(a.workspace) & 15) != 0)
+    return fail(RA_EUNSUPPORTED, "joint_attn_mx: workspace must be 16-byte aligned");
+  char* const ws = static_cast<char*>(a.workspace);
+  MxSet ms{};
+  ra_tensor* const into[3] = {&a.k_cache, &a.v_cache, &a.q_cache};
+  const int64_t row = d.head_dim;
+  for (int i = 0; i < n; ++i) {
+    *into[i] = ra_tensor{ws + i * space.tensor, (int64_t)d.heads * d.n_ref * row, d.n_ref * row, row};
+    ms.plain[i] = view(*into[i]);
+    ms.mx[i] = mx_view(*mx[i]);
+  }
+  ms.n = n;
+  a.workspace = space.inner > 0 ? ws + space.tensor * n : nullptr;
+  a.workspace_bytes = space.inner;
+  return joint_attn(&d, &a, stream, [&] {
+    return launch_mx_read(d.dtype, c.format, d.batch, d.heads, d.n_ref, d.head_dim, ms,
+                          d.kvsrc == RA_KV_DEVICE ? a.decision : nullptr, 2, static_cast<hipStream_t>(stream));
+  });
 }
 
 }  // extern "C"

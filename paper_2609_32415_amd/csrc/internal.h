@@ -116,6 +116,43 @@ struct CommitSet {
 hipError_t launch_cache_commit(int dtype, int32_t B, int32_t H, int32_t n_ref, int32_t head_dim, CommitSet cs,
                                const int32_t* decision, int32_t* age, int32_t step, hipStream_t stream);
 
+// One tensor of the quantised reference cache: codes and scale bytes of [B, H, n, d], byte strides; a row's
+// codes and its scales are contiguous.
+struct MxView {
+  uint8_t* codes;
+  int64_t sb, sh, ss;
+  uint8_t* scales;
+  int64_t eb, eh, es;
+};
+enum { MX_FP4 = 0, MX_FP8 = 1 };
+// Up to three (plain, quantised) pairs that one commit or read launch takes.
+struct MxSet {
+  View plain[3];
+  MxView mx[3];
+  int32_t n;
+};
+hipError_t launch_mx_commit(int dtype, int format, int32_t B, int32_t H, int32_t n_ref, int32_t head_dim,
+                            const MxSet& ms, const int32_t* decision, int32_t* age, int32_t step, hipStream_t stream);
+// With a decision word the first `always` tensors are read unless it is COMPUTE, the others on REACTIVATE only.
+hipError_t launch_mx_read(int dtype, int format, int32_t B, int32_t H, int32_t n_ref, int32_t head_dim,
+                          const MxSet& ms, const int32_t* decision, int32_t always, hipStream_t stream);
+
+// Rotary positions of up to two [B, H, S, d] tensors. The tables travel in the kernel arguments.
+constexpr int kRopeMaxPairs = 128;
+struct RopeParams {
+  View x[2], y[2];
+  const void* pos;  // [B, S, axes] fp32 or int32; element strides, axes contiguous
+  int64_t pos_sb, pos_ss;
+  int32_t n, pos_f32;
+  int32_t B, H, S;
+  int32_t n_pairs;
+  int32_t pieces;     // 16-byte pieces (pairs of pieces) of a row that a thread takes, set by the launcher
+  int32_t heads_per;  // heads that a workgroup walks over, set by the launcher
+  double freq[kRopeMaxPairs];  // quarter turns a position (negative for the inverse)
+  uint8_t axis[kRopeMaxPairs];
+};
+hipError_t launch_rope(int dtype, bool half, int32_t head_dim, RopeParams p, hipStream_t stream);
+
 // Up to two [B, H, n, d] slice pairs whose relative change the diagnostics
 // reduce in one launch; chunks[] is filled by the launcher.
 struct PairSet {

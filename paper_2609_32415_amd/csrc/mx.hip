@@ -1,0 +1,111 @@
+// The reference cache in blocks of 32 elements that share a power-of-two scale (gfx950):
+//   mx_commit  quantises K, V and Q rows into codes and scales when the decision is COMPUTE (or absent)
+//   mx_read    the values that codes and scales stand for, in bf16 or fp32
+//
+// A block x_0..x_31 of a row (32 neighbours along the head dim) is kept as codes c_i and one exponent e,
+// x_i ~ value(c_i) * 2^e. With emax the largest code's exponent (e2m1: 2, largest 6; e4m3: 8, largest 448),
+//   e = floor(log2 max|x_i|) - emax, + 1 where the significand of max|x_i| exceeds T (1.75; 1.8125),
+// held to [lowest, 127 - emax]; c_i rounds x_i * 2^-e to the nearest code, ties to even, saturating. T is the largest
+// significand that the largest code is still within half of its step of (7 of 6, 464 of 448), so
+// saturation adds no error beyond a rounding's: between 6 and 7 the finer scale errs by at most 1, as
+// the codes 4 and 6 do between themselves, and halves the error of every smaller element. e comes from the bits of
+// max|x_i|, without arithmetic, and multiplying by 2^-e is exact: the codes have one right value.
+// lowest (-127; -124) and 127 - emax keep every value a finite bf16: reading back is exact.
+// A block that holds a NaN or an infinity gets the scale byte 255 and reads back as NaN throughout.
+//
+// Both kernels are bound by memory: 2 bytes an element in bf16 against 0.53 (1.03) of codes and scales.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "internal.h"
+#include "mxcodes.h"
+
+namespace refadapt {
+namespace {
+
+constexpr int MX_THREADS = 256;
+
+// A thread takes 8 elements, four threads a block; blockIdx.z is the tensor of the set.
+template <bool FP4, bool BF16>
+__global__ __launch_bounds__(MX_THREADS) void mx_commit_kernel(MxSet ms, int32_t H, int32_t n_rows, int32_t vpr,
+                                                               const int32_t* decision, int32_t* age, int32_t step) {
+  if (decision && *decision != DEC_COMPUTE) return;
+  const int bh = blockIdx.y;
+  const int b = bh / H, h = bh - b * H;
+  const View src = ms.plain[blockIdx.z];
+  const MxView dst = ms.mx[blockIdx.z];
+  const int esz = BF16 ? 2 : 4;
+  const char* sb = static_cast<const char*>(src.p) + (b * src.sb + h * src.sh) * esz;
+  uint8_t* cb = dst.codes + b * dst.sb + h * dst.sh;
+  uint8_t* eb = dst.scales + b * dst.eb + h * dst.eh;
+  const int64_t nvec = (int64_t)n_rows * vpr;
+  for (int64_t v = (int64_t)blockIdx.x * MX_THREADS + threadIdx.x; v < nvec; v += (int64_t)gridDim.x * MX_THREADS) {
+    const int64_t row = v / vpr;
+    const int col = (int)(v - row * vpr);  // of 8 elements
+    const Oct x = load_oct<BF16>(sb + (row * src.ss + 8 * col) * esz);
+    // a row's vectors come in whole blocks of four, so the four lanes of a block are active together
+    uint32_t m = max_bits(x);
+    m = max(m, (uint32_t)__shfl_xor((int)m, 1));
+    m = max(m, (uint32_t)__shfl_xor((int)m, 2));
+    const uint32_t e = scale_byte<FP4>(m);
+    store_codes<FP4>(cb + row * dst.ss + (FP4 ? 4 : 8) * col, x, e);
+    if ((col & 3) == 0) eb[row * dst.es + (col >> 2)] = (uint8_t)e;
+  }
+  if (age && blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == 0) *age = step;
+}
+
+// `decision` (null: always): the tensors of `always` are read unless it is COMPUTE, the rest on REACTIVATE.
+template <bool FP4, bool BF16>
+__global__ __launch_bounds__(MX_THREADS) void mx_read_kernel(MxSet ms, int32_t H, int32_t n_rows, int32_t vpr,
+                                                             const int32_t* decision, int32_t always) {
+  if (decision) {
+    const int dec = *decision;
+    if (dec == DEC_COMPUTE || ((int)blockIdx.z >= always && dec != DEC_REACTIVATE)) return;
+  }
+  const int bh = blockIdx.y;
+  const int b = bh / H, h = bh - b * H;
+  const View dst = ms.plain[blockIdx.z];
+  const MxView src = ms.mx[blockIdx.z];
+  const int esz = BF16 ? 2 : 4;
+  char* db = static_cast<char*>(const_cast<void*>(dst.p)) + (b * dst.sb + h * dst.sh) * esz;
+  const uint8_t* cb = src.codes + b * src.sb + h * src.sh;
+  const uint8_t* eb = src.scales + b * src.eb + h * src.eh;
+  const int64_t nvec = (int64_t)n_rows * vpr;
+  for (int64_t v = (int64_t)blockIdx.x * MX_THREADS + threadIdx.x; v < nvec; v += (int64_t)gridDim.x * MX_THREADS) {
+    const int64_t row = v / vpr;
+    const int col = (int)(v - row * vpr);
+    const u32x2 c = load_codes<FP4>(cb + row * src.ss + (FP4 ? 4 : 8) * col);
+    const u32x4 w = decode_oct<FP4>(c, eb[row * src.es + (col >> 2)]);
+    store_oct<BF16>(db + (row * dst.ss + 8 * col) * esz, w);
+  }
+}
+
+dim3 mx_grid(int32_t bh, int32_t n_rows, int32_t head_dim, int n) {
+  const int64_t nvec = (int64_t)n_rows * (head_dim / 8);
+  const int64_t gx = (nvec + MX_THREADS * 4 - 1) / (MX_THREADS * 4);
+  return dim3((unsigned)(gx < 1 ? 1 : gx > 1024 ? 1024 : gx), bh, n);
+}
+
+}  // namespace
+
+hipError_t launch_mx_commit(int dtype, int format, int32_t B, int32_t H, int32_t n_ref, int32_t head_dim,
+                            const MxSet& ms, const int32_t* decision, int32_t* age, int32_t step, hipStream_t stream) {
+  const dim3 grid = mx_grid(B * H, n_ref, head_dim, ms.n);
+  const auto run = [&](auto* kernel) {
+    return launch_kernel(kernel, grid, dim3(MX_THREADS), 0, stream, ms, H, n_ref, head_dim / 8, decision, age, step);
+  };
+  if (format == MX_FP4) return dtype == 0 ? run(mx_commit_kernel<true, true>) : run(mx_commit_kernel<true, false>);
+  return dtype == 0 ? run(mx_commit_kernel<false, true>) : run(mx_commit_kernel<false, false>);
+}
+
+hipError_t launch_mx_read(int dtype, int format, int32_t B, int32_t H, int32_t n_ref, int32_t head_dim,
+                          const MxSet& ms, const int32_t* decision, int32_t always, hipStream_t stream) {
+  const dim3 grid = mx_grid(B * H, n_ref, head_dim, ms.n);
+  const auto run = [&](auto* kernel) {
+    return launch_kernel(kernel, grid, dim3(MX_THREADS), 0, stream, ms, H, n_ref, head_dim / 8, decision, always);
+  };
+  if (format == MX_FP4) return dtype == 0 ? run(mx_read_kernel<true, true>) : run(mx_read_kernel<true, false>);
+  return dtype == 0 ? run(mx_read_kernel<false, true>) : run(mx_read_kernel<false, false>);
+}
+
+}  // namespace refadapt

@@ -510,6 +510,254 @@ def adjacent_mass_change(mass_log, out=None):
     return out
 
 
+# ---- rotary positions, and the reference cache in 8 or 4 bits
+
+_POS = {torch.int32: L.RA_POS_I32, torch.float32: L.RA_POS_F32}
+_PAIRING = {"interleaved": L.RA_ROPE_INTERLEAVED, "half": L.RA_ROPE_HALF}
+_MX = {"mxfp4": L.RA_MXFP4, "mxfp8": L.RA_MXFP8}
+MX_BLOCK = 32  # neighbouring elements of a row that share a scale
+
+
+def _here(name, t):
+    # on the GPU that the launch goes to
+    _on_gpu(name, t)
+    if t.device.index != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch._C._cuda_getDevice()}")
+
+
+def rope_frequencies(axes, theta=10000.0):
+    """The tables of ``rope`` for ``axes``, the elements of a head that turn with each axis in order (even numbers,
+    e.g. (16, 56, 56) for time, height and width): pair j of an axis of n elements turns by
+    theta^(-2 j / n) radians a position. Returns (freq fp64, axis int32), on the host."""
+    if not axes or any(n < 2 or n % 2 for n in axes):
+        raise ValueError("axes must be even numbers of elements")
+    freq = [theta ** (-2.0 * j / n) for n in axes for j in range(n // 2)]
+    axis = [a for a, n in enumerate(axes) for _ in range(n // 2)]
+    return torch.tensor(freq, dtype=torch.float64), torch.tensor(axis, dtype=torch.int32)
+
+
+def rope(q, k=None, *, pos, freq, axis, pairing="interleaved", inverse=False, q_out=None, k_out=None):
+    """Rotary positions of ``q`` [B, H, S, d], or of ``q`` and ``k`` in one launch, through ``refadapt_rope``.
+
+    ``pos``: int32 or fp32 positions [S, axes] or [B, S, axes] on the device. ``freq`` and ``axis``: host
+    tables of the pairs (``rope_frequencies``, or a model's own): pair i turns by pos[..., axis[i]] * freq[i]
+    radians. ``pairing``: elements (2i, 2i + 1), or "half": (i, i + pairs); elements past the pairs are
+    copied. ``inverse`` turns back, which is also the gradient: with it the gradient of an output gives that
+    of the input. ``q_out=q`` works in place. Returns q_out, or (q_out, k_out) with ``k``.
+    """
+    B, H, S, D = q.shape
+    dt = q.dtype
+    if dt not in _DTYPES:
+        raise ValueError(f"unsupported dtype {dt}")
+    if pairing not in _PAIRING:
+        raise ValueError(f"pairing must be one of {sorted(_PAIRING)}")
+    _here("q", q)
+    _here("pos", pos)
+    if pos.dtype not in _POS or pos.dim() not in (2, 3) or pos.stride(-1) != 1 and pos.shape[-1] != 1:
+        raise ValueError("pos must be int32 or float32 [S, axes] or [B, S, axes] with contiguous axes")
+    if pos.shape[-2] != S or pos.dim() == 3 and pos.shape[0] not in (1, B):
+        raise ValueError(f"pos {tuple(pos.shape)} does not fit {B} x {S} rows")
+    n = freq.numel()
+    for name, t, want in (("freq", freq, torch.float64), ("axis", axis, torch.int32)):
+        if t.is_cuda or t.dtype != want or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {want} host tensor, one entry a pair")
+    if k is not None:
+        _here("k", k)
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    q_out = torch.empty_like(q) if q_out is None else q_out
+    k_out = torch.empty_like(k) if k is not None and k_out is None else k_out
+    for name, t in (("q_out", q_out), ("k_out", k_out)):
+        if t is not None:
+            _here(name, t)
+    shape = (B, H, S, D)
+    views = [_view("q", q, dt), _view("k", k, dt, shape), _view("q_out", q_out, dt, shape),
+             _view("k_out", k_out, dt, shape)]
+    pos_sb = pos.stride(0) if pos.dim() == 3 and pos.shape[0] == B else 0
+    desc = L.ROPE_PACK.pack(B, H, S, D, _DTYPES[dt], n, _PAIRING[pairing], pos.shape[-1], int(bool(inverse)),
+                            _POS[pos.dtype], pos_sb, pos.stride(-2), freq.data_ptr(), axis.data_ptr())
+    L.refadapt_rope(desc, *views, _ptr(pos), _stream())
+    return q_out if k is None else (q_out, k_out)
+
+
+@dataclass
+class MxTensor:
+    """A quantised [B, H, n, d] tensor: uint8 ``codes`` [B, H, n, d / 2] ("mxfp4") or [B, H, n, d] ("mxfp8") and
+    uint8 ``scales`` [B, H, n, d / 32]; see ``mx_tensor``."""
+
+    codes: torch.Tensor
+    scales: torch.Tensor
+    fmt: str
+
+    @property
+    def shape(self):
+        *lead, width = self.codes.shape
+        return torch.Size((*lead, 2 * width if self.fmt == "mxfp4" else width))
+
+    def rows(self, n):
+        """View of the first ``n`` rows of every head (a cache allocated for more reference tokens)."""
+        return MxTensor(self.codes[:, :, :n], self.scales[:, :, :n], self.fmt)
+
+
+def mx_tensor(shape, fmt, device):
+    """An uninitialised ``MxTensor`` for [B, H, n, d] rows: 4.25 ("mxfp4") or 8.25 ("mxfp8") bits an element."""
+    if fmt not in _MX:
+        raise ValueError(f"format must be one of {sorted(_MX)}")
+    B, H, n, d = shape
+    if d < MX_BLOCK or d % MX_BLOCK:
+        raise ValueError(f"the head dimension must be a multiple of {MX_BLOCK}")
+    codes = torch.empty((B, H, n, d // 2 if fmt == "mxfp4" else d), dtype=torch.uint8, device=device)
+    return MxTensor(codes, torch.empty((B, H, n, d // MX_BLOCK), dtype=torch.uint8, device=device), fmt)
+
+
+_NO_MX = (0,) * 8
+
+
+def _oct(name, t, fmt, shape):
+    """(codes, strides, scales, strides) of an MxTensor of this shape, checked."""
+    if t is None:
+        return _NO_MX
+    if t.fmt != fmt:
+        raise ValueError(f"{name}: format {t.fmt} differs from {fmt}")
+    B, H, n, d = shape
+    for what, x, width in (("codes", t.codes, d // 2 if fmt == "mxfp4" else d), ("scales", t.scales, d // MX_BLOCK)):
+        _here(f"{name}.{what}", x)
+        if x.dtype != torch.uint8 or tuple(x.shape) != (B, H, n, width):
+            raise ValueError(f"{name}.{what} must be uint8 of shape {(B, H, n, width)}")
+        if x.stride(3) != 1 and width > 1:
+            raise ValueError(f"{name}.{what}: rows must be contiguous")
+    if 0 in shape:
+        return _NO_MX
+    return (t.codes.data_ptr(), *t.codes.stride()[:3], t.scales.data_ptr(), *t.scales.stride()[:3])
+
+
+def _mx_view(name, t, fmt, shape):
+    return L.ra_mx_tensor(*_oct(name, t, fmt, shape))
+
+
+def _mx_format(*tensors):
+    fmt = next(t.fmt for t in tensors if t is not None)
+    if fmt not in _MX:
+        raise ValueError(f"format must be one of {sorted(_MX)}")
+    return fmt
+
+
+def mx_commit(k_ref, v_ref, k_mx, v_mx, decision=None, age=None, step=0, q_ref=None, q_mx=None):
+    """``cache_commit`` into a quantised cache, through ``refadapt_mx_commit``: rounds the fresh reference K, V (and Q
+    when ``q_ref``/``q_mx`` are given) into the ``MxTensor``s when ``decision`` is COMPUTE (or None); with ``v_ref``
+    and ``v_mx`` None only K. One launch takes every pair."""
+    B, H, n_ref, D = k_ref.shape
+    dt = k_ref.dtype
+    if dt not in _DTYPES:
+        raise ValueError(f"unsupported dtype {dt}")
+    if (v_ref is None) != (v_mx is None):
+        raise ValueError("v_ref and v_mx are both given or both None")
+    if (q_ref is None) != (q_mx is None):
+        raise ValueError("q_ref and q_mx are both given or both None")
+    for name, t in (("decision", decision), ("age", age)):
+        if t is not None:
+            _here(name, t)
+            if t.dtype != torch.int32:
+                raise ValueError(f"{name} must be int32")
+    for name, t in (("k_ref", k_ref), ("v_ref", v_ref), ("q_ref", q_ref)):
+        if t is not None:
+            _here(name, t)
+    fmt, shape = _mx_format(k_mx), k_ref.shape
+    L.refadapt_mx_commit(
+        B, H, n_ref, D, _DTYPES[dt], _MX[fmt], _view("k_ref", k_ref, dt), _view("v_ref", v_ref, dt, shape),
+        _view("q_ref", q_ref, dt, shape), _mx_view("k_mx", k_mx, fmt, shape), _mx_view("v_mx", v_mx, fmt, shape),
+        _mx_view("q_mx", q_mx, fmt, shape), _ptr(decision), _ptr(age), int(step), _stream(),
+    )
+
+
+def mx_read(k_mx, v_mx=None, q_mx=None, dtype=torch.bfloat16, k_out=None, v_out=None, q_out=None):
+    """The values that quantised tensors stand for, exactly, through ``refadapt_mx_read``; one launch reads all
+    of them. Returns a tuple of as many tensors as were given."""
+    if dtype not in _DTYPES:
+        raise ValueError(f"unsupported dtype {dtype}")
+    fmt, shape = _mx_format(k_mx), k_mx.shape
+    outs = []
+    for name, m, o in (("k", k_mx, k_out), ("v", v_mx, v_out), ("q", q_mx, q_out)):
+        if m is None and o is not None:
+            raise ValueError(f"{name}_out without {name}_mx")
+        if m is not None and o is None:
+            o = torch.empty(shape, dtype=dtype, device=k_mx.codes.device)
+        if o is not None:
+            _here(f"{name}_out", o)
+        outs.append(o)
+    B, H, n, D = shape
+    L.refadapt_mx_read(
+        B, H, n, D, _DTYPES[dtype], _MX[fmt], _mx_view("k_mx", k_mx, fmt, shape), _mx_view("v_mx", v_mx, fmt, shape),
+        _mx_view("q_mx", q_mx, fmt, shape), *(_view(f"{n}_out", o, dtype, shape) for n, o in zip("kvq", outs)),
+        _stream(),
+    )
+    return tuple(o for o in outs if o is not None)
+
+
+def joint_attn_mx(q_tgt, k_tgt, v_tgt, *, k_mx, v_mx, q_mx=None, q_ref=None, k_ref=None, v_ref=None, qset="target",
+                  kvsrc="cache", decision=None, scale=None, o_tgt=None, o_ref=None, ref_mass=True, lse=False,
+                  ref_mass_refq=False, workspace=None, clock_probe=None):
+    """``joint_attn`` with ``kvsrc`` "cache" or "device" whose cached reference K, V (and queries, ``q_mx``) are
+    ``MxTensor``s, through ``refadapt_joint_attn_mx``. ``workspace``: None allocates what the library asks for, a
+    uint8 device tensor is used as given (``attn_mx_workspace``). Returns an ``AttnOut``."""
+    B, H, n_tgt, D = q_tgt.shape
+    dt = q_tgt.dtype
+    if dt not in _DTYPES:
+        raise ValueError(f"unsupported dtype {dt}")
+    if kvsrc not in ("cache", "device"):
+        raise ValueError('a quantised cache needs kvsrc "cache" or "device"')
+    for name, t in (("q_tgt", q_tgt), ("k_tgt", k_tgt), ("v_tgt", v_tgt), ("q_ref", q_ref), ("k_ref", k_ref),
+                    ("v_ref", v_ref), ("o_tgt", o_tgt), ("o_ref", o_ref), ("decision", decision)):
+        if t is not None:
+            _here(name, t)
+    if decision is not None and decision.dtype != torch.int32:
+        raise ValueError("decision must be an int32 device tensor")
+    fmt, n_ref, dev = _mx_format(k_mx), k_mx.shape[2], q_tgt.device
+    shp_t, shp_r = (B, H, n_tgt, D), (B, H, n_ref, D)
+    ref_queries = (kvsrc == "device" or qset == "all") and n_ref > 0
+    if o_tgt is None:
+        o_tgt = torch.empty(shp_t, dtype=dt, device=dev)
+    if ref_queries and o_ref is None:
+        o_ref = torch.empty(shp_r, dtype=dt, device=dev)
+
+    def opt(name, flag, shape):
+        if flag is None or flag is False:
+            return None
+        return _f32_out(name, None if flag is True else flag, shape, dev)
+
+    mass_t = opt("ref_mass", ref_mass, (B, H, n_tgt))
+    lse_t = opt("lse", lse, (B, H, n_tgt, 2))
+    mrq_t = opt("ref_mass_refq", ref_mass_refq, (B, H, n_ref)) if n_ref > 0 else None
+    desc = (B, H, D, n_ref, n_tgt, _DTYPES[dt], ctypes.c_float(float(scale)).value if scale else 0.0, _QSET[qset],
+            _KVSRC[kvsrc])
+    if workspace is None:
+        nbytes = L.refadapt_joint_attn_mx_workspace_size(L.ra_attn_desc(*desc), _MX[fmt], q_mx is not None)
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    else:
+        _here("workspace", workspace)
+    word = lambda t: 0 if t is None else t.data_ptr()
+    args = L.ARGS_PACK.pack(
+        *_quad("q_tgt", q_tgt, dt, shp_t), *_quad("k_tgt", k_tgt, dt, shp_t), *_quad("v_tgt", v_tgt, dt, shp_t),
+        *_quad("q_ref", q_ref, dt, shp_r), *_quad("k_ref", k_ref, dt, shp_r), *_quad("v_ref", v_ref, dt, shp_r),
+        *_NO_TENSOR, *_NO_TENSOR, word(decision), *_quad("o_tgt", o_tgt, dt, shp_t), *_quad("o_ref", o_ref, dt, shp_r),
+        word(mass_t), word(lse_t), word(mrq_t), word(workspace), _nbytes(workspace), *_NO_SEG_FIELDS, 0, *_NO_TENSOR,
+        0 if clock_probe is None else _probe_ptr(clock_probe),
+    )
+    cache = L.MX_CACHE_PACK.pack(_MX[fmt], *_oct("k_mx", k_mx, fmt, shp_r), *_oct("v_mx", v_mx, fmt, shp_r),
+                                 *_oct("q_mx", q_mx, fmt, shp_r))
+    L.refadapt_joint_attn_mx_packed(L.DESC_PACK.pack(*desc), args, cache, _stream())
+    return AttnOut(o_tgt, o_ref if ref_queries else None, mass_t, lse_t, mrq_t)
+
+
+def attn_mx_workspace(q_tgt, n_ref, fmt, qset="target", kvsrc="cache", q_cached=False):
+    """Preallocated workspace of ``joint_attn_mx`` calls of this shape (``q_cached``: with ``q_mx``)."""
+    B, H, n_tgt, D = q_tgt.shape
+    desc = L.ra_attn_desc(B, H, D, n_ref, n_tgt, _DTYPES[q_tgt.dtype], 0.0, _QSET[qset], _KVSRC[kvsrc])
+    with torch.cuda.device(q_tgt.device):
+        nbytes = L.refadapt_joint_attn_mx_workspace_size(desc, _MX[fmt], q_cached)
+    return torch.empty(nbytes, dtype=torch.uint8, device=q_tgt.device)
+
+
 def mfma_rate_probe(kind, operands, steps, workgroups=None, sink=None, clock_probe=None):
     """Runs ``refadapt_mfma_rate_probe`` (``kind`` "dense" or "mix") on the current stream and
     returns the sink. ``operands``: a device tensor of at least ``RA_PROBE_OPERAND_BYTES``
