@@ -89,6 +89,15 @@ ra_status check_attn_desc(const ra_attn_desc* desc, const char* who) {
   return RA_OK;
 }
 
+float softmax_scale(const ra_attn_desc& d) { return d.scale > 0.f ? d.scale : 1.0f / std::sqrt((float)d.head_dim); }
+
+ra_status check_kv_stride(const char* name, const ra_tensor& t) {
+  if (t.stride_s > kAttnMaxRowStride)
+    return fail(RA_EUNSUPPORTED, "joint_attn: %s row stride %lld exceeds %lld elements", name, (long long)t.stride_s,
+                (long long)kAttnMaxRowStride);
+  return RA_OK;
+}
+
 ra_status launch_status(hipError_t e, const char* what) {
   if (e != hipSuccess) return fail(RA_ELAUNCH, "%s: %s", what, hipGetErrorString(e));
   return ok();
@@ -180,9 +189,7 @@ ra_status joint_attn(const ra_attn_desc* desc, const ra_attn_args* args, void* s
     const char* kv_name[] = {"k_tgt", "v_tgt", "k_ref", "v_ref", "k_cache", "v_cache"};
     const bool used[] = {true, true, reads_fresh, reads_fresh, reads_cache, reads_cache};
     for (int i = 0; i < 6; ++i)
-      if (used[i] && kv[i]->stride_s > kAttnMaxRowStride)
-        return fail(RA_EUNSUPPORTED, "joint_attn: %s row stride %lld exceeds %lld elements", kv_name[i],
-                    (long long)kv[i]->stride_s, (long long)kAttnMaxRowStride);
+      if (used[i] && (s = check_kv_stride(kv_name[i], *kv[i])) != RA_OK) return s;
   }
   if (d.kvsrc == RA_KV_SEGMENTS && reads_fresh && reads_cache) {
     const auto same = [](const ra_tensor& x, const ra_tensor& y) {
@@ -216,8 +223,7 @@ ra_status joint_attn(const ra_attn_desc* desc, const ra_attn_args* args, void* s
   // With no reference rows there is nothing to choose between: read the (empty) fresh segment.
   p.kvsrc = d.n_ref == 0 ? RA_KV_FRESH : d.kvsrc;
   if (d.n_ref == 0 && device) p.kvsrc = RA_KV_FRESH;
-  const float scale = d.scale > 0.f ? d.scale : 1.0f / std::sqrt((float)d.head_dim);
-  p.sc_log2 = scale * 1.4426950408889634f;
+  p.sc_log2 = softmax_scale(d) * 1.4426950408889634f;
 
   if (seg) {
     p.n_seg = a.n_seg;
@@ -607,8 +613,33 @@ ra_status mx_set(MxSet* ms, const ra_tensor* const plain[3], const char* const p
   return RA_OK;
 }
 
-// Workspace of the attention over a quantised cache: its K, V (and Q) in the run dtype, then the workspace of
-// refadapt_joint_attn.
+// Attention over a quantised cache takes one of two ways. Up to kFewMaxRows target rows a kernel reads the codes
+// itself; other calls read the cache back into the workspace and attend over that with refadapt_joint_attn's kernels.
+constexpr int kFewMaxRows = 256;
+
+bool few_rows(const ra_attn_desc& d) {
+  return d.dtype == RA_BF16 && d.kvsrc == RA_KV_CACHE && d.n_ref > 0 && !launch_mode(d, false).all &&
+         d.n_tgt <= kFewMaxRows;
+}
+
+// Key ranges of a few-rows launch: as many as fill the CUs, with a tile for every wavefront.
+struct FewPlan {
+  int64_t q_tiles, chunks, rows;  // rows: of partial results
+  size_t o_bytes(int head_dim) const { return (size_t)rows * head_dim * sizeof(float); }
+  size_t bytes(int head_dim) const { return o_bytes(head_dim) + (size_t)rows * 5 * sizeof(float); }
+};
+
+FewPlan few_plan(const ra_attn_desc& d) {
+  const int64_t bh = (int64_t)d.batch * d.heads, cus = attn_bf16_slots(d.head_dim, kAttnBf16BM).cus;
+  FewPlan f{};
+  f.q_tiles = (d.n_tgt + kFewRows - 1) / kFewRows;
+  const int64_t nt = ((int64_t)d.n_ref + kFewKeys - 1) / kFewKeys + (d.n_tgt + kFewKeys - 1) / kFewKeys;
+  f.chunks = std::max<int64_t>(1, std::min(cus / (bh * f.q_tiles), (nt + kFewWaves - 1) / kFewWaves));
+  f.rows = f.chunks > 1 ? bh * f.q_tiles * f.chunks * kFewRows : 0;
+  return f;
+}
+
+// Workspace of the other way: the cache's K, V (and Q) in the run dtype, then that of refadapt_joint_attn.
 struct MxAttnSpace {
   size_t tensor;  // bytes of one tensor, in whole 256-byte units
   int tensors;
@@ -625,6 +656,45 @@ MxAttnSpace mx_attn_space(const ra_attn_desc& d, bool with_q) {
   }
   s.inner = refadapt_joint_attn_workspace_size(&d);
   return s;
+}
+
+ra_status joint_attn_mx_few(const ra_attn_desc& d, const ra_attn_args& a, const ra_mx_cache& c, void* stream) {
+  ra_status s;
+  const ra_tensor* const t[4] = {&a.q_tgt, &a.k_tgt, &a.v_tgt, &a.o_tgt};
+  const char* const name[4] = {"q_tgt", "k_tgt", "v_tgt", "o_tgt"};
+  for (int i = 0; i < 4; ++i) {
+    if ((s = check_tensor(name[i], *t[i], d.dtype, d.n_tgt, d.head_dim)) != RA_OK) return s;
+    if ((i == 1 || i == 2) && (s = check_kv_stride(name[i], *t[i])) != RA_OK) return s;
+  }
+  const FewPlan f = few_plan(d);
+  MxFewParams p{};
+  if (const size_t need = f.bytes(d.head_dim); need > 0) {
+    if (a.workspace == nullptr || a.workspace_bytes < need)
+      return fail(RA_EWORKSPACE, "joint_attn_mx: workspace needs %zu bytes (got %zu)", need,
+                  a.workspace ? a.workspace_bytes : 0);
+    if ((reinterpret_cast<uintptr_t>(a.workspace) & 15) != 0)
+      return fail(RA_EUNSUPPORTED, "joint_attn_mx: workspace must be 16-byte aligned");
+    char* const ws = static_cast<char*>(a.workspace);
+    p.part_o = reinterpret_cast<float*>(ws);
+    p.part_st = reinterpret_cast<float4*>(ws + f.o_bytes(d.head_dim));
+    p.part_lo = reinterpret_cast<float*>(p.part_st + f.rows);
+  }
+  p.q = view(a.q_tgt);
+  p.k_tgt = view(a.k_tgt);
+  p.v_tgt = view(a.v_tgt);
+  p.o = view(a.o_tgt);
+  p.k = mx_view(c.k);
+  p.v = mx_view(c.v);
+  p.mass = a.ref_mass;
+  p.lse = a.lse_tgt;
+  p.B = d.batch;
+  p.H = d.heads;
+  p.n_ref = d.n_ref;
+  p.n_tgt = d.n_tgt;
+  p.q_tiles = (int32_t)f.q_tiles;
+  p.chunks = (int32_t)f.chunks;
+  p.sc_log2 = softmax_scale(d) * 1.4426950408889634f;
+  return launch_status(launch_attn_mx_few(p, c.format, d.head_dim, static_cast<hipStream_t>(stream)), "joint_attn_mx");
 }
 
 ra_status check_mx_attn(const char* who, const ra_attn_desc* desc, int32_t format) {
@@ -676,6 +746,7 @@ ra_status refadapt_mx_read(int32_t batch, int32_t heads, int32_t n_ref, int32_t 
 
 size_t refadapt_joint_attn_mx_workspace_size(const ra_attn_desc* desc, int32_t format, int32_t with_q) {
   if (check_mx_attn("joint_attn_mx_workspace_size", desc, format) != RA_OK) return 0;
+  if (few_rows(*desc)) return few_plan(*desc).bytes(desc->head_dim);
   return mx_attn_space(*desc, with_q != 0).total();
 }
 
@@ -697,6 +768,7 @@ ra_status refadapt_joint_attn_mx(const ra_attn_desc* desc, const ra_attn_args* a
   const int n = with_q ? 3 : 2;
   for (int i = 0; i < n; ++i)
     if ((s = check_mx(mx_name[i], *mx[i], c.format, d.n_ref, d.head_dim)) != RA_OK) return s;
+  if (few_rows(d)) return joint_attn_mx_few(d, a, c, stream);
   const MxAttnSpace space = mx_attn_space(d, with_q);
   if (a.workspace == nullptr || a.workspace_bytes < space.total())
     return fail(RA_EWORKSPACE, "joint_attn_mx: workspace needs %zu bytes (got %zu)", space.total(),

@@ -1,0 +1,424 @@
+// Joint attention of few target rows over a quantised reference cache (bf16, gfx950).
+//
+// Few query rows over a long cache are bound by reading it, so this kernel reads codes and
+// scales and nothing in between: against reading the cache back to memory and attending over that, 0.53 (1.03)
+// bytes an element instead of 4.5 (5) of them. Many rows share each K/V tile over many more products, and
+// converting it once per tile of 32 rows costs more than converting it once altogether: those calls read
+// back (the rule stands at few_rows in api.hip).
+//
+// One workgroup is 8 wavefronts that share 32 query rows of one (batch, head) and a range of its key
+// tiles (32 keys, reference first); wavefront w takes every eighth tile. As in attn_bf16.hip scores are formed
+// transposed, S^T = K Q^T with v_mfma_f32_32x32x16_bf16, and P^T feeds O^T += V^T P^T from registers.
+// A code-to-bf16 conversion instruction yields two elements that share a block's scale, which are neighbours
+// along the head dim, as the K operand needs them: K goes from memory to registers to the matrix core. (The
+// product sums over the head dim, whose order is free: lane half g takes elements 32 (2 i + g) .. + 31, one block,
+// of K and of Q alike.) V needs neighbours along the keys: its bf16 pairs pass through a
+// wavefront's own 8 KiB of LDS (no barrier: one wavefront's LDS operations are served in order) and return through
+// the transpose read. The next tile's codes are in flight while a tile is worked on.
+//
+// Statistics: the running maximum m moves only when a score exceeds it by 2^8 (in the exponents of 2: the terms stay below
+// 2^8, far from any limit of fp32); sums are fp32; o is divided by the sum of the probabilities rounded to bf16, as they
+// multiply V, the mass and the log-sum-exp by that of the unrounded ones. At the last reference tile (m, l)
+// freeze as (m_R, l_R). The wavefronts' partial results meet in LDS; where key ranges are split over
+// workgroups, those of the workgroups in the workspace and the merge kernel, in a fixed order.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "internal.h"
+#include "mxcodes.h"
+
+namespace refadapt {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+
+constexpr int KT = kFewKeys;     // keys per tile
+constexpr int BM = kFewRows;     // query rows per workgroup
+constexpr int NW = kFewWaves;    // wavefronts per workgroup
+constexpr float LOWEST = -3.0e38f;  // stands for -inf in a running maximum: differences stay defined
+constexpr float SLACK = 8.0f;       // a maximum moves when it is exceeded by this exponent of 2
+
+// Key of A-row m: with it register r of lane half g holds key 16 (r / 8) + 8 g + r % 8 of the
+// tile, the order of the B operand (P^T) of the second product.
+__device__ __forceinline__ int sigma(int m) { return (m & ~12) | ((m & 4) << 1) | ((m & 8) >> 1); }
+
+__device__ __forceinline__ float xor32(float v, int op) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  const float a = __uint_as_float(r[0]), b = __uint_as_float(r[1]);
+  return op ? fmaxf(a, b) : a + b;
+}
+
+// A tile's operands as loaded: KIND 0 e2m1 codes, 1 e4m3 codes, 2 bf16.
+template <int D, int KIND>
+struct Tile {
+  static constexpr int NI = D / 64;                                // blocks of 32 of a lane's K row
+  static constexpr int KW = KIND == 0 ? 1 : KIND == 1 ? 2 : 4;     // 16-byte loads of such a block
+  static constexpr int NV = D / 32;                                // pieces of 16 elements of V a lane takes
+  static constexpr int VW = KIND == 0 ? 2 : KIND == 1 ? 4 : 8;     // words of such a piece
+  u32x4 k[NI][KW];
+  uint32_t ks[NI];
+  uint32_t v[NV][VW];
+  uint32_t vs[NV];
+};
+
+// Rows past the last repeat it: their scores are masked, their values multiply zeros.
+template <int D, int KIND>
+__device__ __forceinline__ void load_tile(Tile<D, KIND>& t, const MxView& k, const MxView& v, int key0, int n_keys,
+                                          int lane) {
+  using T = Tile<D, KIND>;
+  const int g = lane >> 5, n = lane & 31;
+  constexpr int row_bytes = 2 * T::KW;  // of four elements
+  const int64_t kr = min(key0 + sigma(n), n_keys - 1);
+  const uint8_t* kp = k.codes + kr * k.ss;
+#pragma unroll
+  for (int i = 0; i < T::NI; ++i) {
+#pragma unroll
+    for (int j = 0; j < T::KW; ++j)
+      t.k[i][j] = *reinterpret_cast<const u32x4*>(kp + (2 * i + g) * 8 * row_bytes + 16 * j);
+    if constexpr (KIND != 2) t.ks[i] = k.scales[kr * k.es + 2 * i + g];
+  }
+#pragma unroll
+  for (int i = 0; i < T::NV; ++i) {
+    const int s2 = i / (D / 64), db = 2 * (i % (D / 64)) + g;
+    const int64_t vr = min(key0 + 16 * s2 + ((lane >> 1) & 15), n_keys - 1);
+    const uint8_t* vp = v.codes + vr * v.ss + (2 * db + (lane & 1)) * 4 * row_bytes;
+    if constexpr (KIND == 0) {
+      const u32x2 w = *reinterpret_cast<const u32x2*>(vp);
+      t.v[i][0] = w[0];
+      t.v[i][1] = w[1];
+    } else {
+#pragma unroll
+      for (int j = 0; j < T::VW / 4; ++j) {
+        const u32x4 w = reinterpret_cast<const u32x4*>(vp)[j];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t.v[i][4 * j + e] = w[e];
+      }
+    }
+    if constexpr (KIND != 2) t.vs[i] = v.scales[vr * v.es + db];
+  }
+}
+
+// Elements 8 s .. 8 s + 7 of a K block.
+template <int D, int KIND>
+__device__ __forceinline__ bf16x8 k_operand(const Tile<D, KIND>& t, int i, int s) {
+  u32x4 w;
+  if constexpr (KIND == 0) w = decode_oct<true>(u32x2{t.k[i][0][s], 0u}, t.ks[i]);
+  if constexpr (KIND == 1) w = decode_oct<false>(u32x2{t.k[i][s >> 1][2 * (s & 1)], t.k[i][s >> 1][2 * (s & 1) + 1]}, t.ks[i]);
+  if constexpr (KIND == 2) w = t.k[i][s];
+  return __builtin_bit_cast(bf16x8, w);
+}
+
+// Puts the tile's V into LDS as blocks of 16 keys x 32 dims (1 KiB; 64 bytes a key, its halves swapped where
+// bit 1 of the key is set, which keeps the transpose reads free of bank conflicts).
+template <int D, int KIND>
+__device__ __forceinline__ void store_v(uint16_t* lds, const Tile<D, KIND>& t, int lane) {
+  using T = Tile<D, KIND>;
+  const int r = (lane >> 1) & 15;
+#pragma unroll
+  for (int i = 0; i < T::NV; ++i) {
+    const int s2 = i / (D / 64), db = 2 * (i % (D / 64)) + (lane >> 5);
+    uint16_t* p = lds + 512 * ((D / 32) * s2 + db) + 32 * r + 16 * ((lane & 1) ^ ((r >> 1) & 1));
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      u32x4 w;
+      if constexpr (KIND == 0) w = decode_oct<true>(u32x2{t.v[i][j], 0u}, t.vs[i]);
+      if constexpr (KIND == 1) w = decode_oct<false>(u32x2{t.v[i][2 * j], t.v[i][2 * j + 1]}, t.vs[i]);
+      if constexpr (KIND == 2) w = u32x4{t.v[i][4 * j], t.v[i][4 * j + 1], t.v[i][4 * j + 2], t.v[i][4 * j + 3]};
+      *reinterpret_cast<u32x4*>(p + 8 * j) = w;
+    }
+  }
+}
+
+__device__ __forceinline__ void lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Mass and log-sum-exp of one row from its statistics: sums of the reference keys against 2^M_R, of the target keys
+// against 2^M (M_R <= M: a reference sum of zero has M_R = LOWEST).
+__device__ __forceinline__ void mx_few_stats(const MxFewParams& p, int64_t row, float M, float L_Y, float M_R,
+                                             float L_R) {
+  const float R = L_R > 0.f ? L_R * __builtin_amdgcn_exp2f(M_R - M) : L_R, total = R + L_Y;
+  if (p.mass) p.mass[row] = R / total;
+  if (p.lse) {
+    const float ln2 = 0.69314718055994531f;
+    p.lse[2 * row] = (M_R + __log2f(L_R)) * ln2;
+    p.lse[2 * row + 1] = (M + __log2f(total)) * ln2;
+  }
+}
+
+__device__ __forceinline__ void mx_few_store(const MxFewParams& p, int b, int h, int qr, int col, f32x4 acc, float lo) {
+  uint16_t* op = static_cast<uint16_t*>(const_cast<void*>(p.o.p)) + b * p.o.sb + h * p.o.sh + (int64_t)qr * p.o.ss;
+  const float inv = 1.f / lo;
+  bf16x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = (__bf16)(acc[i] * inv);
+  *reinterpret_cast<u32x2*>(op + col) = __builtin_bit_cast(u32x2, w);
+}
+
+constexpr int ORow(int d) { return d + 4; }  // floats of a row of O in LDS: the rows' starts spread over the banks
+
+template <int D>
+struct FewLds {
+  union {
+    uint16_t v[NW][KT * D];
+    float o[NW][BM][ORow(D)];
+  };
+  float m[NW][BM], l[NW][BM], m_ref[NW][BM], l_ref[NW][BM], lo[NW][BM];
+  float sum[BM];  // of the rounded probabilities of the workgroup's rows
+};
+
+template <int D, bool FP4>
+__global__ __launch_bounds__(64 * NW, 2) void attn_mx_few_kernel(MxFewParams p) {
+  constexpr int DB = D / 32, NI = D / 64;
+  constexpr int KIND = FP4 ? 0 : 1;
+  __shared__ __attribute__((aligned(1024))) FewLds<D> s;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 5, n = lane & 31;
+
+  // item: (batch, head), key range, query tile (fastest: its neighbours read the same keys)
+  const int item = xcd_remap(blockIdx.x, gridDim.x);
+  const int qt = item % p.q_tiles, range = item / p.q_tiles;
+  const int bh = range / p.chunks, chunk = range - bh * p.chunks;
+  const int b = bh / p.H, h = bh - b * p.H;
+  const int n_rt = (p.n_ref + KT - 1) / KT, nt = n_rt + (p.n_tgt + KT - 1) / KT;
+  const int j0 = (int)((int64_t)chunk * nt / p.chunks), j1 = (int)((int64_t)(chunk + 1) * nt / p.chunks);
+
+  MxView kc = p.k, vc = p.v;
+  kc.codes += b * kc.sb + h * kc.sh;
+  kc.scales += b * kc.eb + h * kc.eh;
+  vc.codes += b * vc.sb + h * vc.sh;
+  vc.scales += b * vc.eb + h * vc.eh;
+  const auto plain = [&](const View& v) {
+    return MxView{static_cast<uint8_t*>(const_cast<void*>(v.p)) + 2 * (b * v.sb + h * v.sh), 0, 0, 2 * v.ss, nullptr, 0,
+                  0, 0};
+  };
+  const MxView ky = plain(p.k_tgt), vy = plain(p.v_tgt);
+
+  const int qrow = qt * BM + n;
+  bf16x8 q[NI][4];
+  {
+    const uint16_t* qp = static_cast<const uint16_t*>(p.q.p) + b * p.q.sb + h * p.q.sh + (int64_t)qrow * p.q.ss;
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const u32x4 w = qrow < p.n_tgt ? *reinterpret_cast<const u32x4*>(qp + 64 * i + 32 * g + 8 * t) : u32x4{0, 0, 0, 0};
+        q[i][t] = __builtin_bit_cast(bf16x8, w);
+      }
+  }
+
+  f32x16 o[DB];
+#pragma unroll
+  for (int i = 0; i < DB; ++i) o[i] = f32x16{};
+  float m = LOWEST, l = 0.f, lo = 0.f, m_ref = LOWEST, l_ref = 0.f;  // l, lo: this lane's half of the keys
+  uint16_t* const lds = s.v[wave];
+  const int tr_i = lane & 15, tr_G = lane >> 4;
+  const int v_lane =
+      32 * (8 * (tr_G >> 1) + (tr_i >> 2)) + ((16 * (tr_G & 1) + 4 * (tr_i & 3)) ^ (16 * ((tr_i >> 3) & 1)));
+
+  const auto work = [&](const auto& t, int valid) __attribute__((always_inline)) {
+    lds_order();
+    store_v(lds, t, lane);
+    lds_order();
+    f32x16 sc{};
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(t, i, e), q[i][e], sc, 0, 0, 0);
+    if (valid < KT) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (16 * (r >> 3) + 8 * g + (r & 7) >= valid) sc[r] = -__builtin_inff();
+    }
+    float mx = sc[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
+    mx = xor32(mx, 1) * p.sc_log2;
+    if (__any(mx > m + SLACK)) {
+      const float m_new = fmaxf(m, mx), a = __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= a;
+      lo *= a;
+#pragma unroll
+      for (int i = 0; i < DB; ++i) o[i] *= a;
+    }
+    uint32_t pw[8];
+    float sum = 0.f, lsum = 0.f;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[2 * r], p.sc_log2, -m));
+      const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[2 * r + 1], p.sc_log2, -m));
+      sum += e0 + e1;
+      bf16x2 w;
+      w[0] = (__bf16)e0;
+      w[1] = (__bf16)e1;
+      pw[r] = __builtin_bit_cast(uint32_t, w);
+      lsum = __builtin_amdgcn_fdot2_f32_bf16(w, bf16x2{(__bf16)1.f, (__bf16)1.f}, lsum, false);
+    }
+    l += sum;
+    lo += lsum;
+#pragma unroll
+    for (int i = 0; i < 2 * DB; ++i) {
+      const uint16_t* a = lds + v_lane + 512 * i;
+      const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(a));
+      const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(a + 128));
+      const u32x4 w = {pw[4 * (i / DB)], pw[4 * (i / DB) + 1], pw[4 * (i / DB) + 2], pw[4 * (i / DB) + 3]};
+      o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7),
+                                                          __builtin_bit_cast(bf16x8, w), o[i % DB], 0, 0, 0);
+    }
+  };
+
+  // reference tiles j0 + wave, + NW, ...; then the target tiles that follow in that order
+  int j = j0 + wave;
+  const int jr = min(j1, n_rt);
+  if (j < jr) {
+    Tile<D, KIND> cur, next;
+    load_tile(cur, kc, vc, j * KT, p.n_ref, lane);
+    for (; j < jr; j += NW) {
+      if (j + NW < jr) load_tile(next, kc, vc, (j + NW) * KT, p.n_ref, lane);
+      work(cur, p.n_ref - j * KT);
+      cur = next;
+    }
+  }
+  m_ref = m;
+  l_ref = l;
+  l = 0.f;
+  for (; j < j1; j += NW) {
+    Tile<D, 2> t;
+    load_tile(t, ky, vy, (j - n_rt) * KT, p.n_tgt, lane);
+    work(t, p.n_tgt - (j - n_rt) * KT);
+  }
+
+  // ---- the wavefronts' results, against the largest of their maxima
+  l = xor32(l, 0);
+  l_ref = xor32(l_ref, 0);
+  lo = xor32(lo, 0);
+  if (g == 0) {
+    s.m[wave][n] = m;
+    s.l[wave][n] = l;
+    s.m_ref[wave][n] = m_ref;
+    s.l_ref[wave][n] = l_ref;
+    s.lo[wave][n] = lo;
+  }
+  __syncthreads();  // also: every wavefront is done with its V
+  float M = LOWEST;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) M = fmaxf(M, s.m[w][n]);
+  const float a = __builtin_amdgcn_exp2f(m - M);
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int rr = 0; rr < 4; ++rr)
+      *reinterpret_cast<f32x4*>(&s.o[wave][n][32 * db + 8 * rr + 4 * g]) =
+          f32x4{o[db][4 * rr] * a, o[db][4 * rr + 1] * a, o[db][4 * rr + 2] * a, o[db][4 * rr + 3] * a};
+  const bool split = p.chunks > 1;
+  if (threadIdx.x < BM) {
+    float M_R = LOWEST, L_R = 0.f, L_Y = 0.f, L_o = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) M_R = s.l_ref[w][n] > 0.f ? fmaxf(M_R, s.m_ref[w][n]) : M_R;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float e = __builtin_amdgcn_exp2f(s.m[w][n] - M);
+      L_R += s.l_ref[w][n] * __builtin_amdgcn_exp2f(s.m_ref[w][n] - M_R);
+      L_Y += s.l[w][n] * e;
+      L_o += s.lo[w][n] * e;
+    }
+    s.sum[n] = L_o;
+    if (qrow < p.n_tgt) {
+      if (split) {
+        const int64_t row = (int64_t)item * BM + n;
+        p.part_st[row] = float4{M, L_Y, M_R, L_R};
+        p.part_lo[row] = L_o;
+      } else {
+        mx_few_stats(p, (int64_t)bh * p.n_tgt + qrow, M, L_Y, M_R, L_R);
+      }
+    }
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < BM * (D / 4); e += 64 * NW) {
+    const int row = e / (D / 4), col = 4 * (e % (D / 4)), qr = qt * BM + row;
+    if (qr >= p.n_tgt) break;
+    f32x4 acc = *reinterpret_cast<const f32x4*>(&s.o[0][row][col]);
+#pragma unroll
+    for (int w = 1; w < NW; ++w) acc += *reinterpret_cast<const f32x4*>(&s.o[w][row][col]);
+    if (split)
+      *reinterpret_cast<f32x4*>(p.part_o + ((int64_t)item * BM + row) * D + col) = acc;
+    else
+      mx_few_store(p, b, h, qr, col, acc, s.sum[row]);
+  }
+}
+
+// One output row per D / 4 threads, four columns a thread; the key ranges in order.
+template <int D>
+__global__ __launch_bounds__(256) void attn_mx_merge_kernel(MxFewParams p) {
+  constexpr int TPR = D / 4, BATCH = 8;
+  const int64_t r = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+  const int col = 4 * (threadIdx.x % TPR);
+  const int64_t bh = r / p.n_tgt;
+  if (bh >= (int64_t)p.B * p.H) return;
+  const int qr = (int)(r - bh * p.n_tgt), qt = qr / BM, row = qr - qt * BM;
+  const auto at = [&](int c) { return (((bh * p.chunks + c) * p.q_tiles) + qt) * BM + row; };
+  float M = LOWEST, M_R = LOWEST;
+  for (int c0 = 0; c0 < p.chunks; c0 += BATCH) {
+    float4 st[BATCH];
+#pragma unroll
+    for (int u = 0; u < BATCH; ++u)
+      if (c0 + u < p.chunks) st[u] = p.part_st[at(c0 + u)];
+#pragma unroll
+    for (int u = 0; u < BATCH; ++u)
+      if (c0 + u < p.chunks) {
+        M = fmaxf(M, st[u].x);
+        if (st[u].w > 0.f) M_R = fmaxf(M_R, st[u].z);
+      }
+  }
+  float L_R = 0.f, L_Y = 0.f, L_o = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int c0 = 0; c0 < p.chunks; c0 += BATCH) {
+    float4 st[BATCH];
+    float lo[BATCH];
+    f32x4 o[BATCH];
+#pragma unroll
+    for (int u = 0; u < BATCH; ++u)
+      if (c0 + u < p.chunks) {
+        st[u] = p.part_st[at(c0 + u)];
+        lo[u] = p.part_lo[at(c0 + u)];
+        o[u] = *reinterpret_cast<const f32x4*>(p.part_o + at(c0 + u) * D + col);
+      }
+#pragma unroll
+    for (int u = 0; u < BATCH; ++u)
+      if (c0 + u < p.chunks) {
+        const float e = __builtin_amdgcn_exp2f(st[u].x - M);
+        L_Y += st[u].y * e;
+        L_o += lo[u] * e;
+        L_R += st[u].w * __builtin_amdgcn_exp2f(st[u].z - M_R);
+        acc += o[u] * e;
+      }
+  }
+  const int b = (int)(bh / p.H), h = (int)(bh - (int64_t)b * p.H);
+  mx_few_store(p, b, h, qr, col, acc, L_o);
+  if (col == 0) mx_few_stats(p, r, M, L_Y, M_R, L_R);
+}
+
+template <int D>
+hipError_t launch(const MxFewParams& p, int format, hipStream_t stream) {
+  const dim3 grid((unsigned)((int64_t)p.B * p.H * p.chunks * p.q_tiles));
+  const hipError_t e = format == MX_FP4
+                           ? launch_kernel(attn_mx_few_kernel<D, true>, grid, dim3(64 * NW), 0, stream, p)
+                           : launch_kernel(attn_mx_few_kernel<D, false>, grid, dim3(64 * NW), 0, stream, p);
+  if (e != hipSuccess || p.chunks == 1) return e;
+  const int64_t rows = (int64_t)p.B * p.H * p.n_tgt, per = 256 / (D / 4);
+  return launch_kernel(attn_mx_merge_kernel<D>, dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, stream, p);
+}
+
+}  // namespace
+
+hipError_t launch_attn_mx_few(const MxFewParams& p, int format, int head_dim, hipStream_t stream) {
+  return head_dim == 128 ? launch<128>(p, format, stream) : launch<64>(p, format, stream);
+}
+
+}  // namespace refadapt

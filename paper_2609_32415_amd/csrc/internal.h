@@ -137,6 +137,25 @@ hipError_t launch_mx_commit(int dtype, int format, int32_t B, int32_t H, int32_t
 hipError_t launch_mx_read(int dtype, int format, int32_t B, int32_t H, int32_t n_ref, int32_t head_dim,
                           const MxSet& ms, const int32_t* decision, int32_t always, hipStream_t stream);
 
+// bf16 attention of few target rows over a quantised cache: workgroups of kFewWaves wavefronts and kFewRows query
+// rows, key tiles of kFewKeys, the keys of a (batch, head) in `chunks` ranges.
+constexpr int kFewRows = 32;
+constexpr int kFewKeys = 32;
+constexpr int kFewWaves = 8;
+struct MxFewParams {
+  View q, k_tgt, v_tgt, o;  // target rows; o is written through const_cast
+  MxView k, v;              // the cached reference
+  float* mass;              // [B, H, n_tgt] or null
+  float* lse;               // [B, H, n_tgt, 2] or null
+  int32_t B, H, n_ref, n_tgt;
+  int32_t q_tiles, chunks;
+  float sc_log2;    // softmax scale * log2(e)
+  float* part_o;    // chunks > 1: [B * H][chunks][q_tiles][kFewRows][d] unnormalised outputs,
+  float4* part_st;  // (m, l_Y, m_R, l_R)
+  float* part_lo;   // and the sums of the rounded probabilities
+};
+hipError_t launch_attn_mx_few(const MxFewParams& p, int format, int head_dim, hipStream_t stream);
+
 // Rotary positions of up to two [B, H, S, d] tensors. The tables travel in the kernel arguments.
 constexpr int kRopeMaxPairs = 128;
 struct RopeParams {
