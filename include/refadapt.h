@@ -446,7 +446,8 @@ typedef struct {
  * with_q) bytes, 16-byte aligned (with_q: cache->q is given); it needs no
  * initialisation and must not be used by another call that runs concurrently.
  * Errors: as refadapt_joint_attn; RA_EUNSUPPORTED for other K/V sources,
- * seg_mass, and as refadapt_mx_commit for the cache; RA_EWORKSPACE for a missing
+ * seg_mass, row strides of codes or scales above 2^24 - 8 bytes, and as
+ * refadapt_mx_commit for the cache; RA_EWORKSPACE for a missing
  * or smaller workspace.
  */
 size_t refadapt_joint_attn_mx_workspace_size(const ra_attn_desc* desc, int32_t format, int32_t with_q);

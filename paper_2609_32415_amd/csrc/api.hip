@@ -658,6 +658,14 @@ MxAttnSpace mx_attn_space(const ra_attn_desc& d, bool with_q) {
   return s;
 }
 
+// Both ways take the same views: key tiles are addressed with 32-bit offsets.
+ra_status check_mx_stride(const char* name, const ra_mx_tensor& t) {
+  if (t.stride_s > kAttnMaxRowStride || t.scale_stride_s > kAttnMaxRowStride)
+    return fail(RA_EUNSUPPORTED, "joint_attn_mx: %s row strides %lld and %lld exceed %lld bytes", name,
+                (long long)t.stride_s, (long long)t.scale_stride_s, (long long)kAttnMaxRowStride);
+  return RA_OK;
+}
+
 ra_status joint_attn_mx_few(const ra_attn_desc& d, const ra_attn_args& a, const ra_mx_cache& c, void* stream) {
   ra_status s;
   const ra_tensor* const t[4] = {&a.q_tgt, &a.k_tgt, &a.v_tgt, &a.o_tgt};
@@ -767,7 +775,9 @@ ra_status refadapt_joint_attn_mx(const ra_attn_desc* desc, const ra_attn_args* a
   const char* const mx_name[3] = {"k_mx", "v_mx", "q_mx"};
   const int n = with_q ? 3 : 2;
   for (int i = 0; i < n; ++i)
-    if ((s = check_mx(mx_name[i], *mx[i], c.format, d.n_ref, d.head_dim)) != RA_OK) return s;
+    if ((s = check_mx(mx_name[i], *mx[i], c.format, d.n_ref, d.head_dim)) != RA_OK ||
+        (s = check_mx_stride(mx_name[i], *mx[i])) != RA_OK)
+      return s;
   if (few_rows(d)) return joint_attn_mx_few(d, a, c, stream);
   const MxAttnSpace space = mx_attn_space(d, with_q);
   if (a.workspace == nullptr || a.workspace_bytes < space.total())

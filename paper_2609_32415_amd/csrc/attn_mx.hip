@@ -16,8 +16,8 @@
 // wavefront's own 8 KiB of LDS (no barrier: one wavefront's LDS operations are served in order) and return through
 // the transpose read. The next tile's codes are in flight while a tile is worked on.
 //
-// Statistics: the running maximum m moves only when a score exceeds it by 2^8 (in the exponents of 2: the terms stay below
-// 2^8, far from any limit of fp32); sums are fp32; o is divided by the sum of the probabilities rounded to bf16, as they
+// Statistics: probabilities are formed against a running maximum m that moves only when a lane's sum of them passes
+// 2^12; sums are fp32; o is divided by the sum of the probabilities rounded to bf16, as they
 // multiply V, the mass and the log-sum-exp by that of the unrounded ones. At the last reference tile (m, l)
 // freeze as (m_R, l_R). The wavefronts' partial results meet in LDS; where key ranges are split over
 // workgroups, those of the workgroups in the workspace and the merge kernel, in a fixed order.
@@ -40,7 +40,7 @@ constexpr int KT = kFewKeys;     // keys per tile
 constexpr int BM = kFewRows;     // query rows per workgroup
 constexpr int NW = kFewWaves;    // wavefronts per workgroup
 constexpr float LOWEST = -3.0e38f;  // stands for -inf in a running maximum: differences stay defined
-constexpr float SLACK = 8.0f;       // a maximum moves when it is exceeded by this exponent of 2
+constexpr float BOUND = 4096.0f;    // on a probability against the running maximum
 
 // Key of A-row m: with it register r of lane half g holds key 16 (r / 8) + 8 g + r % 8 of the
 // tile, the order of the B operand (P^T) of the second product.
@@ -59,46 +59,82 @@ struct Tile {
   static constexpr int KW = KIND == 0 ? 1 : KIND == 1 ? 2 : 4;     // 16-byte loads of such a block
   static constexpr int NV = D / 32;                                // pieces of 16 elements of V a lane takes
   static constexpr int VW = KIND == 0 ? 2 : KIND == 1 ? 4 : 8;     // words of such a piece
+  static constexpr int ROW = D / 2 * KW;                           // bytes of a row
   u32x4 k[NI][KW];
   uint32_t ks[NI];
   uint32_t v[NV][VW];
   uint32_t vs[NV];
 };
 
-// Rows past the last repeat it: their scores are masked, their values multiply zeros.
+// One K or V stream: the rows of a (batch, head), read tile by tile through a buffer resource, so that a lane's
+// offsets within a tile never change and rows past the last read as zeros (their scores are masked, and
+// zeros under scale byte 0 are zeros).
+struct Stream {
+  const uint8_t* codes;
+  const uint8_t* scales;
+  int32_t ss, es;  // row strides, bytes (the host holds a tile's rows to 32-bit offsets)
+  int32_t n_keys;
+};
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const uint8_t* base, int32_t stride, int row0, int valid,
+                                                            int row_bytes) {
+  const uint64_t a = reinterpret_cast<uint64_t>(base) + (uint64_t)((int64_t)row0 * stride);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
+  const int nbytes = __builtin_amdgcn_readfirstlane((valid - 1) * stride + row_bytes);
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(((uint64_t)hi << 32) | lo), (short)0, nbytes,
+                                           0x00020000);
+}
+
+// A lane's byte offsets within a tile.
 template <int D, int KIND>
-__device__ __forceinline__ void load_tile(Tile<D, KIND>& t, const MxView& k, const MxView& v, int key0, int n_keys,
-                                          int lane) {
+struct LaneOffsets {
+  uint32_t k, ks, v, vs;  // its K row and block; the first of its V pieces
+  __device__ __forceinline__ LaneOffsets(const Stream& ks_, const Stream& vs_, int lane) {
+    using T = Tile<D, KIND>;
+    const int g = lane >> 5, row = sigma(lane & 31), vrow = (lane >> 1) & 15;
+    k = row * ks_.ss + g * 16 * T::KW;
+    ks = row * ks_.es + g;
+    v = vrow * vs_.ss + (2 * g + (lane & 1)) * 8 * T::KW;
+    vs = vrow * vs_.es + g;
+  }
+};
+
+template <int D, int KIND>
+__device__ __forceinline__ void load_tile(Tile<D, KIND>& t, const Stream& k, const Stream& v,
+                                          const LaneOffsets<D, KIND>& at, int key0) {
   using T = Tile<D, KIND>;
-  const int g = lane >> 5, n = lane & 31;
-  constexpr int row_bytes = 2 * T::KW;  // of four elements
-  const int64_t kr = min(key0 + sigma(n), n_keys - 1);
-  const uint8_t* kp = k.codes + kr * k.ss;
+  const int valid = min(KT, k.n_keys - key0);
+  const auto kr = rows_rsrc(k.codes, k.ss, key0, valid, T::ROW), vr = rows_rsrc(v.codes, v.ss, key0, valid, T::ROW);
 #pragma unroll
-  for (int i = 0; i < T::NI; ++i) {
+  for (int i = 0; i < T::NI; ++i)
 #pragma unroll
     for (int j = 0; j < T::KW; ++j)
-      t.k[i][j] = *reinterpret_cast<const u32x4*>(kp + (2 * i + g) * 8 * row_bytes + 16 * j);
-    if constexpr (KIND != 2) t.ks[i] = k.scales[kr * k.es + 2 * i + g];
-  }
+      t.k[i][j] = __builtin_amdgcn_raw_buffer_load_b128(kr, at.k + 32 * T::KW * i + 16 * j, 0, 0);
 #pragma unroll
-  for (int i = 0; i < T::NV; ++i) {
-    const int s2 = i / (D / 64), db = 2 * (i % (D / 64)) + g;
-    const int64_t vr = min(key0 + 16 * s2 + ((lane >> 1) & 15), n_keys - 1);
-    const uint8_t* vp = v.codes + vr * v.ss + (2 * db + (lane & 1)) * 4 * row_bytes;
+  for (int i = 0; i < T::NV; ++i) {  // keys 16 s2 .. + 15, block 2 d2 + g
+    const int s2 = i / (D / 64), d2 = i % (D / 64);
+    const uint32_t off = at.v + 32 * T::KW * d2;
     if constexpr (KIND == 0) {
-      const u32x2 w = *reinterpret_cast<const u32x2*>(vp);
+      const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(vr, off, 16 * s2 * v.ss, 0);
       t.v[i][0] = w[0];
       t.v[i][1] = w[1];
     } else {
 #pragma unroll
       for (int j = 0; j < T::VW / 4; ++j) {
-        const u32x4 w = reinterpret_cast<const u32x4*>(vp)[j];
+        const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(vr, off + 16 * j, 16 * s2 * v.ss, 0);
 #pragma unroll
         for (int e = 0; e < 4; ++e) t.v[i][4 * j + e] = w[e];
       }
     }
-    if constexpr (KIND != 2) t.vs[i] = v.scales[vr * v.es + db];
+  }
+  if constexpr (KIND != 2) {
+    const auto ke = rows_rsrc(k.scales, k.es, key0, valid, D / 32), ve = rows_rsrc(v.scales, v.es, key0, valid, D / 32);
+#pragma unroll
+    for (int i = 0; i < T::NI; ++i) t.ks[i] = __builtin_amdgcn_raw_buffer_load_b8(ke, at.ks + 2 * i, 0, 0);
+#pragma unroll
+    for (int i = 0; i < T::NV; ++i)
+      t.vs[i] = __builtin_amdgcn_raw_buffer_load_b8(ve, at.vs + 2 * (i % (D / 64)), 16 * (i / (D / 64)) * v.es, 0);
   }
 }
 
@@ -188,16 +224,13 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_mx_few_kernel(MxFewParams p) 
   const int n_rt = (p.n_ref + KT - 1) / KT, nt = n_rt + (p.n_tgt + KT - 1) / KT;
   const int j0 = (int)((int64_t)chunk * nt / p.chunks), j1 = (int)((int64_t)(chunk + 1) * nt / p.chunks);
 
-  MxView kc = p.k, vc = p.v;
-  kc.codes += b * kc.sb + h * kc.sh;
-  kc.scales += b * kc.eb + h * kc.eh;
-  vc.codes += b * vc.sb + h * vc.sh;
-  vc.scales += b * vc.eb + h * vc.eh;
-  const auto plain = [&](const View& v) {
-    return MxView{static_cast<uint8_t*>(const_cast<void*>(v.p)) + 2 * (b * v.sb + h * v.sh), 0, 0, 2 * v.ss, nullptr, 0,
-                  0, 0};
+  const auto cached = [&](const MxView& v) {
+    return Stream{v.codes + b * v.sb + h * v.sh, v.scales + b * v.eb + h * v.eh, (int32_t)v.ss, (int32_t)v.es, p.n_ref};
   };
-  const MxView ky = plain(p.k_tgt), vy = plain(p.v_tgt);
+  const auto plain = [&](const View& v) {
+    return Stream{static_cast<const uint8_t*>(v.p) + 2 * (b * v.sb + h * v.sh), nullptr, 2 * (int32_t)v.ss, 0, p.n_tgt};
+  };
+  const Stream kc = cached(p.k), vc = cached(p.v), ky = plain(p.k_tgt), vy = plain(p.v_tgt);
 
   const int qrow = qt * BM + n;
   bf16x8 q[NI][4];
@@ -231,35 +264,47 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_mx_few_kernel(MxFewParams p) 
 #pragma unroll
       for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(t, i, e), q[i][e], sc, 0, 0, 0);
     if (valid < KT) {
+      asm volatile("");  // a branch: as selects the mask costs every tile 30 instructions
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         if (16 * (r >> 3) + 8 * g + (r & 7) >= valid) sc[r] = -__builtin_inff();
     }
-    float mx = sc[0];
+    // Against the running maximum first: a lane's sum bounds each of its terms, so that a sum within 2^12 (NaN and
+    // infinity are not) lets the maximum stay.
+    uint32_t pw[8];
+    float sum;
+    const auto form = [&]() __attribute__((always_inline)) {
+      float part[2];
 #pragma unroll
-    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
-    mx = xor32(mx, 1) * p.sc_log2;
-    if (__any(mx > m + SLACK)) {
-      const float m_new = fmaxf(m, mx), a = __builtin_amdgcn_exp2f(m - m_new);
+      for (int r = 0; r < 8; ++r) {
+        const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[2 * r], p.sc_log2, -m));
+        const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[2 * r + 1], p.sc_log2, -m));
+        part[r & 1] = r < 2 ? e0 + e1 : part[r & 1] + (e0 + e1);
+        bf16x2 w;
+        w[0] = (__bf16)e0;
+        w[1] = (__bf16)e1;
+        pw[r] = __builtin_bit_cast(uint32_t, w);
+      }
+      sum = part[0] + part[1];
+    };
+    form();
+    if (__any(!(sum <= BOUND))) {  // rare, and always at a wavefront's first tile
+      float mx = sc[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
+      const float m_new = fmaxf(m, xor32(mx, 1) * p.sc_log2), a = __builtin_amdgcn_exp2f(m - m_new);
       m = m_new;
       l *= a;
       lo *= a;
 #pragma unroll
       for (int i = 0; i < DB; ++i) o[i] *= a;
+      form();
     }
-    uint32_t pw[8];
-    float sum = 0.f, lsum = 0.f;
+    float lsum = 0.f;
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[2 * r], p.sc_log2, -m));
-      const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[2 * r + 1], p.sc_log2, -m));
-      sum += e0 + e1;
-      bf16x2 w;
-      w[0] = (__bf16)e0;
-      w[1] = (__bf16)e1;
-      pw[r] = __builtin_bit_cast(uint32_t, w);
-      lsum = __builtin_amdgcn_fdot2_f32_bf16(w, bf16x2{(__bf16)1.f, (__bf16)1.f}, lsum, false);
-    }
+    for (int r = 0; r < 8; ++r)
+      lsum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw[r]), bf16x2{(__bf16)1.f, (__bf16)1.f}, lsum,
+                                             false);
     l += sum;
     lo += lsum;
 #pragma unroll
@@ -273,25 +318,33 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_mx_few_kernel(MxFewParams p) 
     }
   };
 
-  // reference tiles j0 + wave, + NW, ...; then the target tiles that follow in that order
+  // reference tiles j0 + wave, + NW, ..., two in flight; then the target tiles that follow in that order
   int j = j0 + wave;
   const int jr = min(j1, n_rt);
-  if (j < jr) {
-    Tile<D, KIND> cur, next;
-    load_tile(cur, kc, vc, j * KT, p.n_ref, lane);
-    for (; j < jr; j += NW) {
-      if (j + NW < jr) load_tile(next, kc, vc, (j + NW) * KT, p.n_ref, lane);
-      work(cur, p.n_ref - j * KT);
-      cur = next;
+  {
+    const LaneOffsets<D, KIND> at(kc, vc, lane);
+    Tile<D, KIND> even, odd;
+    if (j < jr) load_tile(even, kc, vc, at, j * KT);
+    while (j < jr) {
+      if (j + NW < jr) load_tile(odd, kc, vc, at, (j + NW) * KT);
+      work(even, p.n_ref - j * KT);
+      j += NW;
+      if (j >= jr) break;
+      if (j + NW < jr) load_tile(even, kc, vc, at, (j + NW) * KT);
+      work(odd, p.n_ref - j * KT);
+      j += NW;
     }
   }
   m_ref = m;
   l_ref = l;
   l = 0.f;
-  for (; j < j1; j += NW) {
-    Tile<D, 2> t;
-    load_tile(t, ky, vy, (j - n_rt) * KT, p.n_tgt, lane);
-    work(t, p.n_tgt - (j - n_rt) * KT);
+  {
+    const LaneOffsets<D, 2> at(ky, vy, lane);
+    for (; j < j1; j += NW) {
+      Tile<D, 2> t;
+      load_tile(t, ky, vy, at, (j - n_rt) * KT);
+      work(t, p.n_tgt - (j - n_rt) * KT);
+    }
   }
 
   // ---- the wavefronts' results, against the largest of their maxima
@@ -353,52 +406,56 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_mx_few_kernel(MxFewParams p) 
   }
 }
 
-// One output row per D / 4 threads, four columns a thread; the key ranges in order.
+// One workgroup an output row: groups of D / 4 threads, four columns a thread, take every (1024 / D)-th key range in
+// order and meet in LDS, in order too. (One group walking over all ranges took 6.0 us for 18 of them: each eight
+// were two memory round trips.)
 template <int D>
 __global__ __launch_bounds__(256) void attn_mx_merge_kernel(MxFewParams p) {
-  constexpr int TPR = D / 4, BATCH = 8;
-  const int64_t r = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
-  const int col = 4 * (threadIdx.x % TPR);
+  constexpr int TPR = D / 4, NG = 256 / TPR, BATCH = 4;
+  __shared__ f32x4 s_o[NG][TPR];
+  __shared__ float s_st[NG][5];
+  const int grp = threadIdx.x / TPR, col = 4 * (threadIdx.x % TPR);
+  const int64_t r = blockIdx.x;
   const int64_t bh = r / p.n_tgt;
-  if (bh >= (int64_t)p.B * p.H) return;
   const int qr = (int)(r - bh * p.n_tgt), qt = qr / BM, row = qr - qt * BM;
   const auto at = [&](int c) { return (((bh * p.chunks + c) * p.q_tiles) + qt) * BM + row; };
-  float M = LOWEST, M_R = LOWEST;
-  for (int c0 = 0; c0 < p.chunks; c0 += BATCH) {
-    float4 st[BATCH];
-#pragma unroll
-    for (int u = 0; u < BATCH; ++u)
-      if (c0 + u < p.chunks) st[u] = p.part_st[at(c0 + u)];
-#pragma unroll
-    for (int u = 0; u < BATCH; ++u)
-      if (c0 + u < p.chunks) {
-        M = fmaxf(M, st[u].x);
-        if (st[u].w > 0.f) M_R = fmaxf(M_R, st[u].z);
-      }
-  }
-  float L_R = 0.f, L_Y = 0.f, L_o = 0.f;
+  float M = LOWEST, M_R = LOWEST, L_R = 0.f, L_Y = 0.f, L_o = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int c0 = 0; c0 < p.chunks; c0 += BATCH) {
+  const auto add = [&](float m, float l, float m_ref, float l_ref, float lo, f32x4 o) {
+    const float M_new = fmaxf(M, m), MR_new = l_ref > 0.f ? fmaxf(M_R, m_ref) : M_R;
+    const float a = __builtin_amdgcn_exp2f(M - M_new), e = __builtin_amdgcn_exp2f(m - M_new);
+    L_Y = L_Y * a + l * e;
+    L_o = L_o * a + lo * e;
+    acc = acc * a + o * e;
+    L_R = L_R * __builtin_amdgcn_exp2f(M_R - MR_new) + l_ref * __builtin_amdgcn_exp2f(m_ref - MR_new);
+    M = M_new;
+    M_R = MR_new;
+  };
+  for (int c0 = grp; c0 < p.chunks; c0 += BATCH * NG) {
     float4 st[BATCH];
     float lo[BATCH];
     f32x4 o[BATCH];
 #pragma unroll
     for (int u = 0; u < BATCH; ++u)
-      if (c0 + u < p.chunks) {
-        st[u] = p.part_st[at(c0 + u)];
-        lo[u] = p.part_lo[at(c0 + u)];
-        o[u] = *reinterpret_cast<const f32x4*>(p.part_o + at(c0 + u) * D + col);
+      if (c0 + u * NG < p.chunks) {
+        st[u] = p.part_st[at(c0 + u * NG)];
+        lo[u] = p.part_lo[at(c0 + u * NG)];
+        o[u] = *reinterpret_cast<const f32x4*>(p.part_o + at(c0 + u * NG) * D + col);
       }
 #pragma unroll
     for (int u = 0; u < BATCH; ++u)
-      if (c0 + u < p.chunks) {
-        const float e = __builtin_amdgcn_exp2f(st[u].x - M);
-        L_Y += st[u].y * e;
-        L_o += lo[u] * e;
-        L_R += st[u].w * __builtin_amdgcn_exp2f(st[u].z - M_R);
-        acc += o[u] * e;
-      }
+      if (c0 + u * NG < p.chunks) add(st[u].x, st[u].y, st[u].z, st[u].w, lo[u], o[u]);
   }
+  s_o[grp][threadIdx.x % TPR] = acc;
+  if (col == 0) {
+    const float st[5] = {M, L_Y, M_R, L_R, L_o};
+#pragma unroll
+    for (int i = 0; i < 5; ++i) s_st[grp][i] = st[i];
+  }
+  __syncthreads();
+  if (grp != 0) return;
+  const int used = min(NG, p.chunks);
+  for (int w = 1; w < used; ++w) add(s_st[w][0], s_st[w][1], s_st[w][2], s_st[w][3], s_st[w][4], s_o[w][threadIdx.x]);
   const int b = (int)(bh / p.H), h = (int)(bh - (int64_t)b * p.H);
   mx_few_store(p, b, h, qr, col, acc, L_o);
   if (col == 0) mx_few_stats(p, r, M, L_Y, M_R, L_R);
@@ -411,8 +468,7 @@ hipError_t launch(const MxFewParams& p, int format, hipStream_t stream) {
                            ? launch_kernel(attn_mx_few_kernel<D, true>, grid, dim3(64 * NW), 0, stream, p)
                            : launch_kernel(attn_mx_few_kernel<D, false>, grid, dim3(64 * NW), 0, stream, p);
   if (e != hipSuccess || p.chunks == 1) return e;
-  const int64_t rows = (int64_t)p.B * p.H * p.n_tgt, per = 256 / (D / 4);
-  return launch_kernel(attn_mx_merge_kernel<D>, dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, stream, p);
+  return launch_kernel(attn_mx_merge_kernel<D>, dim3((unsigned)((int64_t)p.B * p.H * p.n_tgt)), dim3(256), 0, stream, p);
 }
 
 }  // namespace

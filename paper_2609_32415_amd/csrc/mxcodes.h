@@ -108,7 +108,7 @@ __device__ __forceinline__ u32x2 load_codes(const uint8_t* p) {
   return *reinterpret_cast<const u32x2*>(p);
 }
 
-// Eight values as bf16 pairs: one conversion instruction a pair, exact.
+// Eight values as bf16 pairs: one conversion instruction a pair, exact; NaN under scale byte 255.
 template <bool FP4>
 __device__ __forceinline__ u32x4 decode_oct(u32x2 c, uint32_t e) {
   const float s = scale_bits(e);
@@ -124,10 +124,9 @@ __device__ __forceinline__ u32x4 decode_oct(u32x2 c, uint32_t e) {
     v[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[1], s, false);
     v[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[1], s, true);
   }
-  const uint32_t nan = 0x7fc07fc0u;
   u32x4 w;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = e == 255 ? nan : __builtin_bit_cast(uint32_t, v[i]);
+  for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(uint32_t, v[i]);
   return w;
 }
 

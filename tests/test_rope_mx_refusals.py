@@ -126,6 +126,8 @@ def _attn(cache=None, ws=0x10000, ws_bytes=1 << 30, desc=None, args=None):
     (dict(cache=dict(format=5)), L.RA_EINVAL, "format"),
     (dict(cache=dict(v=NO_MX)), L.RA_EINVAL, "v_mx"),
     (dict(cache=dict(k=_m(codes=0x1004))), L.RA_EUNSUPPORTED, "k_mx"),
+    (dict(cache=dict(k=_m(ss=1 << 24))), L.RA_EUNSUPPORTED, "k_mx row strides"),
+    (dict(cache=dict(v=_m(es=1 << 24))), L.RA_EUNSUPPORTED, "v_mx row strides"),
     (dict(args=dict(q_tgt=_t(0))), L.RA_EINVAL, "q_tgt"),
     (dict(args=dict(k_tgt=_t(ss=132))), L.RA_EUNSUPPORTED, "k_tgt"),
     (dict(args=dict(v_tgt=_t(ss=1 << 24))), L.RA_EUNSUPPORTED, "row stride"),
