@@ -624,7 +624,7 @@ bool few_rows(const ra_attn_desc& d) {
 
 // Key ranges of a few-rows launch: as many as fill the CUs, with a tile for every wavefront.
 struct FewPlan {
-  int64_t q_tiles, chunks, rows;  // rows: of partial results
+  int64_t q_tiles, key_tiles, chunks, rows;  // rows: of partial results
   size_t o_bytes(int head_dim) const { return (size_t)rows * head_dim * sizeof(float); }
   size_t bytes(int head_dim) const { return o_bytes(head_dim) + (size_t)rows * 5 * sizeof(float); }
 };
@@ -633,8 +633,8 @@ FewPlan few_plan(const ra_attn_desc& d) {
   const int64_t bh = (int64_t)d.batch * d.heads, cus = attn_bf16_slots(d.head_dim, kAttnBf16BM).cus;
   FewPlan f{};
   f.q_tiles = (d.n_tgt + kFewRows - 1) / kFewRows;
-  const int64_t nt = ((int64_t)d.n_ref + kFewKeys - 1) / kFewKeys + (d.n_tgt + kFewKeys - 1) / kFewKeys;
-  f.chunks = std::max<int64_t>(1, std::min(cus / (bh * f.q_tiles), (nt + kFewWaves - 1) / kFewWaves));
+  f.key_tiles = ((int64_t)d.n_ref + kFewKeys - 1) / kFewKeys + (d.n_tgt + kFewKeys - 1) / kFewKeys;
+  f.chunks = std::max<int64_t>(1, std::min(cus / (bh * f.q_tiles), (f.key_tiles + kFewWaves - 1) / kFewWaves));
   f.rows = f.chunks > 1 ? bh * f.q_tiles * f.chunks * kFewRows : 0;
   return f;
 }
@@ -701,6 +701,8 @@ ra_status joint_attn_mx_few(const ra_attn_desc& d, const ra_attn_args& a, const 
   p.n_tgt = d.n_tgt;
   p.q_tiles = (int32_t)f.q_tiles;
   p.chunks = (int32_t)f.chunks;
+  p.tiles_each = (int32_t)(f.key_tiles / f.chunks);
+  p.tiles_more = (int32_t)(f.key_tiles % f.chunks);
   p.sc_log2 = softmax_scale(d) * 1.4426950408889634f;
   return launch_status(launch_attn_mx_few(p, c.format, d.head_dim, static_cast<hipStream_t>(stream)), "joint_attn_mx");
 }

@@ -24,6 +24,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "internal.h"
 #include "mxcodes.h"
 
@@ -46,25 +48,45 @@ constexpr float BOUND = 4096.0f;    // on a probability against the running maxi
 // tile, the order of the B operand (P^T) of the second product.
 __device__ __forceinline__ int sigma(int m) { return (m & ~12) | ((m & 4) << 1) | ((m & 8) >> 1); }
 
+// Keeps a value in a register at this point of the program, so the optimizer cannot sink the instructions that
+// produce it below the bound test (the exponentials of both its sides would stay in registers for them).
+template <typename T>
+__device__ __forceinline__ void pin(T& v) {
+  asm volatile("" : "+v"(v));
+}
+
+// The lane number, computed here and now: what is formed from an earlier one is kept in registers through the key loop.
+__device__ __forceinline__ int lane_now() {
+  int l;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+  return l;
+}
+
 __device__ __forceinline__ float xor32(float v, int op) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   const float a = __uint_as_float(r[0]), b = __uint_as_float(r[1]);
   return op ? fmaxf(a, b) : a + b;
 }
 
-// A tile's operands as loaded: KIND 0 e2m1 codes, 1 e4m3 codes, 2 bf16.
+// A lane's part of a K and of a V tile, as loaded. KIND 0: e2m1 codes, 1: e4m3 codes, 2: bf16.
+// Of K: row sigma(lane % 32), blocks 2 i + g of 32 elements.
 template <int D, int KIND>
-struct Tile {
-  static constexpr int NI = D / 64;                                // blocks of 32 of a lane's K row
-  static constexpr int KW = KIND == 0 ? 1 : KIND == 1 ? 2 : 4;     // 16-byte loads of such a block
-  static constexpr int NV = D / 32;                                // pieces of 16 elements of V a lane takes
-  static constexpr int VW = KIND == 0 ? 2 : KIND == 1 ? 4 : 8;     // words of such a piece
-  static constexpr int ROW = D / 2 * KW;                           // bytes of a row
-  u32x4 k[NI][KW];
-  uint32_t ks[NI];
-  uint32_t v[NV][VW];
-  uint32_t vs[NV];
+struct KTile {
+  static constexpr int NI = D / 64;
+  static constexpr int NL = KIND == 0 ? 1 : KIND == 1 ? 2 : 4;  // 16-byte loads of a block
+  u32x4 w[NI][NL];
+  uint32_t e;  // the row's scale bytes
 };
+// Of V: pieces of 16 elements, keys 16 s2 + (lane / 2) % 16, elements 32 (2 d2 + g) + 16 (lane % 2) .. + 15.
+template <int D, int KIND>
+struct VTile {
+  static constexpr int NV = D / 32;
+  static constexpr int NL = KIND == 0 ? 2 : KIND == 1 ? 4 : 8;  // words of a piece
+  uint32_t w[NV][NL];
+  uint32_t e[2];  // the scale bytes of its two rows
+};
+template <int D, int KIND>
+constexpr int kRowBytes = KIND == 0 ? D / 2 : KIND == 1 ? D : 2 * D;
 
 // One K or V stream: the rows of a (batch, head), read tile by tile through a buffer resource, so that a lane's
 // offsets within a tile never change and rows past the last read as zeros (their scores are masked, and
@@ -86,87 +108,85 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const uint8_t* base,
                                            0x00020000);
 }
 
-// A lane's byte offsets within a tile.
-template <int D, int KIND>
-struct LaneOffsets {
-  uint32_t k, ks, v, vs;  // its K row and block; the first of its V pieces
-  __device__ __forceinline__ LaneOffsets(const Stream& ks_, const Stream& vs_, int lane) {
-    using T = Tile<D, KIND>;
-    const int g = lane >> 5, row = sigma(lane & 31), vrow = (lane >> 1) & 15;
-    k = row * ks_.ss + g * 16 * T::KW;
-    ks = row * ks_.es + g;
-    v = vrow * vs_.ss + (2 * g + (lane & 1)) * 8 * T::KW;
-    vs = vrow * vs_.es + g;
-  }
-};
+// A row's scale bytes in one load, and one of them as the conversions take it: they read bits 30..23 of the scale
+// alone, so byte 0 needs a shift and no mask.
+template <int D>
+__device__ __forceinline__ uint32_t load_scales(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t soff) {
+  if constexpr (D == 128) return __builtin_amdgcn_raw_buffer_load_b32(r, off, soff, 0);
+  return __builtin_amdgcn_raw_buffer_load_b16(r, off, soff, 0);
+}
+__device__ __forceinline__ float block_scale(uint32_t e, int i, int g) {
+  return __uint_as_float((e >> (8 * g)) << (23 - 16 * i));  // byte 2 i + g of the row's
+}
 
 template <int D, int KIND>
-__device__ __forceinline__ void load_tile(Tile<D, KIND>& t, const Stream& k, const Stream& v,
-                                          const LaneOffsets<D, KIND>& at, int key0) {
-  using T = Tile<D, KIND>;
-  const int valid = min(KT, k.n_keys - key0);
-  const auto kr = rows_rsrc(k.codes, k.ss, key0, valid, T::ROW), vr = rows_rsrc(v.codes, v.ss, key0, valid, T::ROW);
+__device__ __forceinline__ void load_k(KTile<D, KIND>& t, const Stream& k, int key0, int lane) {
+  const int valid = min(KT, k.n_keys - key0), g = lane >> 5, row = sigma(lane & 31);
+  const auto r = rows_rsrc(k.codes, k.ss, key0, valid, kRowBytes<D, KIND>);
+  const uint32_t off = row * k.ss + g * kRowBytes<32, KIND>;
 #pragma unroll
-  for (int i = 0; i < T::NI; ++i)
+  for (int i = 0; i < t.NI; ++i)
 #pragma unroll
-    for (int j = 0; j < T::KW; ++j)
-      t.k[i][j] = __builtin_amdgcn_raw_buffer_load_b128(kr, at.k + 32 * T::KW * i + 16 * j, 0, 0);
+    for (int j = 0; j < t.NL; ++j)
+      t.w[i][j] = __builtin_amdgcn_raw_buffer_load_b128(r, off + kRowBytes<64, KIND> * i + 16 * j, 0, 0);
+  if constexpr (KIND != 2) {
+    const auto re = rows_rsrc(k.scales, k.es, key0, valid, D / 32);
+    t.e = load_scales<D>(re, row * k.es, 0);
+  }
+}
+
+template <int D, int KIND>
+__device__ __forceinline__ void load_v(VTile<D, KIND>& t, const Stream& v, int key0, int lane) {
+  const int valid = min(KT, v.n_keys - key0), g = lane >> 5, row = (lane >> 1) & 15;
+  constexpr int piece = kRowBytes<16, KIND>;
+  const auto r = rows_rsrc(v.codes, v.ss, key0, valid, kRowBytes<D, KIND>);
+  const uint32_t off = row * v.ss + (2 * g + (lane & 1)) * piece;
 #pragma unroll
-  for (int i = 0; i < T::NV; ++i) {  // keys 16 s2 .. + 15, block 2 d2 + g
+  for (int i = 0; i < t.NV; ++i) {
     const int s2 = i / (D / 64), d2 = i % (D / 64);
-    const uint32_t off = at.v + 32 * T::KW * d2;
     if constexpr (KIND == 0) {
-      const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(vr, off, 16 * s2 * v.ss, 0);
-      t.v[i][0] = w[0];
-      t.v[i][1] = w[1];
+      const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(r, off + 4 * piece * d2, 16 * s2 * v.ss, 0);
+      t.w[i][0] = w[0];
+      t.w[i][1] = w[1];
     } else {
 #pragma unroll
-      for (int j = 0; j < T::VW / 4; ++j) {
-        const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(vr, off + 16 * j, 16 * s2 * v.ss, 0);
+      for (int j = 0; j < t.NL / 4; ++j) {
+        const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(r, off + 4 * piece * d2 + 16 * j, 16 * s2 * v.ss, 0);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) t.v[i][4 * j + e] = w[e];
+        for (int e = 0; e < 4; ++e) t.w[i][4 * j + e] = w[e];
       }
     }
   }
   if constexpr (KIND != 2) {
-    const auto ke = rows_rsrc(k.scales, k.es, key0, valid, D / 32), ve = rows_rsrc(v.scales, v.es, key0, valid, D / 32);
-#pragma unroll
-    for (int i = 0; i < T::NI; ++i) t.ks[i] = __builtin_amdgcn_raw_buffer_load_b8(ke, at.ks + 2 * i, 0, 0);
-#pragma unroll
-    for (int i = 0; i < T::NV; ++i)
-      t.vs[i] = __builtin_amdgcn_raw_buffer_load_b8(ve, at.vs + 2 * (i % (D / 64)), 16 * (i / (D / 64)) * v.es, 0);
+    const auto re = rows_rsrc(v.scales, v.es, key0, valid, D / 32);
+    t.e[0] = load_scales<D>(re, row * v.es, 0);
+    t.e[1] = load_scales<D>(re, row * v.es, 16 * v.es);
   }
 }
 
 // Elements 8 s .. 8 s + 7 of a K block.
 template <int D, int KIND>
-__device__ __forceinline__ bf16x8 k_operand(const Tile<D, KIND>& t, int i, int s) {
+__device__ __forceinline__ bf16x8 k_operand(const KTile<D, KIND>& t, int i, int s, int g) {
   u32x4 w;
-  if constexpr (KIND == 0) w = decode_oct<true>(u32x2{t.k[i][0][s], 0u}, t.ks[i]);
-  if constexpr (KIND == 1) w = decode_oct<false>(u32x2{t.k[i][s >> 1][2 * (s & 1)], t.k[i][s >> 1][2 * (s & 1) + 1]}, t.ks[i]);
-  if constexpr (KIND == 2) w = t.k[i][s];
+  const float e = KIND == 2 ? 0.f : block_scale(t.e, i, g);
+  if constexpr (KIND == 0) w = decode_oct<true>(u32x2{t.w[i][0][s], 0u}, e);
+  if constexpr (KIND == 1) w = decode_oct<false>(u32x2{t.w[i][s >> 1][2 * (s & 1)], t.w[i][s >> 1][2 * (s & 1) + 1]}, e);
+  if constexpr (KIND == 2) w = t.w[i][s];
   return __builtin_bit_cast(bf16x8, w);
 }
 
-// Puts the tile's V into LDS as blocks of 16 keys x 32 dims (1 KiB; 64 bytes a key, its halves swapped where
+// Puts half j of V piece i into LDS: blocks of 16 keys x 32 elements (1 KiB; 64 bytes a key, its halves swapped where
 // bit 1 of the key is set, which keeps the transpose reads free of bank conflicts).
 template <int D, int KIND>
-__device__ __forceinline__ void store_v(uint16_t* lds, const Tile<D, KIND>& t, int lane) {
-  using T = Tile<D, KIND>;
-  const int r = (lane >> 1) & 15;
-#pragma unroll
-  for (int i = 0; i < T::NV; ++i) {
-    const int s2 = i / (D / 64), db = 2 * (i % (D / 64)) + (lane >> 5);
-    uint16_t* p = lds + 512 * ((D / 32) * s2 + db) + 32 * r + 16 * ((lane & 1) ^ ((r >> 1) & 1));
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      u32x4 w;
-      if constexpr (KIND == 0) w = decode_oct<true>(u32x2{t.v[i][j], 0u}, t.vs[i]);
-      if constexpr (KIND == 1) w = decode_oct<false>(u32x2{t.v[i][2 * j], t.v[i][2 * j + 1]}, t.vs[i]);
-      if constexpr (KIND == 2) w = u32x4{t.v[i][4 * j], t.v[i][4 * j + 1], t.v[i][4 * j + 2], t.v[i][4 * j + 3]};
-      *reinterpret_cast<u32x4*>(p + 8 * j) = w;
-    }
-  }
+__device__ __forceinline__ void store_v(uint16_t* lds, const VTile<D, KIND>& t, int i, int j, int lane) {
+  const int r = (lane >> 1) & 15, s2 = i / (D / 64), d2 = i % (D / 64);
+  uint16_t* const p = lds + 512 * ((D / 32) * s2 + 2 * d2 + (lane >> 5)) + 32 * r + 16 * ((lane & 1) ^ ((r >> 1) & 1));
+  u32x4 w;
+  const float e = KIND == 2 ? 0.f : block_scale(t.e[s2], d2, lane >> 5);
+  if constexpr (KIND == 0) w = decode_oct<true>(u32x2{t.w[i][j], 0u}, e);
+  if constexpr (KIND == 1) w = decode_oct<false>(u32x2{t.w[i][2 * j], t.w[i][2 * j + 1]}, e);
+  if constexpr (KIND == 2) w = u32x4{t.w[i][4 * j], t.w[i][4 * j + 1], t.w[i][4 * j + 2], t.w[i][4 * j + 3]};
+  *reinterpret_cast<u32x4*>(p + 8 * j) = w;
 }
 
 __device__ __forceinline__ void lds_order() {
@@ -218,11 +238,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_mx_few_kernel(MxFewParams p) 
 
   // item: (batch, head), key range, query tile (fastest: its neighbours read the same keys)
   const int item = xcd_remap(blockIdx.x, gridDim.x);
-  const int qt = item % p.q_tiles, range = item / p.q_tiles;
+  const int range = item / p.q_tiles, qt = item - range * p.q_tiles;
   const int bh = range / p.chunks, chunk = range - bh * p.chunks;
   const int b = bh / p.H, h = bh - b * p.H;
-  const int n_rt = (p.n_ref + KT - 1) / KT, nt = n_rt + (p.n_tgt + KT - 1) / KT;
-  const int j0 = (int)((int64_t)chunk * nt / p.chunks), j1 = (int)((int64_t)(chunk + 1) * nt / p.chunks);
+  const int n_rt = (p.n_ref + KT - 1) / KT;
+  const int j0 = chunk * p.tiles_each + min(chunk, p.tiles_more), j1 = j0 + p.tiles_each + (chunk < p.tiles_more ? 1 : 0);
 
   const auto cached = [&](const MxView& v) {
     return Stream{v.codes + b * v.sb + h * v.sh, v.scales + b * v.eb + h * v.eh, (int32_t)v.ss, (int32_t)v.es, p.n_ref};
@@ -232,17 +252,17 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_mx_few_kernel(MxFewParams p) 
   };
   const Stream kc = cached(p.k), vc = cached(p.v), ky = plain(p.k_tgt), vy = plain(p.v_tgt);
 
+  // Q^T as the B operand: lane half g holds elements 32 g .. + 31 of every 64. Rows past the last repeat it.
   const int qrow = qt * BM + n;
   bf16x8 q[NI][4];
   {
-    const uint16_t* qp = static_cast<const uint16_t*>(p.q.p) + b * p.q.sb + h * p.q.sh + (int64_t)qrow * p.q.ss;
+    const uint16_t* qp = static_cast<const uint16_t*>(p.q.p) + b * p.q.sb + h * p.q.sh +
+                         (int64_t)min(qrow, p.n_tgt - 1) * p.q.ss + 32 * g;
 #pragma unroll
     for (int i = 0; i < NI; ++i)
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const u32x4 w = qrow < p.n_tgt ? *reinterpret_cast<const u32x4*>(qp + 64 * i + 32 * g + 8 * t) : u32x4{0, 0, 0, 0};
-        q[i][t] = __builtin_bit_cast(bf16x8, w);
-      }
+      for (int t = 0; t < 4; ++t)
+        q[i][t] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qp + 64 * i + 8 * t));
   }
 
   f32x16 o[DB];
@@ -254,41 +274,71 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_mx_few_kernel(MxFewParams p) 
   const int v_lane =
       32 * (8 * (tr_G >> 1) + (tr_i >> 2)) + ((16 * (tr_G & 1) + 4 * (tr_i & 3)) ^ (16 * ((tr_i >> 3) & 1)));
 
-  const auto work = [&](const auto& t, int valid) __attribute__((always_inline)) {
-    lds_order();
-    store_v(lds, t, lane);
-    lds_order();
+  const auto v_operand = [&](int i) __attribute__((always_inline)) {  // i = DB * s2 + db
+    const uint16_t* a = lds + v_lane + 512 * i;
+    const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(a));
+    const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(a + 128));
+    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  const auto p_operand = [](const uint32_t(&w)[8], int s2) __attribute__((always_inline)) {
+    return __builtin_bit_cast(bf16x8, u32x4{w[4 * s2], w[4 * s2 + 1], w[4 * s2 + 2], w[4 * s2 + 3]});
+  };
+  // S^T of a tile, and its V into LDS, a K operand and a share of V after each product. (Left to itself the
+  // compiler puts the products last, where nothing runs beside them.)
+  const auto score = [&](const auto& k, const auto& v) __attribute__((always_inline)) {
     f32x16 sc{};
+    lds_order();
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(t, i, e), q[i][e], sc, 0, 0, 0);
+    for (int i = 0; i < 4 * NI; ++i) {
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(k, i / 4, i % 4, g), q[i / 4][i % 4], sc, 0, 0, 0);
+      store_v(lds, v, i / 2, i % 2, lane);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    lds_order();
+    return sc;
+  };
+  // Probabilities of a tile's scores, formed under the product of the tile before (FIRST: there is none),
+  // O^T += V^T P^T with that tile's V from LDS and its probabilities `prev`.
+  const auto attend = [&](auto firstc, f32x16& sc, int valid, const uint32_t(&prev)[8], uint32_t(&pw)[8])
+                          __attribute__((always_inline)) {
+    constexpr bool FIRST = decltype(firstc)::value;
+    constexpr int PV = FIRST ? 1 : 2 * DB;
     if (valid < KT) {
-      asm volatile("");  // a branch: as selects the mask costs every tile 30 instructions
+      const int gn = lane_now() >> 5;  // also keeps this a branch (as selects the mask costs every tile 30 instructions)
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        if (16 * (r >> 3) + 8 * g + (r & 7) >= valid) sc[r] = -__builtin_inff();
+        if (16 * (r >> 3) + 8 * gn + (r & 7) >= valid) sc[r] = -__builtin_inff();
     }
     // Against the running maximum first: a lane's sum bounds each of its terms, so that a sum within 2^12 (NaN and
     // infinity are not) lets the maximum stay.
-    uint32_t pw[8];
-    float sum;
-    const auto form = [&]() __attribute__((always_inline)) {
-      float part[2];
-#pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[2 * r], p.sc_log2, -m));
-        const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[2 * r + 1], p.sc_log2, -m));
-        part[r & 1] = r < 2 ? e0 + e1 : part[r & 1] + (e0 + e1);
-        bf16x2 w;
-        w[0] = (__bf16)e0;
-        w[1] = (__bf16)e1;
-        pw[r] = __builtin_bit_cast(uint32_t, w);
-      }
-      sum = part[0] + part[1];
+    float part[2];
+    const auto pair = [&](int r) __attribute__((always_inline)) {
+      const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[2 * r], p.sc_log2, -m));
+      const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[2 * r + 1], p.sc_log2, -m));
+      part[r & 1] = r < 2 ? e0 + e1 : part[r & 1] + (e0 + e1);
+      bf16x2 w;
+      w[0] = (__bf16)e0;
+      w[1] = (__bf16)e1;
+      pw[r] = __builtin_bit_cast(uint32_t, w);
+      pin(pw[r]);
+      pin(part[r & 1]);
     };
-    form();
-    if (__any(!(sum <= BOUND))) {  // rare, and always at a wavefront's first tile
+    bf16x8 va[3];
+    if constexpr (!FIRST) {
+      va[0] = v_operand(0);
+      va[1] = v_operand(1);
+    }
+#pragma unroll
+    for (int i = 0; i < PV; ++i) {
+      if constexpr (!FIRST) {
+        o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[i % 3], p_operand(prev, i / DB), o[i % DB], 0, 0, 0);
+        if (i + 2 < PV) va[(i + 2) % 3] = v_operand(i + 2);
+      }
+#pragma unroll
+      for (int r = 8 * i / PV; r < 8 * (i + 1) / PV; ++r) pair(r);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (__any(!(part[0] + part[1] <= BOUND))) {  // rare, and always at a wavefront's first tile
       float mx = sc[0];
 #pragma unroll
       for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
@@ -298,102 +348,126 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_mx_few_kernel(MxFewParams p) 
       lo *= a;
 #pragma unroll
       for (int i = 0; i < DB; ++i) o[i] *= a;
-      form();
+#pragma unroll
+      for (int r = 0; r < 8; ++r) pair(r);
     }
+    l += part[0] + part[1];
     float lsum = 0.f;
 #pragma unroll
     for (int r = 0; r < 8; ++r)
       lsum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pw[r]), bf16x2{(__bf16)1.f, (__bf16)1.f}, lsum,
                                              false);
-    l += sum;
     lo += lsum;
+  };
+  const auto last_pv = [&](const uint32_t(&prev)[8]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 2 * DB; ++i) {
-      const uint16_t* a = lds + v_lane + 512 * i;
-      const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(a));
-      const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(a + 128));
-      const u32x4 w = {pw[4 * (i / DB)], pw[4 * (i / DB) + 1], pw[4 * (i / DB) + 2], pw[4 * (i / DB) + 3]};
-      o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7),
-                                                          __builtin_bit_cast(bf16x8, w), o[i % DB], 0, 0, 0);
-    }
+    for (int i = 0; i < 2 * DB; ++i)
+      o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(i), p_operand(prev, i / DB), o[i % DB], 0, 0, 0);
   };
 
-  // reference tiles j0 + wave, + NW, ..., two in flight; then the target tiles that follow in that order
+  // Reference tiles j0 + wave, + NW, ...: iteration j forms the probabilities of tile j under the product of the tile
+  // before it, then the scores of the tile after it (and puts V_j where that tile's was). K and V are loaded two tiles
+  // ahead of their use.
   int j = j0 + wave;
   const int jr = min(j1, n_rt);
-  {
-    const LaneOffsets<D, KIND> at(kc, vc, lane);
-    Tile<D, KIND> even, odd;
-    if (j < jr) load_tile(even, kc, vc, at, j * KT);
+  constexpr std::true_type first{};
+  constexpr std::false_type later{};
+  uint32_t p0[8], p1[8];
+  if (j < jr) {
+    KTile<D, KIND> k0{}, k1{};
+    VTile<D, KIND> v0{}, v1{};
+    const auto load = [&](KTile<D, KIND>& k, VTile<D, KIND>& v, int jj) __attribute__((always_inline)) {
+      if (jj < jr) load_k(k, kc, jj * KT, lane);
+      if (jj - NW < jr) load_v(v, vc, (jj - NW) * KT, lane);
+    };
+    load_k(k0, kc, j * KT, lane);
+    load(k1, v0, j + NW);
+    f32x16 s0{}, s1{};
+#pragma unroll
+    for (int i = 0; i < 4 * NI; ++i)
+      s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(k0, i / 4, i % 4, g), q[i / 4][i % 4], s0, 0, 0, 0);
+    load(k0, v1, j + 2 * NW);
+    const auto iteration = [&](auto fc, f32x16& s_cur, f32x16& s_next, auto& k_next, auto& v_cur, auto& p_prev,
+                               auto& p_cur) __attribute__((always_inline)) {
+      attend(fc, s_cur, p.n_ref - j * KT, p_prev, p_cur);
+      s_next = score(k_next, v_cur);  // past the last tile: of an earlier one, not used
+      load(k_next, v_cur, j + 3 * NW);
+      j += NW;
+    };
+    iteration(first, s0, s1, k1, v0, p1, p0);
     while (j < jr) {
-      if (j + NW < jr) load_tile(odd, kc, vc, at, (j + NW) * KT);
-      work(even, p.n_ref - j * KT);
-      j += NW;
-      if (j >= jr) break;
-      if (j + NW < jr) load_tile(even, kc, vc, at, (j + NW) * KT);
-      work(odd, p.n_ref - j * KT);
-      j += NW;
+      iteration(later, s1, s0, k0, v1, p0, p1);
+      if (j >= jr) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) p0[r] = p1[r];
+        break;
+      }
+      iteration(later, s0, s1, k1, v0, p1, p0);
     }
+    last_pv(p0);
   }
   m_ref = m;
   l_ref = l;
   l = 0.f;
-  {
-    const LaneOffsets<D, 2> at(ky, vy, lane);
-    for (; j < j1; j += NW) {
-      Tile<D, 2> t;
-      load_tile(t, ky, vy, at, (j - n_rt) * KT);
-      work(t, p.n_tgt - (j - n_rt) * KT);
-    }
+  // The target tiles that follow in the same order: few, one at a time.
+  for (; j < j1; j += NW) {
+    KTile<D, 2> k;
+    VTile<D, 2> v;
+    load_k(k, ky, (j - n_rt) * KT, lane);
+    load_v(v, vy, (j - n_rt) * KT, lane);
+    f32x16 sc = score(k, v);
+    attend(first, sc, p.n_tgt - (j - n_rt) * KT, p1, p0);
+    last_pv(p0);
   }
 
   // ---- the wavefronts' results, against the largest of their maxima
+  const int le = lane_now(), ge = le >> 5, ne = le & 31, row_e = qt * BM + ne;
   l = xor32(l, 0);
   l_ref = xor32(l_ref, 0);
   lo = xor32(lo, 0);
-  if (g == 0) {
-    s.m[wave][n] = m;
-    s.l[wave][n] = l;
-    s.m_ref[wave][n] = m_ref;
-    s.l_ref[wave][n] = l_ref;
-    s.lo[wave][n] = lo;
+  if (ge == 0) {
+    s.m[wave][ne] = m;
+    s.l[wave][ne] = l;
+    s.m_ref[wave][ne] = m_ref;
+    s.l_ref[wave][ne] = l_ref;
+    s.lo[wave][ne] = lo;
   }
   __syncthreads();  // also: every wavefront is done with its V
   float M = LOWEST;
 #pragma unroll
-  for (int w = 0; w < NW; ++w) M = fmaxf(M, s.m[w][n]);
+  for (int w = 0; w < NW; ++w) M = fmaxf(M, s.m[w][ne]);
   const float a = __builtin_amdgcn_exp2f(m - M);
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
     for (int rr = 0; rr < 4; ++rr)
-      *reinterpret_cast<f32x4*>(&s.o[wave][n][32 * db + 8 * rr + 4 * g]) =
+      *reinterpret_cast<f32x4*>(&s.o[wave][ne][32 * db + 8 * rr + 4 * ge]) =
           f32x4{o[db][4 * rr] * a, o[db][4 * rr + 1] * a, o[db][4 * rr + 2] * a, o[db][4 * rr + 3] * a};
   const bool split = p.chunks > 1;
-  if (threadIdx.x < BM) {
+  if (wave == 0 && ge == 0) {
     float M_R = LOWEST, L_R = 0.f, L_Y = 0.f, L_o = 0.f;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) M_R = s.l_ref[w][n] > 0.f ? fmaxf(M_R, s.m_ref[w][n]) : M_R;
+    for (int w = 0; w < NW; ++w) M_R = s.l_ref[w][ne] > 0.f ? fmaxf(M_R, s.m_ref[w][ne]) : M_R;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      const float e = __builtin_amdgcn_exp2f(s.m[w][n] - M);
-      L_R += s.l_ref[w][n] * __builtin_amdgcn_exp2f(s.m_ref[w][n] - M_R);
-      L_Y += s.l[w][n] * e;
-      L_o += s.lo[w][n] * e;
+      const float e = __builtin_amdgcn_exp2f(s.m[w][ne] - M);
+      L_R += s.l_ref[w][ne] * __builtin_amdgcn_exp2f(s.m_ref[w][ne] - M_R);
+      L_Y += s.l[w][ne] * e;
+      L_o += s.lo[w][ne] * e;
     }
-    s.sum[n] = L_o;
-    if (qrow < p.n_tgt) {
+    s.sum[ne] = L_o;
+    if (row_e < p.n_tgt) {
       if (split) {
-        const int64_t row = (int64_t)item * BM + n;
+        const int64_t row = (int64_t)item * BM + ne;
         p.part_st[row] = float4{M, L_Y, M_R, L_R};
         p.part_lo[row] = L_o;
       } else {
-        mx_few_stats(p, (int64_t)bh * p.n_tgt + qrow, M, L_Y, M_R, L_R);
+        mx_few_stats(p, (int64_t)bh * p.n_tgt + row_e, M, L_Y, M_R, L_R);
       }
     }
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < BM * (D / 4); e += 64 * NW) {
+  for (int e = 64 * wave + le; e < BM * (D / 4); e += 64 * NW) {
     const int row = e / (D / 4), col = 4 * (e % (D / 4)), qr = qt * BM + row;
     if (qr >= p.n_tgt) break;
     f32x4 acc = *reinterpret_cast<const f32x4*>(&s.o[0][row][col]);

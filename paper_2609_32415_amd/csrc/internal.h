@@ -149,6 +149,7 @@ struct MxFewParams {
   float* lse;               // [B, H, n_tgt, 2] or null
   int32_t B, H, n_ref, n_tgt;
   int32_t q_tiles, chunks;
+  int32_t tiles_each, tiles_more;  // key tiles of a range; the first tiles_more ranges have one more
   float sc_log2;    // softmax scale * log2(e)
   float* part_o;    // chunks > 1: [B * H][chunks][q_tiles][kFewRows][d] unnormalised outputs,
   float4* part_st;  // (m, l_Y, m_R, l_R)

@@ -75,7 +75,7 @@ __global__ __launch_bounds__(MX_THREADS) void mx_read_kernel(MxSet ms, int32_t H
     const int64_t row = v / vpr;
     const int col = (int)(v - row * vpr);
     const u32x2 c = load_codes<FP4>(cb + row * src.ss + (FP4 ? 4 : 8) * col);
-    const u32x4 w = decode_oct<FP4>(c, eb[row * src.es + (col >> 2)]);
+    const u32x4 w = decode_oct<FP4>(c, scale_bits(eb[row * src.es + (col >> 2)]));
     store_oct<BF16>(db + (row * dst.ss + 8 * col) * esz, w);
   }
 }

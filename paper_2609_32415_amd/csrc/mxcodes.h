@@ -108,10 +108,10 @@ __device__ __forceinline__ u32x2 load_codes(const uint8_t* p) {
   return *reinterpret_cast<const u32x2*>(p);
 }
 
-// Eight values as bf16 pairs: one conversion instruction a pair, exact; NaN under scale byte 255.
+// Eight values as bf16 pairs: one conversion instruction a pair, exact; NaN under scale byte 255. Of the scale it reads
+// the exponent field alone.
 template <bool FP4>
-__device__ __forceinline__ u32x4 decode_oct(u32x2 c, uint32_t e) {
-  const float s = scale_bits(e);
+__device__ __forceinline__ u32x4 decode_oct(u32x2 c, float s) {
   bf16x2 v[4];
   if constexpr (FP4) {
     v[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c[0], s, 0);
