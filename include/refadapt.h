@@ -362,6 +362,12 @@ typedef struct {
   const int32_t* axis; /* HOST [n_pairs]: axis of each pair, 0..n_axes - 1 */
 } ra_rope_desc;
 
+typedef struct {
+  ra_tensor q, k;         /* [B, H, rows, d]; k with NULL data: q alone */
+  ra_tensor q_out, k_out; /* out, the same sizes */
+  const void* pos;        /* device [B, rows, n_axes] */
+} ra_rope_args;
+
 /*
  * refadapt_rope - rotary positions of Q, or of Q and K, with several axes.
  *
@@ -381,8 +387,7 @@ typedef struct {
  * 16-byte units, RA_ROPE_HALF with n_pairs not in whole 16-byte units, n_pairs
  * above RA_ROPE_MAX_PAIRS, alignment, 2^31 or more 16-byte pieces of q).
  */
-ra_status refadapt_rope(const ra_rope_desc* desc, ra_tensor q, ra_tensor k, ra_tensor q_out, ra_tensor k_out,
-                        const void* pos, void* stream);
+ra_status refadapt_rope(const ra_rope_desc* desc, const ra_rope_args* args, void* stream);
 
 /* ---- Reference cache in 8 or 4 bits ---------------------------------------- */
 
@@ -402,6 +407,22 @@ typedef struct {
   int64_t scale_stride_b, scale_stride_h, scale_stride_s;
 } ra_mx_tensor;
 
+typedef struct {
+  int32_t batch, heads, n_ref, head_dim; /* n_ref >= 0; head_dim a multiple of 32 */
+  int32_t dtype;                         /* ra_dtype of the plain tensors */
+  int32_t format;                        /* ra_mx_format */
+} ra_mx_desc;
+
+/* K is required; each of the V and Q pairs is taken when both of its sides are
+ * non-NULL and skipped when both are NULL. */
+typedef struct {
+  ra_tensor k, v, q;             /* [B, H, n_ref, d] plain: read by the commit, written by the read */
+  ra_mx_tensor k_mx, v_mx, q_mx; /* quantised */
+  const int32_t* decision;       /* commit: device word (ra_decision), or NULL */
+  int32_t* age;                  /* commit: device word, or NULL */
+  int32_t step;                  /* commit: what *age becomes */
+} ra_mx_args;
+
 /*
  * refadapt_mx_commit - refadapt_cache_commit into a quantised cache.
  *
@@ -412,23 +433,19 @@ typedef struct {
  * 127 - emax; an element's code is the nearest to x * 2^-e, ties to the even
  * code, saturating. A block of zeros has the lowest scale, a block that holds a
  * NaN or an infinity byte 255 and codes 0. Every value is a finite bf16.
- * Errors: RA_EINVAL (null K tensors, a pair with one NULL side, sizes, enums),
+ * Errors: RA_EINVAL (null desc or args, null K tensors, a pair with one NULL side,
+ * sizes, enums),
  * RA_EUNSUPPORTED (head_dim not a multiple of 32, alignment, batch * heads >
  * 65535).
  */
-ra_status refadapt_mx_commit(int32_t batch, int32_t heads, int32_t n_ref, int32_t head_dim, int32_t dtype,
-                             int32_t format, ra_tensor k_ref, ra_tensor v_ref, ra_tensor q_ref, ra_mx_tensor k_mx,
-                             ra_mx_tensor v_mx, ra_mx_tensor q_mx, const int32_t* decision, int32_t* age, int32_t step,
-                             void* stream);
+ra_status refadapt_mx_commit(const ra_mx_desc* desc, const ra_mx_args* args, void* stream);
 
 /*
  * refadapt_mx_read - the values that a quantised cache stands for, exactly, in
- * dtype. K is required; V and Q are read when both sides are non-NULL.
+ * dtype, into k, v and q.
  * Errors: as refadapt_mx_commit.
  */
-ra_status refadapt_mx_read(int32_t batch, int32_t heads, int32_t n_ref, int32_t head_dim, int32_t dtype, int32_t format,
-                           ra_mx_tensor k_mx, ra_mx_tensor v_mx, ra_mx_tensor q_mx, ra_tensor k_out, ra_tensor v_out,
-                           ra_tensor q_out, void* stream);
+ra_status refadapt_mx_read(const ra_mx_desc* desc, const ra_mx_args* args, void* stream);
 
 /* The quantised reference cache of a block: K, V and, with non-NULL codes, the reference queries. */
 typedef struct {

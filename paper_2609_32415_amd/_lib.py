@@ -105,6 +105,28 @@ class ra_mx_tensor(ctypes.Structure):
     ]
 
 
+class ra_rope_args(ctypes.Structure):
+    _fields_ = [("q", ra_tensor), ("k", ra_tensor), ("q_out", ra_tensor), ("k_out", ra_tensor), ("pos", ctypes.c_void_p)]
+
+
+class ra_mx_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "heads", "n_ref", "head_dim", "dtype", "format")]
+
+
+class ra_mx_args(ctypes.Structure):
+    _fields_ = [
+        ("k", ra_tensor),
+        ("v", ra_tensor),
+        ("q", ra_tensor),
+        ("k_mx", ra_mx_tensor),
+        ("v_mx", ra_mx_tensor),
+        ("q_mx", ra_mx_tensor),
+        ("decision", ctypes.c_void_p),
+        ("age", ctypes.c_void_p),
+        ("step", ctypes.c_int32),
+    ]
+
+
 class ra_mx_cache(ctypes.Structure):
     _fields_ = [("format", ctypes.c_int32), ("k", ra_mx_tensor), ("v", ra_mx_tensor), ("q", ra_mx_tensor)]
 
@@ -196,11 +218,11 @@ def _load():
     lib.refadapt_cache_commit.argtypes = [i32, i32, i32, i32, i32, ra_tensor, ra_tensor, ra_tensor, ra_tensor,
                                           ra_tensor, ra_tensor, vp, vp, i32, vp]
     lib.refadapt_cache_commit.restype = i32
-    lib.refadapt_rope.argtypes = [ctypes.POINTER(ra_rope_desc), ra_tensor, ra_tensor, ra_tensor, ra_tensor, vp, vp]
+    lib.refadapt_rope.argtypes = [ctypes.POINTER(ra_rope_desc), ctypes.POINTER(ra_rope_args), vp]
     lib.refadapt_rope.restype = i32
-    lib.refadapt_mx_commit.argtypes = [i32] * 6 + [ra_tensor] * 3 + [ra_mx_tensor] * 3 + [vp, vp, i32, vp]
+    lib.refadapt_mx_commit.argtypes = [ctypes.POINTER(ra_mx_desc), ctypes.POINTER(ra_mx_args), vp]
     lib.refadapt_mx_commit.restype = i32
-    lib.refadapt_mx_read.argtypes = [i32] * 6 + [ra_mx_tensor] * 3 + [ra_tensor] * 3 + [vp]
+    lib.refadapt_mx_read.argtypes = [ctypes.POINTER(ra_mx_desc), ctypes.POINTER(ra_mx_args), vp]
     lib.refadapt_mx_read.restype = i32
     lib.refadapt_joint_attn_mx_workspace_size.argtypes = [ctypes.POINTER(ra_attn_desc), i32, i32]
     lib.refadapt_joint_attn_mx_workspace_size.restype = ctypes.c_size_t
@@ -246,14 +268,22 @@ _joint_attn_packed = ctypes.CFUNCTYPE(ctypes.c_int32, ctypes.c_char_p, ctypes.c_
     ("refadapt_joint_attn", LIB))
 
 
-# The rope and quantised-cache calls on packed blocks too: tensors as 4 or 8 words each.
-ROPE_PACK = struct.Struct("=10i4q")  # ra_rope_desc
+# The rope and quantised-cache calls on packed blocks too.
+ROPE_DESC_PACK = struct.Struct("=10i4q")  # ra_rope_desc
+ROPE_ARGS_PACK = struct.Struct("=17q")  # ra_rope_args
+MX_DESC_PACK = struct.Struct("=6i")  # ra_mx_desc
+MX_ARGS_PACK = struct.Struct("=38qi4x")  # ra_mx_args
 MX_CACHE_PACK = struct.Struct("=i4x24q")  # ra_mx_cache
-assert ROPE_PACK.size == ctypes.sizeof(ra_rope_desc) and MX_CACHE_PACK.size == ctypes.sizeof(ra_mx_cache)
+assert [p.size for p in (ROPE_DESC_PACK, ROPE_ARGS_PACK, MX_DESC_PACK, MX_ARGS_PACK, MX_CACHE_PACK)] == [
+    ctypes.sizeof(c) for c in (ra_rope_desc, ra_rope_args, ra_mx_desc, ra_mx_args, ra_mx_cache)]
+_two_blocks = ctypes.CFUNCTYPE(ctypes.c_int32, ctypes.c_char_p, ctypes.c_char_p, ctypes.c_void_p)
+_rope_packed = _two_blocks(("refadapt_rope", LIB))
+_mx_commit_packed = _two_blocks(("refadapt_mx_commit", LIB))
+_mx_read_packed = _two_blocks(("refadapt_mx_read", LIB))
+_joint_attn_mx_ws_packed = ctypes.CFUNCTYPE(ctypes.c_size_t, ctypes.c_char_p, ctypes.c_int32, ctypes.c_int32)(
+    ("refadapt_joint_attn_mx_workspace_size", LIB))
 _joint_attn_mx_packed = ctypes.CFUNCTYPE(ctypes.c_int32, ctypes.c_char_p, ctypes.c_char_p, ctypes.c_char_p,
                                          ctypes.c_void_p)(("refadapt_joint_attn_mx", LIB))
-_rope_packed = ctypes.CFUNCTYPE(ctypes.c_int32, ctypes.c_char_p, ra_tensor, ra_tensor, ra_tensor, ra_tensor,
-                                ctypes.c_void_p, ctypes.c_void_p)(("refadapt_rope", LIB))
 
 
 def _check(status):
@@ -316,24 +346,27 @@ def refadapt_cache_commit(batch, heads, n_ref, head_dim, dtype, k_ref, v_ref, q_
                                             v_cache, q_cache, decision, age, step, stream))
 
 
-def refadapt_rope(desc, q, k, q_out, k_out, pos, stream):
-    """``desc``: bytes of ROPE_PACK."""
-    return _check(_rope_packed(desc, q, k, q_out, k_out, pos, stream))
+def refadapt_rope_packed(desc, args, stream):
+    """``refadapt_rope`` on bytes of ROPE_DESC_PACK and ROPE_ARGS_PACK."""
+    return _check(_rope_packed(desc, args, stream))
 
 
-def refadapt_mx_commit(batch, heads, n_ref, head_dim, dtype, fmt, k_ref, v_ref, q_ref, k_mx, v_mx, q_mx, decision, age,
-                       step, stream):
-    return _check(LIB.refadapt_mx_commit(batch, heads, n_ref, head_dim, dtype, fmt, k_ref, v_ref, q_ref, k_mx, v_mx,
-                                         q_mx, decision, age, step, stream))
+def refadapt_mx_commit_packed(desc, args, stream):
+    """``refadapt_mx_commit`` on bytes of MX_DESC_PACK and MX_ARGS_PACK."""
+    return _check(_mx_commit_packed(desc, args, stream))
 
 
-def refadapt_mx_read(batch, heads, n_ref, head_dim, dtype, fmt, k_mx, v_mx, q_mx, k_out, v_out, q_out, stream):
-    return _check(LIB.refadapt_mx_read(batch, heads, n_ref, head_dim, dtype, fmt, k_mx, v_mx, q_mx, k_out, v_out,
-                                       q_out, stream))
+def refadapt_mx_read_packed(desc, args, stream):
+    """``refadapt_mx_read`` on bytes of MX_DESC_PACK and MX_ARGS_PACK."""
+    return _check(_mx_read_packed(desc, args, stream))
 
 
 def refadapt_joint_attn_mx_workspace_size(desc, fmt, with_q):
     return int(LIB.refadapt_joint_attn_mx_workspace_size(ctypes.byref(desc), fmt, with_q))
+
+
+def refadapt_joint_attn_mx_workspace_size_packed(desc, fmt, with_q):
+    return _joint_attn_mx_ws_packed(desc, fmt, with_q)
 
 
 def refadapt_joint_attn_mx_packed(desc, args, cache, stream):

@@ -496,10 +496,10 @@ ra_status refadapt_cache_commit(int32_t batch, int32_t heads, int32_t n_ref, int
 
 extern "C" {
 
-ra_status refadapt_rope(const ra_rope_desc* desc, ra_tensor q, ra_tensor k, ra_tensor q_out, ra_tensor k_out,
-                        const void* pos, void* stream) {
-  if (!desc) return fail(RA_EINVAL, "rope: null desc");
+ra_status refadapt_rope(const ra_rope_desc* desc, const ra_rope_args* args, void* stream) {
+  if (!desc || !args) return fail(RA_EINVAL, "rope: null desc or args");
   const ra_rope_desc& d = *desc;
+  const ra_rope_args& a = *args;
   if (d.batch < 1 || d.heads < 1 || d.rows < 0) return fail(RA_EINVAL, "rope: bad sizes");
   if (d.dtype != RA_BF16 && d.dtype != RA_F32) return fail(RA_EINVAL, "rope: unknown dtype %d", d.dtype);
   if (d.pos_dtype != RA_POS_I32 && d.pos_dtype != RA_POS_F32)
@@ -529,22 +529,22 @@ ra_status refadapt_rope(const ra_rope_desc* desc, ra_tensor q, ra_tensor k, ra_t
   if (d.rows == 0) return ok();
   if ((int64_t)d.batch * d.rows * (d.head_dim / n) > 0x7fffffff)
     return fail(RA_EUNSUPPORTED, "rope: problem too large for one launch");
-  if (!pos) return fail(RA_EINVAL, "rope: null pos");
-  if ((reinterpret_cast<uintptr_t>(pos) & 3) != 0) return fail(RA_EUNSUPPORTED, "rope: pos must be 4-byte aligned");
+  if (!a.pos) return fail(RA_EINVAL, "rope: null pos");
+  if ((reinterpret_cast<uintptr_t>(a.pos) & 3) != 0) return fail(RA_EUNSUPPORTED, "rope: pos must be 4-byte aligned");
   ra_status s;
-  if ((s = check_tensor("q", q, d.dtype, d.rows, d.head_dim)) != RA_OK) return s;
-  if ((s = check_tensor("q_out", q_out, d.dtype, d.rows, d.head_dim)) != RA_OK) return s;
-  p.x[0] = view(q);
-  p.y[0] = view(q_out);
-  p.n = 1;
-  if (k.data != nullptr || k_out.data != nullptr) {
-    if ((s = check_tensor("k", k, d.dtype, d.rows, d.head_dim)) != RA_OK) return s;
-    if ((s = check_tensor("k_out", k_out, d.dtype, d.rows, d.head_dim)) != RA_OK) return s;
-    p.x[1] = view(k);
-    p.y[1] = view(k_out);
-    p.n = 2;
+  const ra_tensor* const in[2] = {&a.q, &a.k};
+  const ra_tensor* const out[2] = {&a.q_out, &a.k_out};
+  const char* const name[2] = {"q", "k"};
+  const char* const out_name[2] = {"q_out", "k_out"};
+  for (int i = 0; i < 2; ++i) {
+    if (i > 0 && in[i]->data == nullptr && out[i]->data == nullptr) continue;
+    if ((s = check_tensor(name[i], *in[i], d.dtype, d.rows, d.head_dim)) != RA_OK) return s;
+    if ((s = check_tensor(out_name[i], *out[i], d.dtype, d.rows, d.head_dim)) != RA_OK) return s;
+    p.x[i] = view(*in[i]);
+    p.y[i] = view(*out[i]);
+    p.n = i + 1;
   }
-  p.pos = pos;
+  p.pos = a.pos;
   p.pos_sb = d.pos_stride_b;
   p.pos_ss = d.pos_stride_s;
   p.pos_f32 = d.pos_dtype == RA_POS_F32 ? 1 : 0;
@@ -598,14 +598,21 @@ ra_status check_mx(const char* name, const ra_mx_tensor& t, int32_t format, int3
 }
 
 // The (plain, quantised) pairs of a commit or a read: K is required, V and Q are given on both sides or on neither.
-ra_status mx_set(MxSet* ms, const ra_tensor* const plain[3], const char* const plain_name[3],
-                 const ra_mx_tensor* const mx[3], const char* const mx_name[3], int32_t format, int32_t n_ref,
-                 int32_t head_dim, int32_t dtype) {
+ra_status mx_set(const char* who, const ra_mx_desc* desc, const ra_mx_args* args, const char* const plain_name[3],
+                 MxSet* ms) {
+  if (!desc || !args) return fail(RA_EINVAL, "%s: null desc or args", who);
+  const ra_mx_desc& d = *desc;
   ra_status s;
+  if ((s = check_mx_sizes(who, d.batch, d.heads, d.n_ref, d.head_dim, d.dtype, d.format)) != RA_OK) return s;
+  ms->n = 0;
+  if (d.n_ref == 0) return RA_OK;
+  const ra_tensor* const plain[3] = {&args->k, &args->v, &args->q};
+  const ra_mx_tensor* const mx[3] = {&args->k_mx, &args->v_mx, &args->q_mx};
+  const char* const mx_name[3] = {"k_mx", "v_mx", "q_mx"};
   for (int i = 0; i < 3; ++i) {
     if (i > 0 && plain[i]->data == nullptr && mx[i]->codes == nullptr && mx[i]->scales == nullptr) continue;
-    if ((s = check_tensor(plain_name[i], *plain[i], dtype, n_ref, head_dim)) != RA_OK) return s;
-    if ((s = check_mx(mx_name[i], *mx[i], format, n_ref, head_dim)) != RA_OK) return s;
+    if ((s = check_tensor(plain_name[i], *plain[i], d.dtype, d.n_ref, d.head_dim)) != RA_OK) return s;
+    if ((s = check_mx(mx_name[i], *mx[i], d.format, d.n_ref, d.head_dim)) != RA_OK) return s;
     ms->plain[ms->n] = view(*plain[i]);
     ms->mx[ms->n] = mx_view(*mx[i]);
     ++ms->n;
@@ -719,38 +726,26 @@ ra_status check_mx_attn(const char* who, const ra_attn_desc* desc, int32_t forma
 
 extern "C" {
 
-ra_status refadapt_mx_commit(int32_t batch, int32_t heads, int32_t n_ref, int32_t head_dim, int32_t dtype,
-                             int32_t format, ra_tensor k_ref, ra_tensor v_ref, ra_tensor q_ref, ra_mx_tensor k_mx,
-                             ra_mx_tensor v_mx, ra_mx_tensor q_mx, const int32_t* decision, int32_t* age, int32_t step,
-                             void* stream) {
+ra_status refadapt_mx_commit(const ra_mx_desc* desc, const ra_mx_args* args, void* stream) {
   ra_status s;
-  if ((s = check_mx_sizes("mx_commit", batch, heads, n_ref, head_dim, dtype, format)) != RA_OK) return s;
-  if (n_ref == 0) return ok();
   MxSet ms{};
-  const ra_tensor* const plain[3] = {&k_ref, &v_ref, &q_ref};
-  const ra_mx_tensor* const mx[3] = {&k_mx, &v_mx, &q_mx};
-  const char* const plain_name[3] = {"k_ref", "v_ref", "q_ref"};
-  const char* const mx_name[3] = {"k_mx", "v_mx", "q_mx"};
-  if ((s = mx_set(&ms, plain, plain_name, mx, mx_name, format, n_ref, head_dim, dtype)) != RA_OK) return s;
-  return launch_status(launch_mx_commit(dtype, format, batch, heads, n_ref, head_dim, ms, decision, age, step,
+  const char* const names[3] = {"k_ref", "v_ref", "q_ref"};
+  if ((s = mx_set("mx_commit", desc, args, names, &ms)) != RA_OK) return s;
+  if (ms.n == 0) return ok();
+  return launch_status(launch_mx_commit(desc->dtype, desc->format, desc->batch, desc->heads, desc->n_ref,
+                                        desc->head_dim, ms, args->decision, args->age, args->step,
                                         static_cast<hipStream_t>(stream)),
                        "mx_commit");
 }
 
-ra_status refadapt_mx_read(int32_t batch, int32_t heads, int32_t n_ref, int32_t head_dim, int32_t dtype, int32_t format,
-                           ra_mx_tensor k_mx, ra_mx_tensor v_mx, ra_mx_tensor q_mx, ra_tensor k_out, ra_tensor v_out,
-                           ra_tensor q_out, void* stream) {
+ra_status refadapt_mx_read(const ra_mx_desc* desc, const ra_mx_args* args, void* stream) {
   ra_status s;
-  if ((s = check_mx_sizes("mx_read", batch, heads, n_ref, head_dim, dtype, format)) != RA_OK) return s;
-  if (n_ref == 0) return ok();
   MxSet ms{};
-  const ra_tensor* const plain[3] = {&k_out, &v_out, &q_out};
-  const ra_mx_tensor* const mx[3] = {&k_mx, &v_mx, &q_mx};
-  const char* const plain_name[3] = {"k_out", "v_out", "q_out"};
-  const char* const mx_name[3] = {"k_mx", "v_mx", "q_mx"};
-  if ((s = mx_set(&ms, plain, plain_name, mx, mx_name, format, n_ref, head_dim, dtype)) != RA_OK) return s;
-  return launch_status(launch_mx_read(dtype, format, batch, heads, n_ref, head_dim, ms, nullptr, 3,
-                                      static_cast<hipStream_t>(stream)),
+  const char* const names[3] = {"k_out", "v_out", "q_out"};
+  if ((s = mx_set("mx_read", desc, args, names, &ms)) != RA_OK) return s;
+  if (ms.n == 0) return ok();
+  return launch_status(launch_mx_read(desc->dtype, desc->format, desc->batch, desc->heads, desc->n_ref, desc->head_dim,
+                                      ms, nullptr, 3, static_cast<hipStream_t>(stream)),
                        "mx_read");
 }
 

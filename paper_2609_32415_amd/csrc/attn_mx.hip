@@ -311,31 +311,47 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_mx_few_kernel(MxFewParams p) 
     }
     // Against the running maximum first: a lane's sum bounds each of its terms, so that a sum within 2^12 (NaN and
     // infinity are not) lets the maximum stay.
-    float part[2];
-    const auto pair = [&](int r) __attribute__((always_inline)) {
-      const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[2 * r], p.sc_log2, -m));
-      const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[2 * r + 1], p.sc_log2, -m));
-      part[r & 1] = r < 2 ? e0 + e1 : part[r & 1] + (e0 + e1);
-      bf16x2 w;
-      w[0] = (__bf16)e0;
-      w[1] = (__bf16)e1;
-      pw[r] = __builtin_bit_cast(uint32_t, w);
-      pin(pw[r]);
-      pin(part[r & 1]);
+    // A pair takes three steps (exponents, exponentials, sum and rounding) of consecutive slots, so that no instruction
+    // of a slot waits for another of it.
+    float part[2], x0 = 0.f, x1 = 0.f, e0 = 0.f, e1 = 0.f;
+    const auto step = [&](int r) __attribute__((always_inline)) {
+      if (r >= 2) {
+        const int k = r - 2;
+        part[k & 1] = k < 2 ? e0 + e1 : part[k & 1] + (e0 + e1);
+        bf16x2 w;
+        w[0] = (__bf16)e0;
+        w[1] = (__bf16)e1;
+        pw[k] = __builtin_bit_cast(uint32_t, w);
+        pin(pw[k]);
+        pin(part[k & 1]);
+      }
+      if (r >= 1 && r < 9) {
+        e0 = __builtin_amdgcn_exp2f(x0);
+        e1 = __builtin_amdgcn_exp2f(x1);
+        pin(e0);
+        pin(e1);
+      }
+      if (r < 8) {
+        x0 = fmaf(sc[2 * r], p.sc_log2, -m);
+        x1 = fmaf(sc[2 * r + 1], p.sc_log2, -m);
+        pin(x0);
+        pin(x1);
+      }
     };
-    bf16x8 va[3];
+    constexpr int AHEAD = DB;  // V operands in flight
+    bf16x8 va[AHEAD + 1];
     if constexpr (!FIRST) {
-      va[0] = v_operand(0);
-      va[1] = v_operand(1);
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) va[i] = v_operand(i);
     }
 #pragma unroll
     for (int i = 0; i < PV; ++i) {
       if constexpr (!FIRST) {
-        o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[i % 3], p_operand(prev, i / DB), o[i % DB], 0, 0, 0);
-        if (i + 2 < PV) va[(i + 2) % 3] = v_operand(i + 2);
+        o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[i % (AHEAD + 1)], p_operand(prev, i / DB), o[i % DB], 0, 0, 0);
+        if (i + AHEAD < PV) va[(i + AHEAD) % (AHEAD + 1)] = v_operand(i + AHEAD);
       }
 #pragma unroll
-      for (int r = 8 * i / PV; r < 8 * (i + 1) / PV; ++r) pair(r);
+      for (int r = 10 * i / PV; r < 10 * (i + 1) / PV; ++r) step(r);
       __builtin_amdgcn_sched_barrier(0);
     }
     if (__any(!(part[0] + part[1] <= BOUND))) {  // rare, and always at a wavefront's first tile
@@ -349,7 +365,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_mx_few_kernel(MxFewParams p) 
 #pragma unroll
       for (int i = 0; i < DB; ++i) o[i] *= a;
 #pragma unroll
-      for (int r = 0; r < 8; ++r) pair(r);
+      for (int r = 0; r < 10; ++r) step(r);
     }
     l += part[0] + part[1];
     float lsum = 0.f;

@@ -518,11 +518,33 @@ _MX = {"mxfp4": L.RA_MXFP4, "mxfp8": L.RA_MXFP8}
 MX_BLOCK = 32  # neighbouring elements of a row that share a scale
 
 
-def _here(name, t):
-    # on the GPU that the launch goes to
+def _elsewhere(name, t, dev):
     _on_gpu(name, t)
-    if t.device.index != torch._C._cuda_getDevice():
-        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch._C._cuda_getDevice()}")
+    raise ValueError(f"{name} is on {t.device}, the current device is cuda:{dev}")
+
+
+def _words(name, t, dtype, shape, dev):
+    """``_quad`` of a tensor that has to be on the current device ``dev``."""
+    if t is None:
+        return _NO_TENSOR
+    if t.get_device() != dev:
+        _elsewhere(name, t, dev)
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} differs from {dtype} {tuple(shape)}")
+    sb, sh, ss, sd = t.stride()
+    if sd != 1:
+        return _quad(name, t, dtype, shape)
+    return (t.data_ptr(), sb, sh, ss) if t.numel() else _NO_TENSOR
+
+
+def _int_word(name, t, dev):
+    if t is None:
+        return 0
+    if t.get_device() != dev:
+        _elsewhere(name, t, dev)
+    if t.dtype != torch.int32:
+        raise ValueError(f"{name} must be an int32 device tensor")
+    return t.data_ptr()
 
 
 def rope_frequencies(axes, theta=10000.0):
@@ -545,38 +567,37 @@ def rope(q, k=None, *, pos, freq, axis, pairing="interleaved", inverse=False, q_
     copied. ``inverse`` turns back, which is also the gradient: with it the gradient of an output gives that
     of the input. ``q_out=q`` works in place. Returns q_out, or (q_out, k_out) with ``k``.
     """
-    B, H, S, D = q.shape
-    dt = q.dtype
+    shape, dt, dev = q.shape, q.dtype, torch._C._cuda_getDevice()
+    B, H, S, D = shape
     if dt not in _DTYPES:
         raise ValueError(f"unsupported dtype {dt}")
     if pairing not in _PAIRING:
         raise ValueError(f"pairing must be one of {sorted(_PAIRING)}")
-    _here("q", q)
-    _here("pos", pos)
-    if pos.dtype not in _POS or pos.dim() not in (2, 3) or pos.stride(-1) != 1 and pos.shape[-1] != 1:
+    ps, pst = pos.shape, pos.stride()
+    if pos.get_device() != dev:
+        _elsewhere("pos", pos, dev)
+    if pos.dtype not in _POS or len(ps) not in (2, 3) or pst[-1] != 1 and ps[-1] != 1:
         raise ValueError("pos must be int32 or float32 [S, axes] or [B, S, axes] with contiguous axes")
-    if pos.shape[-2] != S or pos.dim() == 3 and pos.shape[0] not in (1, B):
-        raise ValueError(f"pos {tuple(pos.shape)} does not fit {B} x {S} rows")
+    if ps[-2] != S or len(ps) == 3 and ps[0] not in (1, B):
+        raise ValueError(f"pos {tuple(ps)} does not fit {B} x {S} rows")
     n = freq.numel()
     for name, t, want in (("freq", freq, torch.float64), ("axis", axis, torch.int32)):
-        if t.is_cuda or t.dtype != want or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+        if t.is_cuda or t.dtype != want or t.shape != (n,) or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous {want} host tensor, one entry a pair")
-    if k is not None:
-        _here("k", k)
-    elif k_out is not None:
-        raise ValueError("k_out without k")
-    q_out = torch.empty_like(q) if q_out is None else q_out
-    k_out = torch.empty_like(k) if k is not None and k_out is None else k_out
-    for name, t in (("q_out", q_out), ("k_out", k_out)):
-        if t is not None:
-            _here(name, t)
-    shape = (B, H, S, D)
-    views = [_view("q", q, dt), _view("k", k, dt, shape), _view("q_out", q_out, dt, shape),
-             _view("k_out", k_out, dt, shape)]
-    pos_sb = pos.stride(0) if pos.dim() == 3 and pos.shape[0] == B else 0
-    desc = L.ROPE_PACK.pack(B, H, S, D, _DTYPES[dt], n, _PAIRING[pairing], pos.shape[-1], int(bool(inverse)),
-                            _POS[pos.dtype], pos_sb, pos.stride(-2), freq.data_ptr(), axis.data_ptr())
-    L.refadapt_rope(desc, *views, _ptr(pos), _stream())
+    if q_out is None:
+        q_out = torch.empty_like(q)
+    if k is None:
+        if k_out is not None:
+            raise ValueError("k_out without k")
+    elif k_out is None:
+        k_out = torch.empty_like(k)
+    args = L.ROPE_ARGS_PACK.pack(
+        *_words("q", q, dt, shape, dev), *_words("k", k, dt, shape, dev), *_words("q_out", q_out, dt, shape, dev),
+        *_words("k_out", k_out, dt, shape, dev), pos.data_ptr())
+    desc = L.ROPE_DESC_PACK.pack(B, H, S, D, _DTYPES[dt], n, _PAIRING[pairing], ps[-1], 1 if inverse else 0,
+                                 _POS[pos.dtype], pst[0] if len(ps) == 3 and ps[0] == B else 0, pst[-2],
+                                 freq.data_ptr(), axis.data_ptr())
+    L.refadapt_rope_packed(desc, args, _stream())
     return q_out if k is None else (q_out, k_out)
 
 
@@ -613,61 +634,53 @@ def mx_tensor(shape, fmt, device):
 _NO_MX = (0,) * 8
 
 
-def _oct(name, t, fmt, shape):
-    """(codes, strides, scales, strides) of an MxTensor of this shape, checked."""
+def _mx_words(name, t, fmt, shape, dev):
+    """(codes, strides, scales, strides) of an MxTensor of this format and shape, checked."""
     if t is None:
         return _NO_MX
+    codes, scales = t.codes, t.scales
     if t.fmt != fmt:
         raise ValueError(f"{name}: format {t.fmt} differs from {fmt}")
     B, H, n, d = shape
-    for what, x, width in (("codes", t.codes, d // 2 if fmt == "mxfp4" else d), ("scales", t.scales, d // MX_BLOCK)):
-        _here(f"{name}.{what}", x)
-        if x.dtype != torch.uint8 or tuple(x.shape) != (B, H, n, width):
-            raise ValueError(f"{name}.{what} must be uint8 of shape {(B, H, n, width)}")
-        if x.stride(3) != 1 and width > 1:
-            raise ValueError(f"{name}.{what}: rows must be contiguous")
-    if 0 in shape:
+    width = d // 2 if fmt == "mxfp4" else d
+    if codes.get_device() != dev or scales.get_device() != dev:
+        _elsewhere(name, codes if codes.get_device() != dev else scales, dev)
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.shape != (B, H, n, width) or \
+            scales.shape != (B, H, n, d // MX_BLOCK):
+        raise ValueError(f"{name} must hold uint8 codes {(B, H, n, width)} and scales {(B, H, n, d // MX_BLOCK)}")
+    cb, ch, cs, c1 = codes.stride()
+    eb, eh, es, e1 = scales.stride()
+    if c1 != 1 or e1 != 1 and d > MX_BLOCK:
+        raise ValueError(f"{name}: rows of codes and of scales must be contiguous")
+    if not codes.numel():
         return _NO_MX
-    return (t.codes.data_ptr(), *t.codes.stride()[:3], t.scales.data_ptr(), *t.scales.stride()[:3])
+    return codes.data_ptr(), cb, ch, cs, scales.data_ptr(), eb, eh, es
 
 
-def _mx_view(name, t, fmt, shape):
-    return L.ra_mx_tensor(*_oct(name, t, fmt, shape))
-
-
-def _mx_format(*tensors):
-    fmt = next(t.fmt for t in tensors if t is not None)
-    if fmt not in _MX:
+def _mx_format(t):
+    if t.fmt not in _MX:
         raise ValueError(f"format must be one of {sorted(_MX)}")
-    return fmt
+    return t.fmt
 
 
 def mx_commit(k_ref, v_ref, k_mx, v_mx, decision=None, age=None, step=0, q_ref=None, q_mx=None):
     """``cache_commit`` into a quantised cache, through ``refadapt_mx_commit``: rounds the fresh reference K, V (and Q
     when ``q_ref``/``q_mx`` are given) into the ``MxTensor``s when ``decision`` is COMPUTE (or None); with ``v_ref``
     and ``v_mx`` None only K. One launch takes every pair."""
-    B, H, n_ref, D = k_ref.shape
-    dt = k_ref.dtype
+    shape, dt, dev, fmt = k_ref.shape, k_ref.dtype, torch._C._cuda_getDevice(), _mx_format(k_mx)
+    B, H, n_ref, D = shape
     if dt not in _DTYPES:
         raise ValueError(f"unsupported dtype {dt}")
     if (v_ref is None) != (v_mx is None):
         raise ValueError("v_ref and v_mx are both given or both None")
     if (q_ref is None) != (q_mx is None):
         raise ValueError("q_ref and q_mx are both given or both None")
-    for name, t in (("decision", decision), ("age", age)):
-        if t is not None:
-            _here(name, t)
-            if t.dtype != torch.int32:
-                raise ValueError(f"{name} must be int32")
-    for name, t in (("k_ref", k_ref), ("v_ref", v_ref), ("q_ref", q_ref)):
-        if t is not None:
-            _here(name, t)
-    fmt, shape = _mx_format(k_mx), k_ref.shape
-    L.refadapt_mx_commit(
-        B, H, n_ref, D, _DTYPES[dt], _MX[fmt], _view("k_ref", k_ref, dt), _view("v_ref", v_ref, dt, shape),
-        _view("q_ref", q_ref, dt, shape), _mx_view("k_mx", k_mx, fmt, shape), _mx_view("v_mx", v_mx, fmt, shape),
-        _mx_view("q_mx", q_mx, fmt, shape), _ptr(decision), _ptr(age), int(step), _stream(),
-    )
+    args = L.MX_ARGS_PACK.pack(
+        *_words("k_ref", k_ref, dt, shape, dev), *_words("v_ref", v_ref, dt, shape, dev),
+        *_words("q_ref", q_ref, dt, shape, dev), *_mx_words("k_mx", k_mx, fmt, shape, dev),
+        *_mx_words("v_mx", v_mx, fmt, shape, dev), *_mx_words("q_mx", q_mx, fmt, shape, dev),
+        _int_word("decision", decision, dev), _int_word("age", age, dev), int(step))
+    L.refadapt_mx_commit_packed(L.MX_DESC_PACK.pack(B, H, n_ref, D, _DTYPES[dt], _MX[fmt]), args, _stream())
 
 
 def mx_read(k_mx, v_mx=None, q_mx=None, dtype=torch.bfloat16, k_out=None, v_out=None, q_out=None):
@@ -675,23 +688,22 @@ def mx_read(k_mx, v_mx=None, q_mx=None, dtype=torch.bfloat16, k_out=None, v_out=
     of them. Returns a tuple of as many tensors as were given."""
     if dtype not in _DTYPES:
         raise ValueError(f"unsupported dtype {dtype}")
-    fmt, shape = _mx_format(k_mx), k_mx.shape
-    outs = []
-    for name, m, o in (("k", k_mx, k_out), ("v", v_mx, v_out), ("q", q_mx, q_out)):
-        if m is None and o is not None:
-            raise ValueError(f"{name}_out without {name}_mx")
-        if m is not None and o is None:
-            o = torch.empty(shape, dtype=dtype, device=k_mx.codes.device)
-        if o is not None:
-            _here(f"{name}_out", o)
-        outs.append(o)
+    shape, dev, fmt, where = k_mx.shape, torch._C._cuda_getDevice(), _mx_format(k_mx), k_mx.codes.device
     B, H, n, D = shape
-    L.refadapt_mx_read(
-        B, H, n, D, _DTYPES[dtype], _MX[fmt], _mx_view("k_mx", k_mx, fmt, shape), _mx_view("v_mx", v_mx, fmt, shape),
-        _mx_view("q_mx", q_mx, fmt, shape), *(_view(f"{n}_out", o, dtype, shape) for n, o in zip("kvq", outs)),
-        _stream(),
-    )
-    return tuple(o for o in outs if o is not None)
+    if k_out is None:
+        k_out = torch.empty(shape, dtype=dtype, device=where)
+    if v_mx is None and v_out is not None or q_mx is None and q_out is not None:
+        raise ValueError("v_out and q_out need v_mx and q_mx")
+    if v_mx is not None and v_out is None:
+        v_out = torch.empty(shape, dtype=dtype, device=where)
+    if q_mx is not None and q_out is None:
+        q_out = torch.empty(shape, dtype=dtype, device=where)
+    args = L.MX_ARGS_PACK.pack(
+        *_words("k_out", k_out, dtype, shape, dev), *_words("v_out", v_out, dtype, shape, dev),
+        *_words("q_out", q_out, dtype, shape, dev), *_mx_words("k_mx", k_mx, fmt, shape, dev),
+        *_mx_words("v_mx", v_mx, fmt, shape, dev), *_mx_words("q_mx", q_mx, fmt, shape, dev), 0, 0, 0)
+    L.refadapt_mx_read_packed(L.MX_DESC_PACK.pack(B, H, n, D, _DTYPES[dtype], _MX[fmt]), args, _stream())
+    return tuple(o for o in (k_out, v_out, q_out) if o is not None)
 
 
 def joint_attn_mx(q_tgt, k_tgt, v_tgt, *, k_mx, v_mx, q_mx=None, q_ref=None, k_ref=None, v_ref=None, qset="target",
@@ -700,52 +712,50 @@ def joint_attn_mx(q_tgt, k_tgt, v_tgt, *, k_mx, v_mx, q_mx=None, q_ref=None, k_r
     """``joint_attn`` with ``kvsrc`` "cache" or "device" whose cached reference K, V (and queries, ``q_mx``) are
     ``MxTensor``s, through ``refadapt_joint_attn_mx``. ``workspace``: None allocates what the library asks for, a
     uint8 device tensor is used as given (``attn_mx_workspace``). Returns an ``AttnOut``."""
-    B, H, n_tgt, D = q_tgt.shape
-    dt = q_tgt.dtype
+    shp_t, dt, dev, where = q_tgt.shape, q_tgt.dtype, torch._C._cuda_getDevice(), q_tgt.device
+    B, H, n_tgt, D = shp_t
     if dt not in _DTYPES:
         raise ValueError(f"unsupported dtype {dt}")
     if kvsrc not in ("cache", "device"):
         raise ValueError('a quantised cache needs kvsrc "cache" or "device"')
-    for name, t in (("q_tgt", q_tgt), ("k_tgt", k_tgt), ("v_tgt", v_tgt), ("q_ref", q_ref), ("k_ref", k_ref),
-                    ("v_ref", v_ref), ("o_tgt", o_tgt), ("o_ref", o_ref), ("decision", decision)):
-        if t is not None:
-            _here(name, t)
-    if decision is not None and decision.dtype != torch.int32:
-        raise ValueError("decision must be an int32 device tensor")
-    fmt, n_ref, dev = _mx_format(k_mx), k_mx.shape[2], q_tgt.device
-    shp_t, shp_r = (B, H, n_tgt, D), (B, H, n_ref, D)
+    fmt, n_ref = _mx_format(k_mx), k_mx.codes.shape[2]
+    shp_r = (B, H, n_ref, D)
     ref_queries = (kvsrc == "device" or qset == "all") and n_ref > 0
     if o_tgt is None:
-        o_tgt = torch.empty(shp_t, dtype=dt, device=dev)
+        o_tgt = torch.empty(shp_t, dtype=dt, device=where)
     if ref_queries and o_ref is None:
-        o_ref = torch.empty(shp_r, dtype=dt, device=dev)
+        o_ref = torch.empty(shp_r, dtype=dt, device=where)
 
     def opt(name, flag, shape):
         if flag is None or flag is False:
             return None
-        return _f32_out(name, None if flag is True else flag, shape, dev)
+        return _f32_out(name, None if flag is True else flag, shape, where)
 
     mass_t = opt("ref_mass", ref_mass, (B, H, n_tgt))
     lse_t = opt("lse", lse, (B, H, n_tgt, 2))
     mrq_t = opt("ref_mass_refq", ref_mass_refq, (B, H, n_ref)) if n_ref > 0 else None
-    desc = (B, H, D, n_ref, n_tgt, _DTYPES[dt], ctypes.c_float(float(scale)).value if scale else 0.0, _QSET[qset],
-            _KVSRC[kvsrc])
+    desc = L.DESC_PACK.pack(B, H, D, n_ref, n_tgt, _DTYPES[dt], ctypes.c_float(float(scale)).value if scale else 0.0,
+                            _QSET[qset], _KVSRC[kvsrc])
     if workspace is None:
-        nbytes = L.refadapt_joint_attn_mx_workspace_size(L.ra_attn_desc(*desc), _MX[fmt], q_mx is not None)
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        nbytes = L.refadapt_joint_attn_mx_workspace_size_packed(desc, _MX[fmt], q_mx is not None)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=where) if nbytes else None
     else:
-        _here("workspace", workspace)
+        ws = workspace
+        if ws.get_device() != dev:
+            _elsewhere("workspace", ws, dev)
+        nbytes = _nbytes(ws)
     word = lambda t: 0 if t is None else t.data_ptr()
     args = L.ARGS_PACK.pack(
-        *_quad("q_tgt", q_tgt, dt, shp_t), *_quad("k_tgt", k_tgt, dt, shp_t), *_quad("v_tgt", v_tgt, dt, shp_t),
-        *_quad("q_ref", q_ref, dt, shp_r), *_quad("k_ref", k_ref, dt, shp_r), *_quad("v_ref", v_ref, dt, shp_r),
-        *_NO_TENSOR, *_NO_TENSOR, word(decision), *_quad("o_tgt", o_tgt, dt, shp_t), *_quad("o_ref", o_ref, dt, shp_r),
-        word(mass_t), word(lse_t), word(mrq_t), word(workspace), _nbytes(workspace), *_NO_SEG_FIELDS, 0, *_NO_TENSOR,
-        0 if clock_probe is None else _probe_ptr(clock_probe),
+        *_words("q_tgt", q_tgt, dt, shp_t, dev), *_words("k_tgt", k_tgt, dt, shp_t, dev),
+        *_words("v_tgt", v_tgt, dt, shp_t, dev), *_words("q_ref", q_ref, dt, shp_r, dev),
+        *_words("k_ref", k_ref, dt, shp_r, dev), *_words("v_ref", v_ref, dt, shp_r, dev), *_NO_TENSOR, *_NO_TENSOR,
+        _int_word("decision", decision, dev), *_words("o_tgt", o_tgt, dt, shp_t, dev),
+        *_words("o_ref", o_ref, dt, shp_r, dev), word(mass_t), word(lse_t), word(mrq_t), word(ws), nbytes,
+        *_NO_SEG_FIELDS, 0, *_NO_TENSOR, 0 if clock_probe is None else _probe_ptr(clock_probe),
     )
-    cache = L.MX_CACHE_PACK.pack(_MX[fmt], *_oct("k_mx", k_mx, fmt, shp_r), *_oct("v_mx", v_mx, fmt, shp_r),
-                                 *_oct("q_mx", q_mx, fmt, shp_r))
-    L.refadapt_joint_attn_mx_packed(L.DESC_PACK.pack(*desc), args, cache, _stream())
+    cache = L.MX_CACHE_PACK.pack(_MX[fmt], *_mx_words("k_mx", k_mx, fmt, shp_r, dev),
+                                 *_mx_words("v_mx", v_mx, fmt, shp_r, dev), *_mx_words("q_mx", q_mx, fmt, shp_r, dev))
+    L.refadapt_joint_attn_mx_packed(desc, args, cache, _stream())
     return AttnOut(o_tgt, o_ref if ref_queries else None, mass_t, lse_t, mrq_t)
 
 

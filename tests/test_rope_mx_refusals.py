@@ -25,7 +25,7 @@ def _rope(freq=(1.0, 0.5), axis=(0, 1), q=_t(), k=NONE, qo=_t(0x9000), ko=NONE, 
              n_axes=2, inverse=0, pos_dtype=L.RA_POS_I32, pos_stride_b=0, pos_stride_s=2,
              freq=ctypes.addressof(f) if tables else None, axis=ctypes.addressof(a))
     d.update(kw)
-    st = L.LIB.refadapt_rope(ctypes.byref(L.ra_rope_desc(**d)), q, k, qo, ko, pos, None)
+    st = L.LIB.refadapt_rope(ctypes.byref(L.ra_rope_desc(**d)), ctypes.byref(L.ra_rope_args(q, k, qo, ko, pos)), None)
     return st, L.refadapt_last_error()
 
 
@@ -63,7 +63,8 @@ def test_rope(kw, status, msg):
 
 def test_rope_of_no_rows_and_null_desc():
     assert _rope(rows=0, q=NONE, qo=NONE, pos=None)[0] == L.RA_OK
-    assert L.LIB.refadapt_rope(None, NONE, NONE, NONE, NONE, None, None) == L.RA_EINVAL
+    assert L.LIB.refadapt_rope(None, ctypes.byref(L.ra_rope_args()), None) == L.RA_EINVAL
+    assert L.LIB.refadapt_rope(ctypes.byref(L.ra_rope_desc()), None, None) == L.RA_EINVAL
 
 
 CASES = [
@@ -89,19 +90,20 @@ CASES = [
 ]
 
 
-def _call(fn, read, batch=1, heads=2, n_ref=10, head_dim=128, dtype=L.RA_BF16, fmt=L.RA_MXFP4, k=_t(), v=NONE, q=NONE,
+def _call(fn, batch=1, heads=2, n_ref=10, head_dim=128, dtype=L.RA_BF16, fmt=L.RA_MXFP4, k=_t(), v=NONE, q=NONE,
           km=_m(), vm=NO_MX, qm=NO_MX):
-    plain, mx = (k, v, q), (km, vm, qm)
-    head = (batch, heads, n_ref, head_dim, dtype, fmt)
-    return fn(*head, *mx, *plain, None) if read else fn(*head, *plain, *mx, None, None, 0, None)
+    return fn(ctypes.byref(L.ra_mx_desc(batch, heads, n_ref, head_dim, dtype, fmt)),
+              ctypes.byref(L.ra_mx_args(k, v, q, km, vm, qm)), None)
 
 
 @pytest.mark.parametrize("kw,status,msg", CASES)
 def test_commit_and_read(kw, status, msg):
-    for fn, read in ((L.LIB.refadapt_mx_commit, False), (L.LIB.refadapt_mx_read, True)):
-        st = _call(fn, read, **kw)
+    for fn in (L.LIB.refadapt_mx_commit, L.LIB.refadapt_mx_read):
+        st = _call(fn, **kw)
         assert st == status and msg in L.refadapt_last_error(), (st, L.refadapt_last_error())
-        assert _call(fn, read, n_ref=0, k=NONE, km=NO_MX) == L.RA_OK
+        assert _call(fn, n_ref=0, k=NONE, km=NO_MX) == L.RA_OK
+        assert fn(None, ctypes.byref(L.ra_mx_args()), None) == L.RA_EINVAL
+        assert fn(ctypes.byref(L.ra_mx_desc()), None, None) == L.RA_EINVAL
 
 
 def _attn(cache=None, ws=0x10000, ws_bytes=1 << 30, desc=None, args=None):
