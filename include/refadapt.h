@@ -436,7 +436,7 @@ typedef struct {
  * Errors: RA_EINVAL (null desc or args, null K tensors, a pair with one NULL side,
  * sizes, enums),
  * RA_EUNSUPPORTED (head_dim not a multiple of 32, alignment, batch * heads >
- * 65535).
+ * 65535, n_ref * head_dim > 2^34).
  */
 ra_status refadapt_mx_commit(const ra_mx_desc* desc, const ra_mx_args* args, void* stream);
 

@@ -575,6 +575,8 @@ ra_status check_mx_sizes(const char* who, int32_t batch, int32_t heads, int32_t 
   if (head_dim < 32 || head_dim % 32 != 0)
     return fail(RA_EUNSUPPORTED, "%s: head_dim %d must be a positive multiple of 32", who, head_dim);
   if ((int64_t)batch * heads > 65535) return fail(RA_EUNSUPPORTED, "%s: batch*heads must be <= 65535", who);
+  if ((int64_t)n_ref * head_dim > (int64_t(1) << 34))
+    return fail(RA_EUNSUPPORTED, "%s: %d rows of %d elements are too many for one launch", who, n_ref, head_dim);
   return RA_OK;
 }
 

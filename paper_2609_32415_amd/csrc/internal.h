@@ -130,12 +130,13 @@ struct MxSet {
   View plain[3];
   MxView mx[3];
   int32_t n;
+  int32_t octs, oct_shift;  // runs of 8 elements in a row and their log2 (or -1), set by the launcher
 };
 hipError_t launch_mx_commit(int dtype, int format, int32_t B, int32_t H, int32_t n_ref, int32_t head_dim,
-                            const MxSet& ms, const int32_t* decision, int32_t* age, int32_t step, hipStream_t stream);
+                            MxSet ms, const int32_t* decision, int32_t* age, int32_t step, hipStream_t stream);
 // With a decision word the first `always` tensors are read unless it is COMPUTE, the others on REACTIVATE only.
 hipError_t launch_mx_read(int dtype, int format, int32_t B, int32_t H, int32_t n_ref, int32_t head_dim,
-                          const MxSet& ms, const int32_t* decision, int32_t always, hipStream_t stream);
+                          MxSet ms, const int32_t* decision, int32_t always, hipStream_t stream);
 
 // bf16 attention of few target rows over a quantised cache: workgroups of kFewWaves wavefronts and kFewRows query
 // rows, key tiles of kFewKeys, the keys of a (batch, head) in `chunks` ranges.

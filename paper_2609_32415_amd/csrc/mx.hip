@@ -24,85 +24,122 @@ namespace refadapt {
 namespace {
 
 constexpr int MX_THREADS = 256;
+constexpr int MX_UNROLL = 4;  // octs (8 elements) of a thread in flight
+constexpr int MX_WG = MX_THREADS * MX_UNROLL;
 
-// A thread takes 8 elements, four threads a block; blockIdx.z is the tensor of the set.
+// An oct of a head: its row and its place there.
+struct OctAt {
+  int32_t row, col;
+};
+__device__ __forceinline__ OctAt oct_at(const MxSet& ms, uint32_t v) {
+  const uint32_t row = ms.oct_shift >= 0 ? v >> ms.oct_shift : v / (uint32_t)ms.octs;
+  return OctAt{(int32_t)row, (int32_t)(v - row * (uint32_t)ms.octs)};
+}
+
+// blockIdx.x: (batch, head), y: octs of it, z: tensor of the set. Four threads share a block: a row's octs come in
+// fours, so that they are active together.
 template <bool FP4, bool BF16>
-__global__ __launch_bounds__(MX_THREADS) void mx_commit_kernel(MxSet ms, int32_t H, int32_t n_rows, int32_t vpr,
+__global__ __launch_bounds__(MX_THREADS) void mx_commit_kernel(MxSet ms, int32_t H, uint32_t n_octs,
                                                                const int32_t* decision, int32_t* age, int32_t step) {
   if (decision && *decision != DEC_COMPUTE) return;
-  const int bh = blockIdx.y;
+  const int bh = blockIdx.x;
   const int b = bh / H, h = bh - b * H;
   const View src = ms.plain[blockIdx.z];
   const MxView dst = ms.mx[blockIdx.z];
-  const int esz = BF16 ? 2 : 4;
+  constexpr int esz = BF16 ? 2 : 4;
   const char* sb = static_cast<const char*>(src.p) + (b * src.sb + h * src.sh) * esz;
   uint8_t* cb = dst.codes + b * dst.sb + h * dst.sh;
   uint8_t* eb = dst.scales + b * dst.eb + h * dst.eh;
-  const int64_t nvec = (int64_t)n_rows * vpr;
-  for (int64_t v = (int64_t)blockIdx.x * MX_THREADS + threadIdx.x; v < nvec; v += (int64_t)gridDim.x * MX_THREADS) {
-    const int64_t row = v / vpr;
-    const int col = (int)(v - row * vpr);  // of 8 elements
-    const Oct x = load_oct<BF16>(sb + (row * src.ss + 8 * col) * esz);
-    // a row's vectors come in whole blocks of four, so the four lanes of a block are active together
-    uint32_t m = max_bits(x);
-    m = max(m, (uint32_t)__shfl_xor((int)m, 1));
-    m = max(m, (uint32_t)__shfl_xor((int)m, 2));
-    const uint32_t e = scale_byte<FP4>(m);
-    store_codes<FP4>(cb + row * dst.ss + (FP4 ? 4 : 8) * col, x, e);
-    if ((col & 3) == 0) eb[row * dst.es + (col >> 2)] = (uint8_t)e;
+  for (uint32_t v0 = blockIdx.y * MX_WG + threadIdx.x; v0 < n_octs; v0 += gridDim.y * MX_WG) {
+    OctAt at[MX_UNROLL];
+    RawOct<BF16> raw[MX_UNROLL];
+#pragma unroll
+    for (int u = 0; u < MX_UNROLL; ++u) {
+      at[u] = oct_at(ms, v0 + u * MX_THREADS);
+      if (v0 + u * MX_THREADS < n_octs) raw[u].load(sb + (at[u].row * src.ss + 8 * at[u].col) * esz);
+    }
+#pragma unroll
+    for (int u = 0; u < MX_UNROLL; ++u) {
+      if (v0 + u * MX_THREADS >= n_octs) break;
+      const Oct x = raw[u].widen();
+      uint32_t m = max_bits(x);
+      m = max(m, (uint32_t)__shfl_xor((int)m, 1));
+      m = max(m, (uint32_t)__shfl_xor((int)m, 2));
+      const uint32_t e = scale_byte<FP4>(m);
+      store_codes<FP4>(cb + at[u].row * dst.ss + (FP4 ? 4 : 8) * at[u].col, x, e);
+      if ((at[u].col & 3) == 0) eb[at[u].row * dst.es + (at[u].col >> 2)] = (uint8_t)e;
+    }
   }
   if (age && blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == 0) *age = step;
 }
 
 // `decision` (null: always): the tensors of `always` are read unless it is COMPUTE, the rest on REACTIVATE.
 template <bool FP4, bool BF16>
-__global__ __launch_bounds__(MX_THREADS) void mx_read_kernel(MxSet ms, int32_t H, int32_t n_rows, int32_t vpr,
+__global__ __launch_bounds__(MX_THREADS) void mx_read_kernel(MxSet ms, int32_t H, uint32_t n_octs,
                                                              const int32_t* decision, int32_t always) {
   if (decision) {
     const int dec = *decision;
     if (dec == DEC_COMPUTE || ((int)blockIdx.z >= always && dec != DEC_REACTIVATE)) return;
   }
-  const int bh = blockIdx.y;
+  const int bh = blockIdx.x;
   const int b = bh / H, h = bh - b * H;
   const View dst = ms.plain[blockIdx.z];
   const MxView src = ms.mx[blockIdx.z];
-  const int esz = BF16 ? 2 : 4;
+  constexpr int esz = BF16 ? 2 : 4;
   char* db = static_cast<char*>(const_cast<void*>(dst.p)) + (b * dst.sb + h * dst.sh) * esz;
   const uint8_t* cb = src.codes + b * src.sb + h * src.sh;
   const uint8_t* eb = src.scales + b * src.eb + h * src.eh;
-  const int64_t nvec = (int64_t)n_rows * vpr;
-  for (int64_t v = (int64_t)blockIdx.x * MX_THREADS + threadIdx.x; v < nvec; v += (int64_t)gridDim.x * MX_THREADS) {
-    const int64_t row = v / vpr;
-    const int col = (int)(v - row * vpr);
-    const u32x2 c = load_codes<FP4>(cb + row * src.ss + (FP4 ? 4 : 8) * col);
-    const u32x4 w = decode_oct<FP4>(c, scale_bits(eb[row * src.es + (col >> 2)]));
-    store_oct<BF16>(db + (row * dst.ss + 8 * col) * esz, w);
+  for (uint32_t v0 = blockIdx.y * MX_WG + threadIdx.x; v0 < n_octs; v0 += gridDim.y * MX_WG) {
+    OctAt at[MX_UNROLL];
+    u32x2 c[MX_UNROLL];
+    uint32_t e[MX_UNROLL];
+#pragma unroll
+    for (int u = 0; u < MX_UNROLL; ++u) {
+      at[u] = oct_at(ms, v0 + u * MX_THREADS);
+      if (v0 + u * MX_THREADS < n_octs) {
+        c[u] = load_codes<FP4>(cb + at[u].row * src.ss + (FP4 ? 4 : 8) * at[u].col);
+        e[u] = eb[at[u].row * src.es + (at[u].col >> 2)];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < MX_UNROLL; ++u) {
+      if (v0 + u * MX_THREADS >= n_octs) break;
+      store_oct<BF16>(db + (at[u].row * dst.ss + 8 * at[u].col) * esz, decode_oct<FP4>(c[u], scale_bits(e[u])));
+    }
   }
 }
 
-dim3 mx_grid(int32_t bh, int32_t n_rows, int32_t head_dim, int n) {
-  const int64_t nvec = (int64_t)n_rows * (head_dim / 8);
-  const int64_t gx = (nvec + MX_THREADS * 4 - 1) / (MX_THREADS * 4);
-  return dim3((unsigned)(gx < 1 ? 1 : gx > 1024 ? 1024 : gx), bh, n);
+// Sizes of a launch over n_rows x head_dim of every (batch, head). Octs are numbered in 32 bits with room for a
+// workgroup past the last (the host refuses more).
+uint32_t mx_octs(MxSet& ms, int32_t n_rows, int32_t head_dim) {
+  ms.octs = head_dim / 8;
+  ms.oct_shift = (ms.octs & (ms.octs - 1)) == 0 ? __builtin_ctz(ms.octs) : -1;
+  return (uint32_t)n_rows * (uint32_t)ms.octs;
+}
+dim3 mx_grid(int32_t bh, uint32_t n_octs, int n) {
+  const uint32_t gy = (n_octs + MX_WG - 1) / MX_WG;
+  return dim3(bh, gy > 4096 ? 4096 : gy, n);
 }
 
 }  // namespace
 
 hipError_t launch_mx_commit(int dtype, int format, int32_t B, int32_t H, int32_t n_ref, int32_t head_dim,
-                            const MxSet& ms, const int32_t* decision, int32_t* age, int32_t step, hipStream_t stream) {
-  const dim3 grid = mx_grid(B * H, n_ref, head_dim, ms.n);
+                            MxSet ms, const int32_t* decision, int32_t* age, int32_t step, hipStream_t stream) {
+  const uint32_t n_octs = mx_octs(ms, n_ref, head_dim);
+  const dim3 grid = mx_grid(B * H, n_octs, ms.n);
   const auto run = [&](auto* kernel) {
-    return launch_kernel(kernel, grid, dim3(MX_THREADS), 0, stream, ms, H, n_ref, head_dim / 8, decision, age, step);
+    return launch_kernel(kernel, grid, dim3(MX_THREADS), 0, stream, ms, H, n_octs, decision, age, step);
   };
   if (format == MX_FP4) return dtype == 0 ? run(mx_commit_kernel<true, true>) : run(mx_commit_kernel<true, false>);
   return dtype == 0 ? run(mx_commit_kernel<false, true>) : run(mx_commit_kernel<false, false>);
 }
 
 hipError_t launch_mx_read(int dtype, int format, int32_t B, int32_t H, int32_t n_ref, int32_t head_dim,
-                          const MxSet& ms, const int32_t* decision, int32_t always, hipStream_t stream) {
-  const dim3 grid = mx_grid(B * H, n_ref, head_dim, ms.n);
+                          MxSet ms, const int32_t* decision, int32_t always, hipStream_t stream) {
+  const uint32_t n_octs = mx_octs(ms, n_ref, head_dim);
+  const dim3 grid = mx_grid(B * H, n_octs, ms.n);
   const auto run = [&](auto* kernel) {
-    return launch_kernel(kernel, grid, dim3(MX_THREADS), 0, stream, ms, H, n_ref, head_dim / 8, decision, always);
+    return launch_kernel(kernel, grid, dim3(MX_THREADS), 0, stream, ms, H, n_octs, decision, always);
   };
   if (format == MX_FP4) return dtype == 0 ? run(mx_read_kernel<true, true>) : run(mx_read_kernel<true, false>);
   return dtype == 0 ? run(mx_read_kernel<false, true>) : run(mx_read_kernel<false, false>);

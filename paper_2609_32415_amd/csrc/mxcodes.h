@@ -19,26 +19,29 @@ struct Oct {
   float f[8];
 };
 
+// The same as loaded.
 template <bool BF16>
-__device__ __forceinline__ Oct load_oct(const char* p) {
-  Oct x;
-  if constexpr (BF16) {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x.f[2 * i] = __uint_as_float(w[i] << 16);
-      x.f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  } else {
-    const u32x4 a = reinterpret_cast<const u32x4*>(p)[0], b = reinterpret_cast<const u32x4*>(p)[1];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x.f[i] = __uint_as_float(a[i]);
-      x.f[4 + i] = __uint_as_float(b[i]);
-    }
+struct RawOct {
+  u32x4 w[BF16 ? 1 : 2];
+  __device__ __forceinline__ void load(const char* p) {
+    w[0] = reinterpret_cast<const u32x4*>(p)[0];
+    if constexpr (!BF16) w[1] = reinterpret_cast<const u32x4*>(p)[1];
   }
-  return x;
-}
+  __device__ __forceinline__ Oct widen() const {
+    Oct x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (BF16) {
+        x.f[2 * i] = __uint_as_float(w[0][i] << 16);
+        x.f[2 * i + 1] = __uint_as_float(w[0][i] & 0xffff0000u);
+      } else {
+        x.f[i] = __uint_as_float(w[0][i]);
+        x.f[4 + i] = __uint_as_float(w[1][i]);
+      }
+    }
+    return x;
+  }
+};
 
 // Stores eight bf16 values (pairs, the first in the low half), widened for fp32.
 template <bool BF16>

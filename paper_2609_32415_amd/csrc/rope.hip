@@ -13,6 +13,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "internal.h"
 
 namespace refadapt {
@@ -22,14 +24,14 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int ROPE_THREADS = 256;
+constexpr int ROPE_WGS = 1024;
 
 // Elements of a 16-byte piece, widened to fp32 and rounded back to nearest.
 template <bool BF16>
 struct Piece {
   static constexpr int N = BF16 ? 8 : 4;
   float f[N];
-  __device__ __forceinline__ void load(const char* p) {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+  __device__ __forceinline__ void widen(u32x4 w) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if constexpr (BF16) {
@@ -98,34 +100,48 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_kernel(RopeParams p) {
       cs[i] = turn(pos * freq[pair0 + i]);
     }
   }
+  // heads [h0, h1) of one tensor after the other, UNROLL pieces in flight
   const int h0 = blockIdx.y * p.heads_per, h1 = min(p.H, h0 + p.heads_per);
   for (int t = 0; t < p.n; ++t) {
     const View x = p.x[t], y = p.y[t];
     const char* xp = static_cast<const char*>(x.p) + (b * x.sb + s * x.ss + col) * esz;
     char* yp = static_cast<char*>(const_cast<void*>(y.p)) + (b * y.sb + s * y.ss + col) * esz;
-    for (int h = h0; h < h1; ++h) {
-      Piece<BF16> u, w;
-      u.load(xp + h * x.sh * esz);
-      if constexpr (HALF) {
-        if (turns) {
-          w.load(xp + (h * x.sh + p.n_pairs) * esz);
+    constexpr int UNROLL = HALF ? 2 : 4;
+    for (int hb = h0; hb < h1; hb += UNROLL) {
+      u32x4 uw[UNROLL], ww[UNROLL];
 #pragma unroll
-          for (int i = 0; i < N; ++i) {
-            const float a = u.f[i], c = w.f[i];
-            u.f[i] = a * cs[i].x - c * cs[i].y;
-            w.f[i] = a * cs[i].y + c * cs[i].x;
-          }
-          w.store(yp + (h * y.sh + p.n_pairs) * esz);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-          const float a = u.f[2 * i], c = u.f[2 * i + 1];
-          u.f[2 * i] = i < n_turn ? a * cs[i].x - c * cs[i].y : a;
-          u.f[2 * i + 1] = i < n_turn ? a * cs[i].y + c * cs[i].x : c;
-        }
+      for (int k = 0; k < UNROLL; ++k) {
+        if (hb + k >= h1) break;
+        uw[k] = *reinterpret_cast<const u32x4*>(xp + (hb + k) * x.sh * esz);
+        if (HALF && turns) ww[k] = *reinterpret_cast<const u32x4*>(xp + ((hb + k) * x.sh + p.n_pairs) * esz);
       }
-      u.store(yp + h * y.sh * esz);
+#pragma unroll
+      for (int k = 0; k < UNROLL; ++k) {
+        if (hb + k >= h1) break;
+        Piece<BF16> u;
+        u.widen(uw[k]);
+        if constexpr (HALF) {
+          if (turns) {
+            Piece<BF16> w;
+            w.widen(ww[k]);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+              const float a = u.f[i], c = w.f[i];
+              u.f[i] = a * cs[i].x - c * cs[i].y;
+              w.f[i] = a * cs[i].y + c * cs[i].x;
+            }
+            w.store(yp + ((hb + k) * y.sh + p.n_pairs) * esz);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < NP; ++i) {
+            const float a = u.f[2 * i], c = u.f[2 * i + 1];
+            u.f[2 * i] = i < n_turn ? a * cs[i].x - c * cs[i].y : a;
+            u.f[2 * i + 1] = i < n_turn ? a * cs[i].y + c * cs[i].x : c;
+          }
+        }
+        u.store(yp + (hb + k) * y.sh * esz);
+      }
     }
   }
 }
@@ -136,8 +152,11 @@ hipError_t launch_rope(int dtype, bool half, int32_t head_dim, RopeParams p, hip
   const int n = dtype == 0 ? 8 : 4;
   p.pieces = half ? (head_dim - p.n_pairs) / n : head_dim / n;
   const int64_t gx = ((int64_t)p.B * p.S * p.pieces + ROPE_THREADS - 1) / ROPE_THREADS;
-  p.heads_per = p.H;
-  const dim3 grid((unsigned)gx, 1);
+  // Heads are cut into ranges until the launch holds ROPE_WGS workgroups; each range forms the angles again, about
+  // the work of turning four heads.
+  const int64_t cuts = std::max<int64_t>(1, std::min<int64_t>((p.H + 3) / 4, (ROPE_WGS + gx - 1) / gx));
+  p.heads_per = (int32_t)((p.H + cuts - 1) / cuts);
+  const dim3 grid((unsigned)gx, (unsigned)((p.H + p.heads_per - 1) / p.heads_per));
   const auto run = [&](auto* kernel) { return launch_kernel(kernel, grid, dim3(ROPE_THREADS), 0, stream, p); };
   if (half) return dtype == 0 ? run(rope_kernel<true, true>) : run(rope_kernel<false, true>);
   return dtype == 0 ? run(rope_kernel<true, false>) : run(rope_kernel<false, false>);

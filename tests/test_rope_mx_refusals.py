@@ -74,6 +74,7 @@ CASES = [
     (dict(fmt=2), L.RA_EINVAL, "format"),
     (dict(head_dim=48), L.RA_EUNSUPPORTED, "head_dim"),
     (dict(heads=65536), L.RA_EUNSUPPORTED, "65535"),
+    (dict(n_ref=(1 << 27) + 1), L.RA_EUNSUPPORTED, "too many"),
     (dict(k=_t(0)), L.RA_EINVAL, "k_"),
     (dict(km=NO_MX), L.RA_EINVAL, "k_mx"),
     (dict(km=_m(scales=0)), L.RA_EINVAL, "k_mx"),
