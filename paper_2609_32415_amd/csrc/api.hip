@@ -622,28 +622,51 @@ ra_status mx_set(const char* who, const ra_mx_desc* desc, const ra_mx_args* args
   return RA_OK;
 }
 
-// Attention over a quantised cache takes one of two ways. Up to kFewMaxRows target rows a kernel reads the codes
-// itself; other calls read the cache back into the workspace and attend over that with refadapt_joint_attn's kernels.
-constexpr int kFewMaxRows = 256;
+// Attention over a quantised cache takes one of two ways. A kernel for few target rows reads the codes itself, each
+// query tile of 32 rows on its own; other calls read the cache back into the workspace and attend over that with
+// refadapt_joint_attn's kernels, which share a tile of keys between 256 rows. The first takes up to 256 target rows,
+// and up to 1024 where all query tiles run at once. Measured, in us, first against second way: 24 heads of 128, 4352
+// reference rows in 4 bits, 61 rows 17 / 36, 256 28 / 45, 512 58 / 58, 1024 105 / 93; 3 heads, 1024 rows 29 / 36; 48 (batch,
+// head) pairs, 256 rows 54 / 67; in 8 bits 24 heads, 256 rows 35 / 46, 512 70 / 61.
+constexpr int kFewMaxRows = 256, kFewMaxRowsAtOnce = 1024;
 
-bool few_rows(const ra_attn_desc& d) {
-  return d.dtype == RA_BF16 && d.kvsrc == RA_KV_CACHE && d.n_ref > 0 && !launch_mode(d, false).all &&
-         d.n_tgt <= kFewMaxRows;
+bool few_rows(const ra_attn_desc& d, int format) {
+  if (d.dtype != RA_BF16 || d.kvsrc != RA_KV_CACHE || d.n_ref == 0 || launch_mode(d, false).all) return false;
+  if (d.n_tgt <= kFewMaxRows) return true;
+  const int64_t tiles = (int64_t)d.batch * d.heads * ((d.n_tgt + kFewRows - 1) / kFewRows);
+  return d.n_tgt <= kFewMaxRowsAtOnce && tiles <= attn_mx_few_slots(d.head_dim, format);
 }
 
-// Key ranges of a few-rows launch: as many as fill the CUs, with a tile for every wavefront.
+// Key ranges of a few-rows launch, from its estimated time: rounds of workgroups, a step (one tile of every wavefront) at
+// a time, each round with its start and end; more than one range adds the merge. Measured: 1.15 us a step at head dim
+// 128 in 4 bits, 1.55 in 8, 6 us to start and end a workgroup, 4 us for a merge.
 struct FewPlan {
   int64_t q_tiles, key_tiles, chunks, rows;  // rows: of partial results
+  double us;
   size_t o_bytes(int head_dim) const { return (size_t)rows * head_dim * sizeof(float); }
   size_t bytes(int head_dim) const { return o_bytes(head_dim) + (size_t)rows * 5 * sizeof(float); }
 };
 
-FewPlan few_plan(const ra_attn_desc& d) {
-  const int64_t bh = (int64_t)d.batch * d.heads, cus = attn_bf16_slots(d.head_dim, kAttnBf16BM).cus;
+FewPlan few_plan(const ra_attn_desc& d, int format) {
+  const int64_t bh = (int64_t)d.batch * d.heads;
+  const int64_t slots = attn_mx_few_slots(d.head_dim, format);
   FewPlan f{};
   f.q_tiles = (d.n_tgt + kFewRows - 1) / kFewRows;
   f.key_tiles = ((int64_t)d.n_ref + kFewKeys - 1) / kFewKeys + (d.n_tgt + kFewKeys - 1) / kFewKeys;
-  f.chunks = std::max<int64_t>(1, std::min(cus / (bh * f.q_tiles), (f.key_tiles + kFewWaves - 1) / kFewWaves));
+  f.chunks = 1;
+  const double step = (format == RA_MXFP4 ? 1.15 : 1.55) * (d.head_dim == 128 ? 1.0 : 0.6), start = 6.0, merge = 4.0;
+  const int64_t most = std::min<int64_t>(64, (f.key_tiles + kFewWaves - 1) / kFewWaves);
+  for (int64_t c = 1; c <= most && slots > 0; ++c) {
+    const int64_t items = bh * f.q_tiles * c;
+    if (c > 1 && items > 8 * slots) break;
+    const int64_t tiles = (f.key_tiles + c - 1) / c, rounds = (items + slots - 1) / slots;
+    const double us = rounds * (((tiles + kFewWaves - 1) / kFewWaves) * step + start) +
+                      (c > 1 ? merge + 2.0 * items * kFewRows * d.head_dim * 4 / 4.0e6 : 0.0);
+    if (c == 1 || us < f.us) {
+      f.us = us;
+      f.chunks = c;
+    }
+  }
   f.rows = f.chunks > 1 ? bh * f.q_tiles * f.chunks * kFewRows : 0;
   return f;
 }
@@ -683,7 +706,7 @@ ra_status joint_attn_mx_few(const ra_attn_desc& d, const ra_attn_args& a, const 
     if ((s = check_tensor(name[i], *t[i], d.dtype, d.n_tgt, d.head_dim)) != RA_OK) return s;
     if ((i == 1 || i == 2) && (s = check_kv_stride(name[i], *t[i])) != RA_OK) return s;
   }
-  const FewPlan f = few_plan(d);
+  const FewPlan f = few_plan(d, c.format);
   MxFewParams p{};
   if (const size_t need = f.bytes(d.head_dim); need > 0) {
     if (a.workspace == nullptr || a.workspace_bytes < need)
@@ -753,7 +776,7 @@ ra_status refadapt_mx_read(const ra_mx_desc* desc, const ra_mx_args* args, void*
 
 size_t refadapt_joint_attn_mx_workspace_size(const ra_attn_desc* desc, int32_t format, int32_t with_q) {
   if (check_mx_attn("joint_attn_mx_workspace_size", desc, format) != RA_OK) return 0;
-  if (few_rows(*desc)) return few_plan(*desc).bytes(desc->head_dim);
+  if (few_rows(*desc, format)) return few_plan(*desc, format).bytes(desc->head_dim);
   return mx_attn_space(*desc, with_q != 0).total();
 }
 
@@ -777,7 +800,7 @@ ra_status refadapt_joint_attn_mx(const ra_attn_desc* desc, const ra_attn_args* a
     if ((s = check_mx(mx_name[i], *mx[i], c.format, d.n_ref, d.head_dim)) != RA_OK ||
         (s = check_mx_stride(mx_name[i], *mx[i])) != RA_OK)
       return s;
-  if (few_rows(d)) return joint_attn_mx_few(d, a, c, stream);
+  if (few_rows(d, c.format)) return joint_attn_mx_few(d, a, c, stream);
   const MxAttnSpace space = mx_attn_space(d, with_q);
   if (a.workspace == nullptr || a.workspace_bytes < space.total())
     return fail(RA_EWORKSPACE, "joint_attn_mx: workspace needs %zu bytes (got %zu)", space.total(),

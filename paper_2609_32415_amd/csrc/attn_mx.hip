@@ -24,6 +24,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "internal.h"
@@ -562,6 +563,25 @@ hipError_t launch(const MxFewParams& p, int format, hipStream_t stream) {
 }
 
 }  // namespace
+
+int attn_mx_few_slots(int head_dim, int format) {
+  static std::atomic<int> cache[64][2][2];
+  int dev = 0, cus = 0, per_cu = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0) return 0;
+  std::atomic<int>* const known = dev < 64 ? &cache[dev][head_dim == 128][format == MX_FP4] : nullptr;
+  if (known && known->load(std::memory_order_relaxed) > 0) return known->load(std::memory_order_relaxed);
+  if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return 0;
+  const auto occupancy = [&](auto* kernel) {
+    return hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, kernel, 64 * NW, 0);
+  };
+  const hipError_t e = head_dim == 128 ? (format == MX_FP4 ? occupancy(attn_mx_few_kernel<128, true>)
+                                                           : occupancy(attn_mx_few_kernel<128, false>))
+                                       : (format == MX_FP4 ? occupancy(attn_mx_few_kernel<64, true>)
+                                                           : occupancy(attn_mx_few_kernel<64, false>));
+  if (e != hipSuccess || per_cu < 1) return 0;
+  if (known) known->store(cus * per_cu, std::memory_order_relaxed);
+  return cus * per_cu;
+}
 
 hipError_t launch_attn_mx_few(const MxFewParams& p, int format, int head_dim, hipStream_t stream) {
   return head_dim == 128 ? launch<128>(p, format, stream) : launch<64>(p, format, stream);

@@ -156,6 +156,8 @@ struct MxFewParams {
   float4* part_st;  // (m, l_Y, m_R, l_R)
   float* part_lo;   // and the sums of the rounded probabilities
 };
+// Workgroups that the current device holds at once; 0 if it cannot be queried.
+int attn_mx_few_slots(int head_dim, int format);
 hipError_t launch_attn_mx_few(const MxFewParams& p, int format, int head_dim, hipStream_t stream);
 
 // Rotary positions of up to two [B, H, S, d] tensors. The tables travel in the kernel arguments.

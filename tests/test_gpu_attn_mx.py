@@ -58,6 +58,7 @@ SIZES = [
     (1, 1, 1, 1, 64), (1, 2, 31, 1, 128), (2, 1, 33, 2, 64), (1, 3, 64, 17, 128), (1, 2, 65, 32, 128),
     (1, 2, 300, 33, 64), (2, 2, 129, 64, 128), (1, 4, 1000, 61, 128), (1, 2, 511, 65, 64), (1, 3, 257, 130, 128),
     (1, 2, 700, 257, 128), (1, 1, 4352, 5, 128), (1, 2, 5000, 40, 64), (3, 5, 96, 48, 64),
+    (1, 2, 130, 1024, 64), (1, 1, 90, 1025, 128), (2, 30, 40, 300, 64), (3, 100, 33, 3, 64),
 ]
 
 
