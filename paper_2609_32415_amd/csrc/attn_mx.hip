@@ -78,25 +78,26 @@ struct KTile {
   u32x4 w[NI][NL];
   uint32_t e;  // the row's scale bytes
 };
-// Of V: pieces of 16 elements, keys 16 s2 + (lane / 2) % 16, elements 32 (2 d2 + g) + 16 (lane % 2) .. + 15.
+// Of V: pieces of 16 elements, the pieces of a row on neighbouring lanes (the address unit takes a line of memory a
+// clock: with a row's pieces spread over the lanes it bound the loop).
 template <int D, int KIND>
 struct VTile {
-  static constexpr int NV = D / 32;
+  static constexpr int PR = D / 16;      // pieces of a row
+  static constexpr int NV = KT / (64 / PR);  // pieces of a lane: rows i * 64 / PR + lane / PR
   static constexpr int NL = KIND == 0 ? 2 : KIND == 1 ? 4 : 8;  // words of a piece
   uint32_t w[NV][NL];
-  uint32_t e[2];  // the scale bytes of its two rows
+  uint32_t e[NV];  // the scale bytes of their rows
 };
 template <int D, int KIND>
 constexpr int kRowBytes = KIND == 0 ? D / 2 : KIND == 1 ? D : 2 * D;
 
 // One K or V stream: the rows of a (batch, head), read tile by tile through a buffer resource, so that a lane's
 // offsets within a tile never change and rows past the last read as zeros (their scores are masked, and
-// zeros under scale byte 0 are zeros).
+// zeros under scale byte 0 are zeros). A tile with no valid rows reads nothing.
 struct Stream {
   const uint8_t* codes;
   const uint8_t* scales;
   int32_t ss, es;  // row strides, bytes (the host holds a tile's rows to 32-bit offsets)
-  int32_t n_keys;
 };
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const uint8_t* base, int32_t stride, int row0, int valid,
@@ -104,7 +105,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const uint8_t* base,
   const uint64_t a = reinterpret_cast<uint64_t>(base) + (uint64_t)((int64_t)row0 * stride);
   const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a);
   const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
-  const int nbytes = __builtin_amdgcn_readfirstlane((valid - 1) * stride + row_bytes);
+  const int nbytes = __builtin_amdgcn_readfirstlane(valid > 0 ? (valid - 1) * stride + row_bytes : 0);
   return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(((uint64_t)hi << 32) | lo), (short)0, nbytes,
                                            0x00020000);
 }
@@ -121,8 +122,8 @@ __device__ __forceinline__ float block_scale(uint32_t e, int i, int g) {
 }
 
 template <int D, int KIND>
-__device__ __forceinline__ void load_k(KTile<D, KIND>& t, const Stream& k, int key0, int lane) {
-  const int valid = min(KT, k.n_keys - key0), g = lane >> 5, row = sigma(lane & 31);
+__device__ __forceinline__ void load_k(KTile<D, KIND>& t, const Stream& k, int key0, int valid, int lane) {
+  const int g = lane >> 5, row = sigma(lane & 31);
   const auto r = rows_rsrc(k.codes, k.ss, key0, valid, kRowBytes<D, KIND>);
   const uint32_t off = row * k.ss + g * kRowBytes<32, KIND>;
 #pragma unroll
@@ -137,22 +138,20 @@ __device__ __forceinline__ void load_k(KTile<D, KIND>& t, const Stream& k, int k
 }
 
 template <int D, int KIND>
-__device__ __forceinline__ void load_v(VTile<D, KIND>& t, const Stream& v, int key0, int lane) {
-  const int valid = min(KT, v.n_keys - key0), g = lane >> 5, row = (lane >> 1) & 15;
-  constexpr int piece = kRowBytes<16, KIND>;
+__device__ __forceinline__ void load_v(VTile<D, KIND>& t, const Stream& v, int key0, int valid, int lane) {
+  constexpr int PR = VTile<D, KIND>::PR, step = 64 / PR, piece = kRowBytes<16, KIND>;
   const auto r = rows_rsrc(v.codes, v.ss, key0, valid, kRowBytes<D, KIND>);
-  const uint32_t off = row * v.ss + (2 * g + (lane & 1)) * piece;
+  const uint32_t off = lane / PR * v.ss + lane % PR * piece;
 #pragma unroll
   for (int i = 0; i < t.NV; ++i) {
-    const int s2 = i / (D / 64), d2 = i % (D / 64);
     if constexpr (KIND == 0) {
-      const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(r, off + 4 * piece * d2, 16 * s2 * v.ss, 0);
+      const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(r, off, i * step * v.ss, 0);
       t.w[i][0] = w[0];
       t.w[i][1] = w[1];
     } else {
 #pragma unroll
       for (int j = 0; j < t.NL / 4; ++j) {
-        const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(r, off + 4 * piece * d2 + 16 * j, 16 * s2 * v.ss, 0);
+        const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(r, off + 16 * j, i * step * v.ss, 0);
 #pragma unroll
         for (int e = 0; e < 4; ++e) t.w[i][4 * j + e] = w[e];
       }
@@ -160,8 +159,9 @@ __device__ __forceinline__ void load_v(VTile<D, KIND>& t, const Stream& v, int k
   }
   if constexpr (KIND != 2) {
     const auto re = rows_rsrc(v.scales, v.es, key0, valid, D / 32);
-    t.e[0] = load_scales<D>(re, row * v.es, 0);
-    t.e[1] = load_scales<D>(re, row * v.es, 16 * v.es);
+#pragma unroll
+    for (int i = 0; i < t.NV; ++i)
+      t.e[i] = __builtin_amdgcn_raw_buffer_load_b8(re, lane / PR * v.es + lane % PR / 2, i * step * v.es, 0);
   }
 }
 
@@ -176,14 +176,19 @@ __device__ __forceinline__ bf16x8 k_operand(const KTile<D, KIND>& t, int i, int 
   return __builtin_bit_cast(bf16x8, w);
 }
 
-// Puts half j of V piece i into LDS: blocks of 16 keys x 32 elements (1 KiB; 64 bytes a key, its halves swapped where
-// bit 1 of the key is set, which keeps the transpose reads free of bank conflicts).
+// Puts half j of V piece i into LDS: blocks of 16 keys x 32 elements (64 bytes a key, its halves swapped where bit 1 of
+// the key is set, which keeps the transpose reads free of bank conflicts), 64 bytes apart, which keeps the writes of a
+// row free of them.
+constexpr int VBLOCK = 512 + 32;  // elements from one block to the next
 template <int D, int KIND>
 __device__ __forceinline__ void store_v(uint16_t* lds, const VTile<D, KIND>& t, int i, int j, int lane) {
-  const int r = (lane >> 1) & 15, s2 = i / (D / 64), d2 = i % (D / 64);
-  uint16_t* const p = lds + 512 * ((D / 32) * s2 + 2 * d2 + (lane >> 5)) + 32 * r + 16 * ((lane & 1) ^ ((r >> 1) & 1));
+  constexpr int PR = VTile<D, KIND>::PR, step = 64 / PR;  // 8 or 16 rows: row + i * step keeps the lane's bit 1 and, of 16 rows, its place
+  const int row = lane / PR, col = lane % PR;
+  const int key = i * step;
+  uint16_t* const p = lds + VBLOCK * ((D / 32) * (key / 16) + col / 2) + 32 * (row + key % 16) +
+                      16 * ((col & 1) ^ ((row >> 1) & 1));
   u32x4 w;
-  const float e = KIND == 2 ? 0.f : block_scale(t.e[s2], d2, lane >> 5);
+  const float e = KIND == 2 ? 0.f : scale_bits(t.e[i]);
   if constexpr (KIND == 0) w = decode_oct<true>(u32x2{t.w[i][j], 0u}, e);
   if constexpr (KIND == 1) w = decode_oct<false>(u32x2{t.w[i][2 * j], t.w[i][2 * j + 1]}, e);
   if constexpr (KIND == 2) w = u32x4{t.w[i][4 * j], t.w[i][4 * j + 1], t.w[i][4 * j + 2], t.w[i][4 * j + 3]};
@@ -222,7 +227,7 @@ constexpr int ORow(int d) { return d + 4; }  // floats of a row of O in LDS: the
 template <int D>
 struct FewLds {
   union {
-    uint16_t v[NW][KT * D];
+    uint16_t v[NW][KT * D / 512 * VBLOCK];
     float o[NW][BM][ORow(D)];
   };
   float m[NW][BM], l[NW][BM], m_ref[NW][BM], l_ref[NW][BM], lo[NW][BM];
@@ -230,7 +235,7 @@ struct FewLds {
 };
 
 template <int D, bool FP4>
-__global__ __launch_bounds__(64 * NW, 2) void attn_mx_few_kernel(MxFewParams p) {
+__global__ __launch_bounds__(64 * NW, D == 64 && FP4 ? 4 : 2) void attn_mx_few_kernel(MxFewParams p) {
   constexpr int DB = D / 32, NI = D / 64;
   constexpr int KIND = FP4 ? 0 : 1;
   __shared__ __attribute__((aligned(1024))) FewLds<D> s;
@@ -246,10 +251,10 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_mx_few_kernel(MxFewParams p) 
   const int j0 = chunk * p.tiles_each + min(chunk, p.tiles_more), j1 = j0 + p.tiles_each + (chunk < p.tiles_more ? 1 : 0);
 
   const auto cached = [&](const MxView& v) {
-    return Stream{v.codes + b * v.sb + h * v.sh, v.scales + b * v.eb + h * v.eh, (int32_t)v.ss, (int32_t)v.es, p.n_ref};
+    return Stream{v.codes + b * v.sb + h * v.sh, v.scales + b * v.eb + h * v.eh, (int32_t)v.ss, (int32_t)v.es};
   };
   const auto plain = [&](const View& v) {
-    return Stream{static_cast<const uint8_t*>(v.p) + 2 * (b * v.sb + h * v.sh), nullptr, 2 * (int32_t)v.ss, 0, p.n_tgt};
+    return Stream{static_cast<const uint8_t*>(v.p) + 2 * (b * v.sb + h * v.sh), nullptr, 2 * (int32_t)v.ss, 0};
   };
   const Stream kc = cached(p.k), vc = cached(p.v), ky = plain(p.k_tgt), vy = plain(p.v_tgt);
 
@@ -276,7 +281,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_mx_few_kernel(MxFewParams p) 
       32 * (8 * (tr_G >> 1) + (tr_i >> 2)) + ((16 * (tr_G & 1) + 4 * (tr_i & 3)) ^ (16 * ((tr_i >> 3) & 1)));
 
   const auto v_operand = [&](int i) __attribute__((always_inline)) {  // i = DB * s2 + db
-    const uint16_t* a = lds + v_lane + 512 * i;
+    const uint16_t* a = lds + v_lane + VBLOCK * i;
     const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(a));
     const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(a + 128));
     return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -289,9 +294,12 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_mx_few_kernel(MxFewParams p) 
   const auto score = [&](const auto& k, const auto& v) __attribute__((always_inline)) {
     f32x16 sc{};
     lds_order();
+    bf16x8 a[2];
+    a[0] = k_operand(k, 0, 0, g);
 #pragma unroll
     for (int i = 0; i < 4 * NI; ++i) {
-      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(k, i / 4, i % 4, g), q[i / 4][i % 4], sc, 0, 0, 0);
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i & 1], q[i / 4][i % 4], sc, 0, 0, 0);
+      if (i + 1 < 4 * NI) a[(i + 1) & 1] = k_operand(k, (i + 1) / 4, (i + 1) % 4, g);
       store_v(lds, v, i / 2, i % 2, lane);
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -393,11 +401,14 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_mx_few_kernel(MxFewParams p) 
   if (j < jr) {
     KTile<D, KIND> k0{}, k1{};
     VTile<D, KIND> v0{}, v1{};
+    // Always issued, past the last tile for no rows: behind a branch the compiler does not know how many loads are in
+    // flight and waits for all of them.
+    const auto rows = [&](int jj) __attribute__((always_inline)) { return jj < jr ? min(KT, p.n_ref - jj * KT) : 0; };
     const auto load = [&](KTile<D, KIND>& k, VTile<D, KIND>& v, int jj) __attribute__((always_inline)) {
-      if (jj < jr) load_k(k, kc, jj * KT, lane);
-      if (jj - NW < jr) load_v(v, vc, (jj - NW) * KT, lane);
+      load_k(k, kc, jj * KT, rows(jj), lane);
+      load_v(v, vc, (jj - NW) * KT, rows(jj - NW), lane);
     };
-    load_k(k0, kc, j * KT, lane);
+    load_k(k0, kc, j * KT, rows(j), lane);
     load(k1, v0, j + NW);
     f32x16 s0{}, s1{};
 #pragma unroll
@@ -433,10 +444,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_mx_few_kernel(MxFewParams p) 
   for (; j < j1; j += NW) {
     KTile<D, 2> k;
     VTile<D, 2> v;
-    load_k(k, ky, (j - n_rt) * KT, lane);
-    load_v(v, vy, (j - n_rt) * KT, lane);
+    const int key0 = (j - n_rt) * KT, valid = min(KT, p.n_tgt - key0);
+    load_k(k, ky, key0, valid, lane);
+    load_v(v, vy, key0, valid, lane);
     f32x16 sc = score(k, v);
-    attend(first, sc, p.n_tgt - (j - n_rt) * KT, p1, p0);
+    attend(first, sc, valid, p1, p0);
     last_pv(p0);
   }
 
