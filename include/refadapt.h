@@ -380,7 +380,7 @@ typedef struct {
  * q [B, H, rows, d] -> q_out and, with non-NULL data, k -> k_out, in one launch
  * that forms each angle once. An output may be its own input (same data and
  * strides); otherwise outputs overlap nothing. `pos` [B, rows, n_axes] is on the
- * device. phi is reduced in fp64 (off by at most 2^-52 |phi| + 2^-24 radians),
+ * device. phi is reduced in fp64 (off by at most 2^-51 |phi| + 2^-22 radians),
  * the rest is fp32, rounded once to dtype. Infinite or NaN positions give NaN.
  * Errors: RA_EINVAL (null pointers, sizes, unknown enums, freq not finite, axis
  * out of range, one of k and k_out NULL); RA_EUNSUPPORTED (head_dim not in whole
@@ -427,7 +427,7 @@ typedef struct {
  * refadapt_mx_commit - refadapt_cache_commit into a quantised cache.
  *
  * As refadapt_cache_commit (decision, age, step and the optional V and Q pairs),
- * but quantises the rows. Of a block of 32 elements with largest magnitude m the
+ * but quantises the rows; the tensors written overlap nothing. Of a block of 32 elements with largest magnitude m the
  * scale is 2^e, e = floor(log2 m) - emax (emax 2 for RA_MXFP4, 8 for RA_MXFP8),
  * plus 1 where m's significand exceeds 1.75 (1.8125), held to -127 (-124) ..
  * 127 - emax; an element's code is the nearest to x * 2^-e, ties to the even
@@ -462,6 +462,10 @@ typedef struct {
  * args->workspace must hold refadapt_joint_attn_mx_workspace_size(desc, format,
  * with_q) bytes, 16-byte aligned (with_q: cache->q is given); it needs no
  * initialisation and must not be used by another call that runs concurrently.
+ * Calls of few target rows (RA_BF16, RA_KV_CACHE, RA_Q_TARGET) attend straight over
+ * the codes; the others read the cache back into the workspace, and only those
+ * count on args->clock_probe. Both are deterministic, and equal to within the
+ * roundings of refadapt_joint_attn.
  * Errors: as refadapt_joint_attn; RA_EUNSUPPORTED for other K/V sources,
  * seg_mass, row strides of codes or scales above 2^24 - 8 bytes, and as
  * refadapt_mx_commit for the cache; RA_EWORKSPACE for a missing

@@ -13,9 +13,14 @@
 // lowest (-127; -124) and 127 - emax keep every value a finite bf16: reading back is exact.
 // A block that holds a NaN or an infinity gets the scale byte 255 and reads back as NaN throughout.
 //
-// Both kernels are bound by memory: 2 bytes an element in bf16 against 0.53 (1.03) of codes and scales.
+// Both kernels are bound by memory: 2 bytes an element in bf16 and 0.53 (1.03) of codes and scales. A thread keeps four
+// runs of 8 elements in flight. Measured: 24 heads x 4352 x 128 of K and V to 4 bits 13.9 us (4.9 TB/s) and back 12.4 us;
+// K, V and Q of 12544 rows to 8 bits 68 to 80 us (5.2 to 4.4 TB/s; the rows of a head 6 KiB apart) and back 53 us
+// (6.6 TB/s, part of it into the last-level cache). A large copy moves 5.2 TB/s.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <algorithm>
 
 #include "internal.h"
 #include "mxcodes.h"
@@ -116,9 +121,10 @@ uint32_t mx_octs(MxSet& ms, int32_t n_rows, int32_t head_dim) {
   ms.oct_shift = (ms.octs & (ms.octs - 1)) == 0 ? __builtin_ctz(ms.octs) : -1;
   return (uint32_t)n_rows * (uint32_t)ms.octs;
 }
+// A workgroup's octs, or several times as many where the launch would hold 2^32 threads.
 dim3 mx_grid(int32_t bh, uint32_t n_octs, int n) {
-  const uint32_t gy = (n_octs + MX_WG - 1) / MX_WG;
-  return dim3(bh, gy > 4096 ? 4096 : gy, n);
+  const int64_t gy = ((int64_t)n_octs + MX_WG - 1) / MX_WG, most = 0xffffffffLL / ((int64_t)MX_THREADS * bh * n);
+  return dim3(bh, (unsigned)std::min<int64_t>(std::min<int64_t>(gy, 4096), most), n);
 }
 
 }  // namespace

@@ -129,6 +129,12 @@ def test_nan_block_reaches_the_rows_that_see_it_and_no_reference(n_tgt):
     torch.cuda.synchronize()
     assert torch.isfinite(r.o_tgt[0, 0]).all() and torch.isfinite(r.o_tgt[0, 1, :, :32]).all()
     assert torch.isnan(r.o_tgt[0, 1, :, 32:]).all() and torch.isfinite(r.ref_mass).all()
+    # a NaN block of K: every row of its head, no other
+    c["k"].scales[0, 0, 3, 0] = 255
+    r = ops.joint_attn_mx(x["q_tgt"], x["k_tgt"], x["v_tgt"], k_mx=c["k"], v_mx=c["v"])
+    torch.cuda.synchronize()
+    assert torch.isnan(r.o_tgt[0, 0]).all() and torch.isnan(r.ref_mass[0, 0]).all()
+    assert torch.isfinite(r.o_tgt[0, 1, :, :32]).all() and torch.isfinite(r.ref_mass[0, 1]).all()
     # an empty cache: plain self-attention
     empty = ops.mx_tensor((1, 2, 0, 64), "mxfp4", "cuda:0")
     r = ops.joint_attn_mx(x["q_tgt"], x["k_tgt"], x["v_tgt"], k_mx=empty, v_mx=empty, lse=True)
@@ -190,6 +196,35 @@ def test_graph_replays_and_two_streams(n_tgt):
                 x[n].copy_(v)
             for dst, v in zip((c["k"].codes, c["k"].scales, c["v"].codes, c["v"].scales), put[1:]):
                 dst.copy_(v)
+
+
+@pytest.mark.parametrize("n_tgt", [5, 300])
+def test_infinite_target_keys_and_queries(n_tgt):
+    """A target key whose scores are all -inf drops out; an infinite query element makes its row NaN and no other."""
+    x, c, vals = _inputs(31, 1, 1, 100, n_tgt, 64, "bf16", "mxfp8")
+    x["q_tgt"][0, 0, :, 0] = 1.0
+    x["k_tgt"][0, 0, 2, 0] = float("-inf")
+    r = ops.joint_attn_mx(x["q_tgt"], x["k_tgt"], x["v_tgt"], k_mx=c["k"], v_mx=c["v"])
+    torch.cuda.synchronize()
+    keep = [i for i in range(n_tgt) if i != 2]
+    y = dict(x, k_tgt=x["k_tgt"][:, :, keep], v_tgt=x["v_tgt"][:, :, keep])
+    _check_rows(r.o_tgt, r.ref_mass, None, host(x["q_tgt"]), vals["k"], vals["v"], y, "bf16")
+    x["k_tgt"][0, 0, 2, 0] = 0.0
+    x["q_tgt"][0, 0, 1, 3] = float("inf")
+    r = ops.joint_attn_mx(x["q_tgt"], x["k_tgt"], x["v_tgt"], k_mx=c["k"], v_mx=c["v"])
+    torch.cuda.synchronize()
+    bad = torch.isnan(r.o_tgt[0, 0]).any(-1)
+    assert bad.nonzero().flatten().tolist() == [1] and torch.isnan(r.o_tgt[0, 0, 1]).all()
+
+
+def test_clock_probe_counts_where_the_cache_is_read_back():
+    x, c, _ = _inputs(37, 1, 2, 64, 300, 64, "bf16", "mxfp4")
+    probe = torch.zeros(2, dtype=torch.int64, device="cuda:0")
+    word = torch.tensor([ops.REUSE], dtype=torch.int32, device="cuda:0")
+    ops.joint_attn_mx(x["q_tgt"], x["k_tgt"], x["v_tgt"], k_mx=c["k"], v_mx=c["v"], q_mx=c["q"], q_ref=x["q_ref"],
+                      k_ref=x["k_ref"], v_ref=x["v_ref"], kvsrc="device", decision=word, clock_probe=probe)
+    torch.cuda.synchronize()
+    assert (probe > 0).all()
 
 
 def test_wrong_arguments_are_refused():
