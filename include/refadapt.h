@@ -398,8 +398,10 @@ typedef enum { RA_MXFP4 = 0, RA_MXFP8 = 1 } ra_mx_format;
 /* A quantised [B, H, S, d] tensor: d / 2 (RA_MXFP4) or d (RA_MXFP8) bytes of
  * codes and d / 32 scale bytes a row, each row contiguous, with BYTE strides.
  * Codes: 16-byte aligned, strides in multiples of 16; scales: base and strides in
- * multiples of the largest power of two, at most 4, that divides d / 32. Elements 32 j .. 32 j + 31 of a row share scale byte j:
- * value = code * 2^(byte - 127); byte 255 makes them all NaN. */
+ * multiples of the largest power of two, at most 4, that divides d / 32. Elements
+ * 32 j .. 32 j + 31 of a row share scale byte j: value = code * 2^(byte - 127); byte
+ * 255 makes them all NaN. Every value under a byte that the commit writes is a bf16;
+ * other bytes (above 252 / 246 and, with e4m3, below 3) are not read exactly. */
 typedef struct {
   void* codes;
   int64_t stride_b, stride_h, stride_s;
@@ -427,15 +429,14 @@ typedef struct {
  * refadapt_mx_commit - refadapt_cache_commit into a quantised cache.
  *
  * As refadapt_cache_commit (decision, age, step and the optional V and Q pairs),
- * but quantises the rows; the tensors written overlap nothing. Of a block of 32 elements with largest magnitude m the
- * scale is 2^e, e = floor(log2 m) - emax (emax 2 for RA_MXFP4, 8 for RA_MXFP8),
+ * but quantises the rows; the tensors written overlap nothing. Of a block of 32
+ * elements with largest magnitude m the scale is 2^e, e = floor(log2 m) - emax (emax 2 for RA_MXFP4, 8 for RA_MXFP8),
  * plus 1 where m's significand exceeds 1.75 (1.8125), held to -127 (-124) ..
  * 127 - emax; an element's code is the nearest to x * 2^-e, ties to the even
  * code, saturating. A block of zeros has the lowest scale, a block that holds a
  * NaN or an infinity byte 255 and codes 0. Every value is a finite bf16.
  * Errors: RA_EINVAL (null desc or args, null K tensors, a pair with one NULL side,
- * sizes, enums),
- * RA_EUNSUPPORTED (head_dim not a multiple of 32, alignment, batch * heads >
+ * sizes, enums), RA_EUNSUPPORTED (head_dim not a multiple of 32, alignment, batch * heads >
  * 65535, n_ref * head_dim > 2^34).
  */
 ra_status refadapt_mx_commit(const ra_mx_desc* desc, const ra_mx_args* args, void* stream);
