@@ -566,7 +566,55 @@ def rope(q, k=None, *, pos, freq, axis, pairing="interleaved", inverse=False, q_
     radians. ``pairing``: elements (2i, 2i + 1), or "half": (i, i + pairs); elements past the pairs are
     copied. ``inverse`` turns back, which is also the gradient: with it the gradient of an output gives that
     of the input. ``q_out=q`` works in place. Returns q_out, or (q_out, k_out) with ``k``.
+
+    Where gradients are recorded and ``q`` or ``k`` requires them, the results carry them; ``q_out`` and
+    ``k_out`` are refused then. ``pos`` and ``freq`` have none.
     """
+    if (q.requires_grad or pos.requires_grad or freq.requires_grad or
+            any(t is not None and t.requires_grad for t in (k, q_out, k_out))) and torch.is_grad_enabled():
+        if pos.requires_grad or freq.requires_grad:
+            raise ValueError("rope has no gradients of pos and freq")
+        if q_out is not None or k_out is not None:
+            raise ValueError("q_out and k_out cannot be given where a tensor requires grad")
+        return _Rope.apply(q, k, pos, freq, axis, pairing, inverse)
+    return _rope(q, k, pos, freq, axis, pairing, inverse, q_out, k_out)
+
+
+class _Rope(torch.autograd.Function):
+    """``rope`` with its gradient, the turn back (which has a gradient in its turn)."""
+
+    @staticmethod
+    def forward(ctx, q, k, pos, freq, axis, pairing, inverse):
+        ctx.save_for_backward(pos, freq, axis)
+        ctx.pairing, ctx.inverse = pairing, inverse
+        ctx.set_materialize_grads(False)
+        out = _rope(q, k, pos, freq, axis, pairing, inverse)
+        if k is not None:
+            ctx.mark_non_differentiable(*(o for o, needs in zip(out, ctx.needs_input_grad) if not needs))
+        return out
+
+    @staticmethod
+    def backward(ctx, *grads):
+        pos, freq, axis = ctx.saved_tensors
+        back = [_readable(g) if g is not None and ctx.needs_input_grad[i] else None for i, g in enumerate(grads)]
+        given = [g for g in back if g is not None]
+        if given:
+            turned = rope(*given, pos=pos, freq=freq, axis=axis, pairing=ctx.pairing, inverse=not ctx.inverse)
+            turned = iter(turned if len(given) == 2 else (turned,))
+            back = [g if g is None else next(turned) for g in back]
+        return (*back, *(None,) * (7 - len(back)))
+
+
+def _readable(t):
+    """``t``, or a copy of it where the library does not take its layout (a gradient comes in any)."""
+    unit = 16 // t.element_size()
+    sb, sh, ss, sd = t.stride()
+    if sd == 1 and ss >= t.shape[3] and not (sb | sh | ss) % unit and t.data_ptr() % 16 == 0:
+        return t
+    return t.clone(memory_format=torch.contiguous_format)
+
+
+def _rope(q, k, pos, freq, axis, pairing, inverse, q_out=None, k_out=None):
     shape, dt, dev = q.shape, q.dtype, torch._C._cuda_getDevice()
     B, H, S, D = shape
     if dt not in _DTYPES:
