@@ -57,11 +57,14 @@ class Rope:
     pos_tgt: torch.Tensor
     pairing: str = "interleaved"
 
-    def turned(self, x):
-        """The block inputs ``x`` with their Q and K turned (new tensors)."""
-        kw = dict(freq=self.freq, axis=self.axis, pairing=self.pairing)
-        q_tgt, k_tgt = ops.rope(x["q_tgt"], x["k_tgt"], pos=self.pos_tgt, **kw)
-        q_ref, k_ref = ops.rope(x["q_ref"], x["k_ref"], pos=self.pos_ref, **kw)
+    def turned(self, x, into=None):
+        """The block inputs ``x`` with their Q and K turned: written to the tensors of ``into`` (by the same names),
+        or new ones where it has none."""
+        kw, into = dict(freq=self.freq, axis=self.axis, pairing=self.pairing), into or {}
+        q_tgt, k_tgt = ops.rope(x["q_tgt"], x["k_tgt"], pos=self.pos_tgt, q_out=into.get("q_tgt"),
+                                k_out=into.get("k_tgt"), **kw)
+        q_ref, k_ref = ops.rope(x["q_ref"], x["k_ref"], pos=self.pos_ref, q_out=into.get("q_ref"),
+                                k_out=into.get("k_ref"), **kw)
         return {**x, "q_tgt": q_tgt, "k_tgt": k_tgt, "q_ref": q_ref, "k_ref": k_ref}
 
 
@@ -114,6 +117,13 @@ class Controller:
         self.attn_ws = (ops.attn_workspace(q_like, n_ref, kvsrc="device") if cache_format is None else
                         ops.attn_mx_workspace(q_like, n_ref, cache_format, kvsrc="device", q_cached=True))
         self.sidecar = sidecar
+        if rope is not None:
+            # Where a block's turned Q and K go. Its target Q has to last until the block's next step has compared
+            # with it: two buffers a block, by the parity that its mass has. The others are done with at the end of
+            # the block and serve every block. (Allocated by the block they would be kept by each captured step.)
+            self._turned_q = [[torch.empty_like(q_like) for _ in range(2)] for _ in range(n_blocks)]
+            self._turned = {"k_tgt": torch.empty_like(q_like),
+                            **{n: torch.empty(self.shape_r, dtype=dtype, device=device) for n in ("q_ref", "k_ref")}}
 
     def block(self, t, b, x, mark=None, clock_probe=None):
         """Enqueue Alg. 1's work for block ``b`` at step ``t`` on fresh inputs ``x``.
@@ -122,7 +132,11 @@ class Controller:
         controller has it, "gate", "attn", "commit"), e.g. to record timing events;
         ``clock_probe`` is passed to the attention launch (see ``ops.joint_attn``)."""
         if self.rope is not None:
-            x = self.rope.turned(x)
+            into = {**self._turned, "q_tgt": self._turned_q[b][self.parity[b]]}
+            if self.sidecar is not None:  # it compares with the K of the block's last step: new tensors
+                del into["k_tgt"], into["k_ref"]
+            with torch.no_grad():  # the path records none, whatever its inputs come from
+                x = self.rope.turned(x, into)
             if mark:
                 mark("rope")
         if self.cue == "anchor":
