@@ -379,13 +379,16 @@ typedef struct {
  * gradient of its output, it gives the gradient of its input.
  * q [B, H, rows, d] -> q_out and, with non-NULL data, k -> k_out, in one launch
  * that forms each angle once. An output may be its own input (same data and
- * strides); otherwise outputs overlap nothing. `pos` [B, rows, n_axes] is on the
- * device. phi is reduced in fp64 (off by at most 2^-51 |phi| + 2^-22 radians),
- * the rest is fp32, rounded once to dtype. Infinite or NaN positions give NaN.
+ * strides, none of them a broadcast's zero); otherwise outputs overlap nothing.
+ * `pos` [B, rows, n_axes] is on the device. phi is reduced in fp64 (off by at
+ * most 2^-51 |phi| + 2^-22 radians), the rest is fp32, rounded once to dtype.
+ * Infinite or NaN positions give NaN.
  * Errors: RA_EINVAL (null pointers, sizes, unknown enums, freq not finite, axis
- * out of range, one of k and k_out NULL); RA_EUNSUPPORTED (head_dim not in whole
- * 16-byte units, RA_ROPE_HALF with n_pairs not in whole 16-byte units, n_pairs
- * above RA_ROPE_MAX_PAIRS, alignment, 2^31 or more 16-byte pieces of q).
+ * out of range, one of k and k_out NULL, a broadcast input turned in place, an
+ * output at the other one's or at the other input's address); RA_EUNSUPPORTED
+ * (head_dim not in whole 16-byte units, RA_ROPE_HALF with n_pairs not in whole
+ * 16-byte units, n_pairs above RA_ROPE_MAX_PAIRS, alignment, 2^31 or more
+ * 16-byte pieces of q).
  */
 ra_status refadapt_rope(const ra_rope_desc* desc, const ra_rope_args* args, void* stream);
 

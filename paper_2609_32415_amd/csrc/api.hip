@@ -540,10 +540,15 @@ ra_status refadapt_rope(const ra_rope_desc* desc, const ra_rope_args* args, void
     if (i > 0 && in[i]->data == nullptr && out[i]->data == nullptr) continue;
     if ((s = check_tensor(name[i], *in[i], d.dtype, d.rows, d.head_dim)) != RA_OK) return s;
     if ((s = check_tensor(out_name[i], *out[i], d.dtype, d.rows, d.head_dim)) != RA_OK) return s;
+    if (out[i]->data == in[i]->data &&
+        ((d.batch > 1 && in[i]->stride_b == 0) || (d.heads > 1 && in[i]->stride_h == 0)))
+      return fail(RA_EINVAL, "rope: %s is broadcast and cannot be turned in place", name[i]);
     p.x[i] = view(*in[i]);
     p.y[i] = view(*out[i]);
     p.n = i + 1;
   }
+  if (p.n == 2 && (a.q_out.data == a.k_out.data || a.q_out.data == a.k.data || a.k_out.data == a.q.data))
+    return fail(RA_EINVAL, "rope: q_out and k_out overlap each other or the other's input");
   p.pos = a.pos;
   p.pos_sb = d.pos_stride_b;
   p.pos_ss = d.pos_stride_s;

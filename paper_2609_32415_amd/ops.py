@@ -565,7 +565,7 @@ def rope(q, k=None, *, pos, freq, axis, pairing="interleaved", inverse=False, q_
     tables of the pairs (``rope_frequencies``, or a model's own): pair i turns by pos[..., axis[i]] * freq[i]
     radians. ``pairing``: elements (2i, 2i + 1), or "half": (i, i + pairs); elements past the pairs are
     copied. ``inverse`` turns back, which is also the gradient: with it the gradient of an output gives that
-    of the input. ``q_out=q`` works in place. Returns q_out, or (q_out, k_out) with ``k``.
+    of the input. ``q_out=q`` works in place, but not on a broadcast ``q``. Returns q_out, or (q_out, k_out) with ``k``.
 
     Where gradients are recorded and ``q`` or ``k`` requires them, the results carry them; ``q_out`` and
     ``k_out`` are refused then. ``pos`` and ``freq`` have none.
