@@ -41,7 +41,7 @@
 // each of its terms, so a sum within 2^12 proves that every probability is at
 // most 2^12 and m may stay. The test runs (wave-wide, NaN and inf failing it)
 // once a tile, before any of its probabilities enters O; when it fails (always at a
-// workgroup's first tile, where m = -inf), a cold path takes the row max of
+// workgroup's first tile with a finite score, where m stands for -inf), a cold path takes the row max of
 // the scores, rescales O and l, and forms the probabilities again. The
 // O rescale and the row max are thus almost never executed.
 // Row sums add the fp32 probabilities, so the reference mass and the
@@ -95,6 +95,9 @@ typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 
 constexpr int BN = kAttnBf16BN;  // keys per LDS tile
 constexpr float PBOUND = 4096.0f;  // bound on a probability against the running max (2^12)
+// Stands for -inf in a running max. Differences with it stay defined, so a tile whose scores are all -inf leaves a
+// row with sums of zero.
+constexpr float LOWEST = -3.0e38f;
 
 // Row permutation of a 32-key MFMA block: swaps bits 2 and 3 of the row index.
 // With key sigma(m) in A-row m of S^T = K Q^T, output register r of lane-half g
@@ -418,12 +421,12 @@ __global__ __launch_bounds__(2 * BM, 2) void attn_bf16_kernel(AttnParams p) {
   for (int i = 0; i < DB; ++i) o[i] = f32x16{};
   // l_run and l_ref hold this lane's half of the query's keys (its partner lane l ^ 32 the
   // other half; both see the same max): the halves are added where a whole sum is read.
-  float m_run = -__builtin_inff(), l_run = 0.f;
+  float m_run = LOWEST, l_run = 0.f;
   // Sum of the bf16-rounded probabilities that enter O (this lane's keys, against m_run): the
   // output is normalised by it, so the weights applied to V sum to one (l_run, the fp32 sum,
   // gives the mass and the log-sum-exp).
   float lo_run = 0.f;
-  float m_ref = -__builtin_inff(), l_ref = 0.f;
+  float m_ref = LOWEST, l_ref = 0.f;
   const float c = p.sc_log2;
   // SEG with seg_mass: the reference segment that holds this range's first key tile (a key
   // chunk may start inside one), the key tile that ends it, this row's seg_mass offset and,
