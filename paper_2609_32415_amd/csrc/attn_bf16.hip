@@ -130,6 +130,11 @@ __device__ __forceinline__ int lane_now() {
   return l;
 }
 
+// A sum of probabilities, taken to another maximum. An empty one has no maximum; one with a NaN stays NaN.
+__device__ __forceinline__ float weighed(float sum, float exponent) {
+  return sum == 0.f ? 0.f : sum * __builtin_amdgcn_exp2f(exponent);
+}
+
 // acc + lo + hi of a packed pair of bf16 values (one v_dot2c_f32_bf16 against (1, 1)).
 __device__ __forceinline__ float add_bf16x2(uint32_t w, float acc) {
   const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
@@ -746,7 +751,7 @@ __global__ __launch_bounds__(2 * BM, 2) void attn_bf16_kernel(AttnParams p) {
   }
 
   // ---- epilogue
-  const float L_R = l_ref_sum > 0.f ? l_ref_sum * __builtin_amdgcn_exp2f(m_ref - m_run) : 0.f;
+  const float L_R = weighed(l_ref_sum, m_ref - m_run);
   const float total = L_R + l_sum;
   const float inv = 1.f / total;
   const float inv_o = 1.f / lo_sum;
@@ -847,7 +852,7 @@ __device__ __forceinline__ void merge_rows(const AttnParams& p, const SplitPlan&
     for (int u = 0; u < MERGE_BATCH; ++u) {
       if (c0 + u < nc) {
         M = fmaxf(M, sv[u].x);
-        if (sv[u].w > 0.f) M_R = fmaxf(M_R, sv[u].z);
+        if (sv[u].w != 0.f) M_R = fmaxf(M_R, sv[u].z);
       }
     }
   };
@@ -873,7 +878,7 @@ __device__ __forceinline__ void merge_rows(const AttnParams& p, const SplitPlan&
         const float wgt = __builtin_amdgcn_exp2f(sv[u].x - M);
         L_Y += sv[u].y * wgt;
         L_o += lv[u] * wgt;
-        if (sv[u].w > 0.f) L_Rr += sv[u].w * __builtin_amdgcn_exp2f(sv[u].z - M_R);
+        if (sv[u].w != 0.f) L_Rr += sv[u].w * __builtin_amdgcn_exp2f(sv[u].z - M_R);
         acc.x += ov4[u].x * wgt;
         acc.y += ov4[u].y * wgt;
         acc.z += ov4[u].z * wgt;
@@ -881,7 +886,7 @@ __device__ __forceinline__ void merge_rows(const AttnParams& p, const SplitPlan&
       }
     }
   }
-  const float L_R = L_Rr > 0.f ? L_Rr * __builtin_amdgcn_exp2f(M_R - M) : 0.f;
+  const float L_R = weighed(L_Rr, M_R - M);
   const float total = L_R + L_Y;
   const float inv = 1.f / total, inv_o = 1.f / L_o;
   const View ov = ref_rows ? p.o_ref : p.o_tgt;
@@ -918,15 +923,14 @@ __device__ __forceinline__ void merge_rows(const AttnParams& p, const SplitPlan&
     const int32_t* const ends = p.seg_tile_end;  // read through a pointer: no scratch copy
     const int s0 = s > 0 ? ends[s - 1] : 0, s1 = ends[s];
     const float* ps = p.part_seg + (int64_t)st * nc * BM * p.n_seg + (int64_t)rr * p.n_seg + s;
-    float Ms = -__builtin_inff();
+    float Ms = LOWEST;
     for (int c = 0; c < nc; ++c)
       if (c * nt / nc < s1 && (c + 1) * nt / nc > s0) Ms = fmaxf(Ms, ps[(int64_t)c * BM * p.n_seg]);
     float Ls = 0.f;
-    if (Ms > -__builtin_inff())
-      for (int c = 0; c < nc; ++c)
-        if (c * nt / nc < s1 && (c + 1) * nt / nc > s0) Ls += __builtin_amdgcn_exp2f(ps[(int64_t)c * BM * p.n_seg] - Ms);
+    for (int c = 0; c < nc; ++c)
+      if (c * nt / nc < s1 && (c + 1) * nt / nc > s0) Ls += __builtin_amdgcn_exp2f(ps[(int64_t)c * BM * p.n_seg] - Ms);
     p.seg_mass[((int64_t)bh * p.n_tgt + qrow) * p.n_seg + s] =
-        Ls > 0.f ? __builtin_amdgcn_exp2f(Ms + __log2f(Ls) - (M + __log2f(total))) : 0.f;
+        __builtin_amdgcn_exp2f(Ms + __log2f(Ls) - (M + __log2f(total)));
   }
 }
 

@@ -429,7 +429,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_f32_kernel(AttnParams p) {
     // a group without keys has sums of zero
     float w = exp2f((m_run - M) * c);
     l_run *= w;
-    L_Rr = l_ref > 0.f ? l_ref * exp2f((m_ref - M_R) * c) : 0.f;
+    L_Rr = l_ref == 0.f ? 0.f : l_ref * exp2f((m_ref - M_R) * c);
 #pragma unroll
     for (int i = 0; i < DB; ++i) o[i] *= w;
 #pragma unroll
@@ -438,7 +438,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_f32_kernel(AttnParams p) {
       w = exp2f((r0[64 * S::OREGS] - M) * c);
       l_run += r0[64 * (S::OREGS + 1)] * w;
       const float lr = r0[64 * (S::OREGS + 3)];
-      if (lr > 0.f) L_Rr += lr * exp2f((r0[64 * (S::OREGS + 2)] - M_R) * c);
+      if (lr != 0.f) L_Rr += lr * exp2f((r0[64 * (S::OREGS + 2)] - M_R) * c);
 #pragma unroll
       for (int i = 0; i < DB; ++i)
 #pragma unroll
@@ -447,7 +447,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_f32_kernel(AttnParams p) {
     m_run = M;
   }
   if (!qvalid) return;
-  L_R = L_Rr > 0.f ? L_Rr * exp2f((M_R - m_run) * c) : 0.f;
+  L_R = L_Rr == 0.f ? 0.f : L_Rr * exp2f((M_R - m_run) * c);  // a NaN stays one
   const float sum = L_R + l_run, inv = 1.f / sum;
   float* op = static_cast<float*>(const_cast<void*>(ov.p)) + b * ov.sb + h * ov.sh + (int64_t)qrow * ov.ss;
 #pragma unroll

@@ -1,9 +1,11 @@
-"""Keys without weight in joint attention of both types: whole query tiles, key ranges and
-their merge, reference segments.
+"""Keys without weight, and keys that are no numbers, in joint attention of both types: whole query tiles, key ranges
+and their merge, reference segments.
 
-A key of scores of -inf, or far below the rest, has no part in any output: they are those of the fp64 formula. Tolerance of a
-bf16 output: its own rounding (2^-8 of the value), the probabilities' (2^-8 each, of the numerator and of the sum that
-divides) and fp32 scores (below 2^-10 in the exponent), of the attention-weighted mean of |v|; the path's bars otherwise.
+A key of scores of -inf, or far below the rest, has no part in any output: they are those of the fp64 formula. Tolerance
+of a bf16 output: its own rounding (2^-8 of the value), the probabilities' (2^-8 each, of the numerator and of the sum
+that divides) and fp32 scores (below 2^-10 in the exponent), of the attention-weighted mean of |v|; the path's bars
+otherwise. A NaN key is in every sum over its side: o, the masses and the log-sum-exp of all keys are NaN, and that of
+the reference where the key is one of it.
 """
 
 import numpy as np
@@ -57,7 +59,9 @@ PATH_IDS = ["bf16 whole", "bf16 ranges", "f32"]
 
 
 def _close(o, want, av, dtype):
-    tol = O_TOL["f32"] if dtype == "f32" else 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -10) * (av + np.abs(want)) + 1e-6
+    tol = O_TOL["f32"]
+    if dtype == "bf16":
+        tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -10) * (av + np.abs(want)) + 1e-6
     return (np.abs(host(o) - want) <= tol).all()
 
 
@@ -115,3 +119,46 @@ def test_segments_without_weight(d, workspace):
     assert max_abs(host(r.ref_mass), want.sum(-1)) <= MASS_TOL["bf16"]
     v = np.concatenate((host(x["v_ref"]), host(x["v_tgt"])), 2)
     assert _close(r.o_tgt, p @ v, p @ np.abs(v), "bf16")
+
+
+@pytest.mark.parametrize("dtype,workspace", PATHS, ids=PATH_IDS)
+@pytest.mark.parametrize("n_ref,n_tgt", SIZES)
+@pytest.mark.parametrize("d", [64, 128])
+def test_nan_keys(dtype, d, n_ref, n_tgt, workspace):
+    x = _inputs(dtype, d, n_ref, n_tgt)
+    clean = _run(x, workspace)
+    for side, n in (("ref", n_ref), ("tgt", n_tgt)):
+        for row in (0, n // 2, n - 1):
+            k = x["k_" + side]
+            old = k[0, 1, row, 5].clone()
+            k[0, 1, row, 5] = float("nan")
+            r = _run(x, workspace)
+            k[0, 1, row, 5] = old
+            torch.cuda.synchronize()
+            print(dtype, d, n_ref, n_tgt, workspace, side, row, flush=True)
+            for t in (r.o_tgt, r.o_ref, r.ref_mass, r.ref_mass_refq, r.lse[..., 1]):
+                assert torch.isnan(t[0, 1]).all(), (side, row)
+            if side == "ref":
+                assert torch.isnan(r.lse[0, 1, :, 0]).all(), row
+            else:  # formed before the target's keys, but by another tile's maximum in a range with the NaN
+                assert max_abs(host(r.lse[0, 1, :, 0]), host(clean.lse[0, 1, :, 0])) <= FINE, row
+            for a, b in ((r.o_tgt, clean.o_tgt), (r.o_ref, clean.o_ref), (r.ref_mass, clean.ref_mass), (r.lse, clean.lse),
+                         (r.ref_mass_refq, clean.ref_mass_refq)):
+                assert torch.equal(a[0, 0], b[0, 0]), (side, row)
+
+
+@pytest.mark.parametrize("workspace", [False, True], ids=["whole", "ranges"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_nan_keys_of_segments(d, workspace):
+    """The NaN is in the sum that every segment's mass is a share of."""
+    n_ref, n_tgt, ends = 700, 290, [128, 320, 640, 700]
+    x = _inputs("bf16", d, n_ref, n_tgt)
+    for row in (3, 400, 699):
+        old = x["k_ref"][0, 0, row, 5].clone()
+        x["k_ref"][0, 0, row, 5] = float("nan")
+        r = _run(x, workspace, n_seg=4, seg_end=ends, seg_mass=True)
+        x["k_ref"][0, 0, row, 5] = old
+        torch.cuda.synchronize()
+        assert torch.isnan(r.seg_mass[0, 0]).all() and torch.isnan(r.ref_mass[0, 0]).all() and \
+            torch.isnan(r.o_tgt[0, 0]).all(), row
+        assert torch.isfinite(r.seg_mass[0, 1]).all() and torch.isfinite(r.o_tgt[0, 1]).all(), row
