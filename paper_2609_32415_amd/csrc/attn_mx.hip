@@ -105,7 +105,8 @@ constexpr int kRowBytes = KIND == 0 ? D / 2 : KIND == 1 ? D : 2 * D;
 
 // One K or V stream: the rows of a (batch, head), read tile by tile through a buffer resource, so that a lane's
 // offsets within a tile never change and rows past the last read as zeros (their scores are masked, and
-// zeros under scale byte 0 are zeros). A tile with no valid rows reads nothing.
+// zeros under scale byte 0 are zeros; the range check covers the scalar offset too). A tile with no valid rows reads
+// nothing.
 struct Stream {
   const uint8_t* codes;
   const uint8_t* scales;

@@ -142,8 +142,8 @@ def test_nan_keys(dtype, d, n_ref, n_tgt, workspace):
                 assert torch.isnan(r.lse[0, 1, :, 0]).all(), row
             else:  # formed before the target's keys, but by another tile's maximum in a range with the NaN
                 assert max_abs(host(r.lse[0, 1, :, 0]), host(clean.lse[0, 1, :, 0])) <= FINE, row
-            for a, b in ((r.o_tgt, clean.o_tgt), (r.o_ref, clean.o_ref), (r.ref_mass, clean.ref_mass), (r.lse, clean.lse),
-                         (r.ref_mass_refq, clean.ref_mass_refq)):
+            for a, b in ((r.o_tgt, clean.o_tgt), (r.o_ref, clean.o_ref), (r.ref_mass, clean.ref_mass),
+                         (r.lse, clean.lse), (r.ref_mass_refq, clean.ref_mass_refq)):
                 assert torch.equal(a[0, 0], b[0, 0]), (side, row)
 
 
