@@ -570,8 +570,10 @@ def rope(q, k=None, *, pos, freq, axis, pairing="interleaved", inverse=False, q_
     Where gradients are recorded and ``q`` or ``k`` requires them, the results carry them; ``q_out`` and
     ``k_out`` are refused then. ``pos`` and ``freq`` have none.
     """
-    if (q.requires_grad or pos.requires_grad or freq.requires_grad or
-            any(t is not None and t.requires_grad for t in (k, q_out, k_out))) and torch.is_grad_enabled():
+    # (written out: a loop over the tensors takes longer than the launch's own checks)
+    if torch.is_grad_enabled() and (
+            q.requires_grad or k is not None and k.requires_grad or pos.requires_grad or freq.requires_grad or
+            q_out is not None and q_out.requires_grad or k_out is not None and k_out.requires_grad):
         if pos.requires_grad or freq.requires_grad:
             raise ValueError("rope has no gradients of pos and freq")
         if q_out is not None or k_out is not None:
