@@ -779,7 +779,10 @@ def joint_attn_mx(q_tgt, k_tgt, v_tgt, *, k_mx, v_mx, q_mx=None, q_ref=None, k_r
     def opt(name, flag, shape):
         if flag is None or flag is False:
             return None
-        return _f32_out(name, None if flag is True else flag, shape, where)
+        t = _f32_out(name, None if flag is True else flag, shape, where)
+        if flag is not True and t.get_device() != dev:
+            _elsewhere(name, t, dev)
+        return t
 
     mass_t = opt("ref_mass", ref_mass, (B, H, n_tgt))
     lse_t = opt("lse", lse, (B, H, n_tgt, 2))
@@ -794,6 +797,8 @@ def joint_attn_mx(q_tgt, k_tgt, v_tgt, *, k_mx, v_mx, q_mx=None, q_ref=None, k_r
         if ws.get_device() != dev:
             _elsewhere("workspace", ws, dev)
         nbytes = _nbytes(ws)
+    if clock_probe is not None and clock_probe.get_device() != dev:
+        _elsewhere("clock_probe", clock_probe, dev)
     word = lambda t: 0 if t is None else t.data_ptr()
     args = L.ARGS_PACK.pack(
         *_words("q_tgt", q_tgt, dt, shp_t, dev), *_words("k_tgt", k_tgt, dt, shp_t, dev),
