@@ -630,9 +630,13 @@ ra_status mx_set(const char* who, const ra_mx_desc* desc, const ra_mx_args* args
 // Attention over a quantised cache takes one of two ways. A kernel for few target rows reads the codes itself, each
 // query tile of 32 rows on its own; other calls read the cache back into the workspace and attend over that with
 // refadapt_joint_attn's kernels, which share a tile of keys between 256 rows. The first takes up to 256 target rows,
-// and up to 1024 where all query tiles run at once. Measured, in us, first against second way: 24 heads of 128, 4352
-// reference rows in 4 bits, 61 rows 17 / 36, 256 28 / 45, 512 58 / 58, 1024 105 / 93; 3 heads, 1024 rows 29 / 36; 48 (batch,
-// head) pairs, 256 rows 54 / 67; in 8 bits 24 heads, 256 rows 35 / 46, 512 70 / 61.
+// and up to 1024 where all query tiles run at once. Measured, in us, first against second way, 4352 reference rows. Heads
+// of 128 in 4 bits: 24 heads, 33 rows 15 / 36, 256 27 / 45, 512 54 / 59, 1024 100 / 92; 3 heads, 1024 rows 29 / 36; 48
+// heads, 256 rows 52 / 69; in 8 bits 24 heads, 256 rows 33 / 47, 512 66 / 60. Heads of 64 in 4 bits: 24 heads, 256 rows
+// 27 / 33, 512 32 / 40, 1024 55 / 63; in 8 bits 256 20 / 33, 512 38 / 41, 1024 64 / 65. Where the rule takes the slower
+// way: 257 to 512 rows that do not run at once (48 heads of 64 over 1024 rows in 4 bits, 384 rows 22 / 30; of 128 over
+// 16384, 512 rows 236 / 336), 2048 rows of few heads (3 of 64 over 1024 rows 19 / 28), and, the other way round, 1024
+// rows over a long cache in 8 bits (3 heads of 128 over 16384 rows 60 / 53).
 constexpr int kFewMaxRows = 256, kFewMaxRowsAtOnce = 1024;
 
 bool few_rows(const ra_attn_desc& d, int format) {
@@ -644,7 +648,9 @@ bool few_rows(const ra_attn_desc& d, int format) {
 
 // Key ranges of a few-rows launch, from its estimated time: rounds of workgroups, a step (one tile of every wavefront) at
 // a time, each round with its start and end; more than one range adds the merge. Measured: 1.15 us a step at head dim
-// 128 in 4 bits, 1.55 in 8, 6 us to start and end a workgroup, 4 us for a merge.
+// 128 in 4 bits, 1.55 in 8, 6 us to start and end a workgroup, 4 us for a merge. Head dim 64 is set to 0.6 of a step. In
+// full rounds of later kernels a step took 1.07 and 1.27 us at head dim 128, 0.69 at 64 in 8 bits, and 1.18 in 4, where
+// two workgroups share a CU.
 struct FewPlan {
   int64_t q_tiles, key_tiles, chunks, rows;  // rows: of partial results
   double us;

@@ -27,12 +27,13 @@
 // freeze as (m_R, l_R). The wavefronts' partial results meet in LDS; where key ranges are split over
 // workgroups, those of the workgroups in the workspace and the merge kernel, in a fixed order.
 //
-// Measured, 24 heads of 128 over 16384 cached rows, with the merge: in 4 bits 18 us for 1 row, 27 for 61, 70 for 256 (780
-// TFLOP/s); in 8 bits 29, 39, 95. One row in 8 bits reads 3.8 TB/s. A tile takes a wavefront about 130 vector
-// instructions beside 16 products and the LDS 192 clocks (it takes 64 bytes a clock in); without V's stores to
-// LDS 256 rows would take 62 us, without exponentials 68, and with every read from L2 no less. In 8 bits the address
-// unit adds to it: a wavefront's K loads touch 32 rows each (78 us instead of 95 if they did not). Workgroups of 4
-// wavefronts, or of several query groups that share codes through L1, were no faster.
+// Measured, 24 heads of 128 over 16384 cached rows, with the merge, caches out of the last-level cache (and in it): in
+// 4 bits 21 us (19) for 1 row, 28 for 61, 72 for 256 (725 TFLOP/s); in 8 bits 29 (25), 35 (31), 95 (89). One row in 8
+// bits reads 3.5 TB/s (4.2). A tile takes a wavefront about 130 vector instructions beside 16 products and the LDS 192
+// clocks (it takes 64 bytes a clock in); of 70 us in 4 bits for 256 rows V's stores to LDS were 8, exponentials 2, and
+// with every read from L2 it took no less. In 8 bits the address unit adds to it: a wavefront's K loads touch 32 rows
+// each (78 us instead of 95 if they did not). Workgroups of 4 wavefronts, or of several query groups that share codes
+// through L1, were no faster.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -195,7 +196,8 @@ __device__ __forceinline__ bf16x8 k_operand(const KTile<D, KIND>& t, int i, int 
 constexpr int VBLOCK = 512 + 32;  // elements from one block to the next
 template <int D, int KIND>
 __device__ __forceinline__ void store_v(uint16_t* lds, const VTile<D, KIND>& t, int i, int j, int lane) {
-  constexpr int PR = VTile<D, KIND>::PR, step = 64 / PR;  // 8 or 16 rows: row + i * step keeps the lane's bit 1 and, of 16 rows, its place
+  // 8 or 16 rows: row + i * step keeps the lane's bit 1 and, of 16 rows, its place
+  constexpr int PR = VTile<D, KIND>::PR, step = 64 / PR;
   const int row = lane / PR, col = lane % PR;
   const int key = i * step;
   uint16_t* const p = lds + VBLOCK * ((D / 32) * (key / 16) + col / 2) + 32 * (row + key % 16) +
@@ -247,6 +249,9 @@ struct FewLds {
   float sum[BM];  // of the rounded probabilities of the workgroup's rows
 };
 
+// Head dim 64 in 4 bits is held to 128 registers (one of them spilled) for two workgroups a CU: 24 heads over 4352
+// rows, 512 target rows 31 us (37 with one), 1024 55 (63); 256, which one a CU would hold at once, 27 (19). In 8 bits
+// 512 rows take 38 us with one and 45 with two; head dim 128 has no room in LDS for a second.
 template <int D, bool FP4>
 __global__ __launch_bounds__(64 * NW, D == 64 && FP4 ? 4 : 2) void attn_mx_few_kernel(MxFewParams p) {
   constexpr int DB = D / 32, NI = D / 64;

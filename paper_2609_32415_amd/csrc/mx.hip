@@ -14,9 +14,9 @@
 // A block that holds a NaN or an infinity gets the scale byte 255 and reads back as NaN throughout.
 //
 // Both kernels are bound by memory: 2 bytes an element in bf16 and 0.53 (1.03) of codes and scales. A thread keeps four
-// runs of 8 elements in flight. Measured: 24 heads x 4352 x 128 of K and V to 4 bits 13.9 us (4.9 TB/s) and back 12.4 us;
-// K, V and Q of 12544 rows to 8 bits 68 to 80 us (5.2 to 4.4 TB/s; the rows of a head 6 KiB apart) and back 53 us
-// (6.6 TB/s, part of it into the last-level cache). A large copy moves 5.2 TB/s.
+// runs of 8 elements in flight. Measured: 24 heads x 4352 x 128 of K and V to 4 bits 13.8 us (4.9 TB/s) and back 12.7
+// us (5.3); K, V and Q of 12544 rows to 8 bits 66 us (5.3 TB/s; 67 with the rows of a head 6 KiB apart) and back 67 us.
+// In turn 75 to 82 and 54 us: part of the codes is read from the last-level cache. A large copy moves 5.2 TB/s.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
