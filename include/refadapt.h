@@ -142,8 +142,8 @@ typedef struct {
  * [0, 1] by construction and is 0 when n_ref == 0. lse values are natural-log
  * log-sum-exp of the scaled logits over reference keys / all keys (lse_ref is
  * -inf when n_ref == 0). A key whose score is -inf drops out; a NaN key makes o
- * and every mass and lse value that it enters NaN. Outputs are written in `dtype` (accumulation is fp32,
- * bf16 MFMA for RA_BF16). Writing ref_mass / lse does not change o (the
+ * and every mass and lse value that it enters NaN. Outputs are written in
+ * `dtype` (accumulation is fp32, bf16 MFMA for RA_BF16). Writing ref_mass / lse does not change o (the
  * attention output is bit-identical with them on or off). Requesting seg_mass
  * folds the reference sums segment by segment, so o then differs from the
  * launch without it by fp32 rounding only.

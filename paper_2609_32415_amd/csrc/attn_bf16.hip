@@ -41,9 +41,9 @@
 // each of its terms, so a sum within 2^12 proves that every probability is at
 // most 2^12 and m may stay. The test runs (wave-wide, NaN and inf failing it)
 // once a tile, before any of its probabilities enters O; when it fails (always at a
-// workgroup's first tile with a finite score, where m stands for -inf), a cold path takes the row max of
-// the scores, rescales O and l, and forms the probabilities again. The
-// O rescale and the row max are thus almost never executed.
+// workgroup's first tile with a finite score, where m stands for -inf), a cold path
+// takes the row max of the scores, rescales O and l, and forms the probabilities again.
+// The O rescale and the row max are thus almost never executed.
 // Row sums add the fp32 probabilities, so the reference mass and the
 // log-sum-exp carry no bf16 rounding. O is divided by a second sum, that of
 // the bf16-rounded probabilities it accumulated (one v_dot2c_f32_bf16 per
