@@ -4,7 +4,8 @@
  * sequence with fresh or cached reference K/V and per-query reference mass,
  * the consecutive target-Q change, the reuse gate and the cache commit; the
  * rotary positions of Q and K, and a reference cache in 8 or 4 bits with the
- * attention over it.
+ * attention over it; the layer norm of the hidden rows, and their projections
+ * in 8 or 4 bits, with their gradients.
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -479,6 +480,143 @@ typedef struct {
 size_t refadapt_joint_attn_mx_workspace_size(const ra_attn_desc* desc, int32_t format, int32_t with_q);
 ra_status refadapt_joint_attn_mx(const ra_attn_desc* desc, const ra_attn_args* args, const ra_mx_cache* cache,
                                  void* stream);
+
+/* ---- Around the attention: layer norm and the projections ------------------ */
+
+/* Rows [batch, rows, width]: ra_tensor.stride_h is not read; elements of a row are
+ * contiguous, at any alignment of the element type. */
+typedef struct {
+  int32_t batch, rows, width; /* batch >= 1, rows >= 0, 1 <= width <= 16384 */
+  int32_t dtype;              /* ra_dtype of the rows */
+  int32_t param_dtype;        /* ra_dtype of weight, bias, scale, shift and their gradients: dtype or RA_F32 */
+  int32_t format;             /* ra_mx_format of y_mx; not read without it */
+  float eps;                  /* >= 0, added to the variance */
+} ra_norm_desc;
+
+typedef struct {
+  ra_tensor x;
+  ra_tensor y;            /* the result; NULL data with y_mx */
+  ra_mx_tensor y_mx;      /* the result as codes (head strides are not read); NULL codes and scales with y */
+  const void* weight;     /* [width], or NULL: ones */
+  const void* bias;       /* [width], or NULL: zeros */
+  const void* scale;      /* [batch, width], or NULL: zeros */
+  const void* shift;      /* [batch, width], or NULL: zeros */
+  int64_t scale_stride, shift_stride; /* elements from one batch entry to the next; 0: one for all */
+  float* stats;           /* [batch, rows, 2] mean and 1 / deviation of each row, written; or NULL */
+} ra_norm_args;
+
+/*
+ * refadapt_layer_norm - layer norm of hidden rows with a block's modulation.
+ *
+ *   h = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps)      (over a row's width)
+ *   y = (h * weight + bias) * (1 + scale[b]) + shift[b]
+ * in fp32, rounded once to dtype; with y_mx those rounded rows become codes as
+ * refadapt_mx_commit makes them (bit for bit). y may be x itself (same data and
+ * strides, batch entries apart); otherwise what is written overlaps nothing else.
+ * A row with a NaN or an infinity is NaN throughout and touches no other row.
+ * Errors: RA_EINVAL (null desc, args or tensors, both of y and y_mx, sizes, dtypes,
+ * eps, negative or overlapping strides, x broadcast over the batch and normalised in
+ * place), RA_EUNSUPPORTED (width above 16384, or not a multiple of 32 with y_mx,
+ * alignment, batch above 65535, 2^26 or more rows of up to 1024, 2^24 of up to 8192,
+ * 2^22 of more elements).
+ */
+ra_status refadapt_layer_norm(const ra_norm_desc* desc, const ra_norm_args* args, void* stream);
+
+typedef struct {
+  ra_tensor dy;           /* the gradient of y */
+  ra_tensor x;            /* as given to refadapt_layer_norm, with weight, bias and scale */
+  ra_tensor dx;           /* NULL data: not wanted */
+  const float* stats;     /* as written by refadapt_layer_norm */
+  const void *weight, *bias, *scale;
+  int64_t scale_stride;
+  void *dweight, *dbias;  /* [width], or NULL: not wanted */
+  void *dscale, *dshift;  /* [batch, width], or NULL: not wanted */
+  void* workspace;        /* refadapt_layer_norm_grad_workspace_size(desc) bytes where one of the four is wanted */
+  size_t workspace_bytes;
+} ra_norm_grad_args;
+
+/*
+ * refadapt_layer_norm_grad - the gradients of refadapt_layer_norm.
+ *
+ * With r = 1 / deviation and e = dy * (1 + scale[b]) * weight:
+ *   dx = r * (e - mean(e) - h * mean(e * h))
+ *   dweight = sum of dy * (1 + scale) * h, dbias = sum of dy * (1 + scale)   (all rows)
+ *   dscale[b] = sum of dy * (h * weight + bias), dshift[b] = sum of dy       (rows of b)
+ * Sums are fp32 over a chunk of rows and fp64 over the chunks, in a fixed order
+ * (results are bitwise reproducible), rounded once to param_dtype. dx may be dy or x
+ * itself. Without rows the sums are zeros. A scale shared over the batch
+ * (scale_stride 0) still has one gradient per entry. The workspace needs no
+ * initialisation and must not be used by another call that runs concurrently.
+ * Errors: as refadapt_layer_norm; RA_EINVAL (no gradient wanted, null stats);
+ * RA_EWORKSPACE (missing or smaller workspace).
+ */
+size_t refadapt_layer_norm_grad_workspace_size(const ra_norm_desc* desc);
+ra_status refadapt_layer_norm_grad(const ra_norm_desc* desc, const ra_norm_grad_args* args, void* stream);
+
+/* Products of microscaled operands: rows [batch, rows, n_in] times weights [n_out, n_in]. */
+typedef struct {
+  int32_t batch, rows;        /* batch >= 1, rows >= 0 */
+  int32_t n_in;               /* a multiple of 32 */
+  int32_t n_out;              /* >= 1 */
+  int32_t dtype;              /* ra_dtype of x, y and bias, and of dy, dx and dbias */
+  int32_t x_format, w_format; /* ra_mx_format of the rows (as x_mx has it, or as x is rounded) and of the weights */
+} ra_linear_desc;
+
+typedef struct {
+  ra_tensor x;       /* plain rows, 16-byte aligned with strides in whole 16-byte units; NULL data with x_mx */
+  ra_mx_tensor x_mx; /* rows as codes (head strides are not read); NULL codes and scales with x */
+  ra_mx_tensor w;    /* weights as codes: row n at stride_s * n (batch and head strides are not read) */
+  const void* bias;  /* [n_out] of dtype, or NULL */
+  ra_tensor y;       /* [batch, rows, n_out] at any alignment of its elements */
+  void* workspace;   /* refadapt_mx_linear_workspace_size(desc, x_mx given) bytes, 16-byte aligned */
+  size_t workspace_bytes;
+} ra_linear_args;
+
+/*
+ * refadapt_mx_linear - a projection over microscaled operands.
+ *
+ *   y = Q(x) w^T + bias
+ * with Q(x) the values of x as refadapt_mx_commit rounds it to x_format (of x_mx: its
+ * values) and w the values of the weights. Sums are fp32, rounded once to dtype. Of
+ * RA_BF16 results with an RA_MXFP8 side each 64 products are added by a matrix
+ * instruction that keeps about 13 bits below the largest of them (an error of at most
+ * 2^-10 of the sum of their magnitudes, about 2e-5 of the result for normal data);
+ * RA_F32 results and those of two RA_MXFP4 sides are exact to fp32 roundings. Codes
+ * under scale byte 255 are NaN. Results are deterministic. Scale rows that are not in
+ * whole 4-byte words are read as the aligned words that hold them.
+ * The workspace needs no initialisation and must not be used by another call that runs
+ * concurrently; y overlaps nothing.
+ * Errors: RA_EINVAL (null desc, args or tensors, both of x and x_mx, sizes, enums,
+ * strides), RA_EUNSUPPORTED (n_in not a multiple of 32, alignment, rows of x_mx not
+ * evenly spaced over the batch, rows longer or further apart than 4 MiB, batch above
+ * 65535, 2^32 or more elements of x or of y in rows of whole eights), RA_EWORKSPACE.
+ */
+size_t refadapt_mx_linear_workspace_size(const ra_linear_desc* desc, int32_t x_mx);
+ra_status refadapt_mx_linear(const ra_linear_desc* desc, const ra_linear_args* args, void* stream);
+
+typedef struct {
+  ra_tensor dy;    /* [batch, rows, n_out], the gradient of y */
+  ra_mx_tensor w;  /* as given to refadapt_mx_linear; not read without dx */
+  ra_tensor dx;    /* [batch, rows, n_in]; NULL data: not wanted */
+  void* dbias;     /* [n_out] of dtype, or NULL: not wanted */
+  void* workspace; /* refadapt_mx_linear_grad_workspace_size(desc) bytes, 16-byte aligned */
+  size_t workspace_bytes;
+} ra_linear_grad_args;
+
+/*
+ * refadapt_mx_linear_grad - the gradients of refadapt_mx_linear.
+ *
+ *   dx = dy w            (the rounding of x passes gradients on as they are)
+ *   dbias = sum over the rows of dy
+ * with w the values of the weights, which have no gradient of their own. Products and
+ * sums are exact to fp32 roundings (fp32 dy enters as three bf16 terms), rounded once
+ * to dtype, and deterministic. Where dtype is RA_BF16 and n_out a multiple of 8, rows
+ * of dy lie in whole 16-byte units and evenly over the batch. Without rows dbias is
+ * zeros. desc->x_format is not read beyond its check.
+ * Errors: as refadapt_mx_linear; RA_EINVAL (no gradient wanted).
+ */
+size_t refadapt_mx_linear_grad_workspace_size(const ra_linear_desc* desc);
+ra_status refadapt_mx_linear_grad(const ra_linear_desc* desc, const ra_linear_grad_args* args, void* stream);
 
 /* ---- Diagnostics sidecar --------------------------------------------------
  *

@@ -38,6 +38,9 @@ diagnostics          The analysis quantities of Secs. 3.1-3.3 and App. A.2:
 rope                 Rotary positions with several axes.
 mx                   The reference cache in blocks of 32 elements that share
                      a power-of-two scale: codes, scales and their values.
+norm                 The layer norm of hidden rows with a block's modulation, and
+                     its gradients.
+linear               Projections over microscaled operands, and their gradients.
 
 Every function is pinned by ``-m "not gpu"`` tests in ``tests/`` against
 closed forms, library routines (torch SDPA in fp64, scipy logsumexp),
@@ -49,7 +52,7 @@ from .joint_attention import joint_attention, joint_attention_loops, segment_mas
 from .stats import q_change, head_exposure, gate, GateResult, REUSE, REACTIVATE, COMPUTE
 from .controller import run_controller, local_impact, ControllerTrace
 from .rope import rope
-from . import diagnostics, mx
+from . import diagnostics, linear, mx, norm
 
 __all__ = [
     "joint_attention",
@@ -67,5 +70,7 @@ __all__ = [
     "ControllerTrace",
     "diagnostics",
     "rope",
+    "linear",
     "mx",
+    "norm",
 ]

@@ -59,6 +59,13 @@ EXPORTED = (
     "refadapt_mx_read",
     "refadapt_joint_attn_mx_workspace_size",
     "refadapt_joint_attn_mx",
+    "refadapt_layer_norm",
+    "refadapt_layer_norm_grad_workspace_size",
+    "refadapt_layer_norm_grad",
+    "refadapt_mx_linear_workspace_size",
+    "refadapt_mx_linear",
+    "refadapt_mx_linear_grad_workspace_size",
+    "refadapt_mx_linear_grad",
     "refadapt_kv_drift_workspace_size",
     "refadapt_kv_drift",
     "refadapt_drift_log_ratio_workspace_size",
@@ -129,6 +136,72 @@ class ra_mx_args(ctypes.Structure):
 
 class ra_mx_cache(ctypes.Structure):
     _fields_ = [("format", ctypes.c_int32), ("k", ra_mx_tensor), ("v", ra_mx_tensor), ("q", ra_mx_tensor)]
+
+
+class ra_norm_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "rows", "width", "dtype", "param_dtype", "format")] + [
+        ("eps", ctypes.c_float)]
+
+
+class ra_norm_args(ctypes.Structure):
+    _fields_ = [
+        ("x", ra_tensor),
+        ("y", ra_tensor),
+        ("y_mx", ra_mx_tensor),
+        ("weight", ctypes.c_void_p),
+        ("bias", ctypes.c_void_p),
+        ("scale", ctypes.c_void_p),
+        ("shift", ctypes.c_void_p),
+        ("scale_stride", ctypes.c_int64),
+        ("shift_stride", ctypes.c_int64),
+        ("stats", ctypes.c_void_p),
+    ]
+
+
+class ra_norm_grad_args(ctypes.Structure):
+    _fields_ = [
+        ("dy", ra_tensor),
+        ("x", ra_tensor),
+        ("dx", ra_tensor),
+        ("stats", ctypes.c_void_p),
+        ("weight", ctypes.c_void_p),
+        ("bias", ctypes.c_void_p),
+        ("scale", ctypes.c_void_p),
+        ("scale_stride", ctypes.c_int64),
+        ("dweight", ctypes.c_void_p),
+        ("dbias", ctypes.c_void_p),
+        ("dscale", ctypes.c_void_p),
+        ("dshift", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class ra_linear_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "rows", "n_in", "n_out", "dtype", "x_format", "w_format")]
+
+
+class ra_linear_args(ctypes.Structure):
+    _fields_ = [
+        ("x", ra_tensor),
+        ("x_mx", ra_mx_tensor),
+        ("w", ra_mx_tensor),
+        ("bias", ctypes.c_void_p),
+        ("y", ra_tensor),
+        ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class ra_linear_grad_args(ctypes.Structure):
+    _fields_ = [
+        ("dy", ra_tensor),
+        ("w", ra_mx_tensor),
+        ("dx", ra_tensor),
+        ("dbias", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_size_t),
+    ]
 
 
 class ra_attn_desc(ctypes.Structure):
@@ -229,6 +302,17 @@ def _load():
     lib.refadapt_joint_attn_mx.argtypes = [ctypes.POINTER(ra_attn_desc), ctypes.POINTER(ra_attn_args),
                                            ctypes.POINTER(ra_mx_cache), vp]
     lib.refadapt_joint_attn_mx.restype = i32
+    for name, desc, args in (("layer_norm", ra_norm_desc, ra_norm_args),
+                             ("layer_norm_grad", ra_norm_desc, ra_norm_grad_args),
+                             ("mx_linear", ra_linear_desc, ra_linear_args),
+                             ("mx_linear_grad", ra_linear_desc, ra_linear_grad_args)):
+        f = getattr(lib, "refadapt_" + name)
+        f.argtypes, f.restype = [ctypes.POINTER(desc), ctypes.POINTER(args), vp], i32
+    for name, args in (("layer_norm_grad", [ctypes.POINTER(ra_norm_desc)]),
+                       ("mx_linear", [ctypes.POINTER(ra_linear_desc), i32]),
+                       ("mx_linear_grad", [ctypes.POINTER(ra_linear_desc)])):
+        f = getattr(lib, f"refadapt_{name}_workspace_size")
+        f.argtypes, f.restype = args, ctypes.c_size_t
     lib.refadapt_kv_drift_workspace_size.argtypes = [i32, i32, i32, i32]
     lib.refadapt_kv_drift_workspace_size.restype = ctypes.c_size_t
     lib.refadapt_kv_drift.argtypes = [i32, i32, i32, i32, i32, ra_tensor, ra_tensor, ra_tensor, ra_tensor, f32,
@@ -284,6 +368,27 @@ _joint_attn_mx_ws_packed = ctypes.CFUNCTYPE(ctypes.c_size_t, ctypes.c_char_p, ct
     ("refadapt_joint_attn_mx_workspace_size", LIB))
 _joint_attn_mx_packed = ctypes.CFUNCTYPE(ctypes.c_int32, ctypes.c_char_p, ctypes.c_char_p, ctypes.c_char_p,
                                          ctypes.c_void_p)(("refadapt_joint_attn_mx", LIB))
+
+# And those of the layer norm and of the projections.
+NORM_DESC_PACK = struct.Struct("=6if")  # ra_norm_desc
+NORM_ARGS_PACK = struct.Struct("=23q")  # ra_norm_args
+NORM_GRAD_ARGS_PACK = struct.Struct("=23q")  # ra_norm_grad_args
+LINEAR_DESC_PACK = struct.Struct("=7i")  # ra_linear_desc
+LINEAR_ARGS_PACK = struct.Struct("=27q")  # ra_linear_args
+LINEAR_GRAD_ARGS_PACK = struct.Struct("=19q")  # ra_linear_grad_args
+assert [p.size for p in (NORM_DESC_PACK, NORM_ARGS_PACK, NORM_GRAD_ARGS_PACK, LINEAR_DESC_PACK, LINEAR_ARGS_PACK,
+                         LINEAR_GRAD_ARGS_PACK)] == [
+    ctypes.sizeof(c) for c in (ra_norm_desc, ra_norm_args, ra_norm_grad_args, ra_linear_desc, ra_linear_args,
+                               ra_linear_grad_args)]
+_layer_norm_packed = _two_blocks(("refadapt_layer_norm", LIB))
+_layer_norm_grad_packed = _two_blocks(("refadapt_layer_norm_grad", LIB))
+_mx_linear_packed = _two_blocks(("refadapt_mx_linear", LIB))
+_mx_linear_grad_packed = _two_blocks(("refadapt_mx_linear_grad", LIB))
+_one_block_size = ctypes.CFUNCTYPE(ctypes.c_size_t, ctypes.c_char_p)
+_layer_norm_grad_ws_packed = _one_block_size(("refadapt_layer_norm_grad_workspace_size", LIB))
+_mx_linear_ws_packed = ctypes.CFUNCTYPE(ctypes.c_size_t, ctypes.c_char_p, ctypes.c_int32)(
+    ("refadapt_mx_linear_workspace_size", LIB))
+_mx_linear_grad_ws_packed = _one_block_size(("refadapt_mx_linear_grad_workspace_size", LIB))
 
 
 def _check(status):
@@ -372,6 +477,38 @@ def refadapt_joint_attn_mx_workspace_size_packed(desc, fmt, with_q):
 def refadapt_joint_attn_mx_packed(desc, args, cache, stream):
     """``refadapt_joint_attn_mx`` on bytes of DESC_PACK, ARGS_PACK and MX_CACHE_PACK."""
     return _check(_joint_attn_mx_packed(desc, args, cache, stream))
+
+
+def refadapt_layer_norm_packed(desc, args, stream):
+    """``refadapt_layer_norm`` on bytes of NORM_DESC_PACK and NORM_ARGS_PACK."""
+    return _check(_layer_norm_packed(desc, args, stream))
+
+
+def refadapt_layer_norm_grad_workspace_size_packed(desc):
+    return _layer_norm_grad_ws_packed(desc)
+
+
+def refadapt_layer_norm_grad_packed(desc, args, stream):
+    """``refadapt_layer_norm_grad`` on bytes of NORM_DESC_PACK and NORM_GRAD_ARGS_PACK."""
+    return _check(_layer_norm_grad_packed(desc, args, stream))
+
+
+def refadapt_mx_linear_workspace_size_packed(desc, x_mx):
+    return _mx_linear_ws_packed(desc, x_mx)
+
+
+def refadapt_mx_linear_packed(desc, args, stream):
+    """``refadapt_mx_linear`` on bytes of LINEAR_DESC_PACK and LINEAR_ARGS_PACK."""
+    return _check(_mx_linear_packed(desc, args, stream))
+
+
+def refadapt_mx_linear_grad_workspace_size_packed(desc):
+    return _mx_linear_grad_ws_packed(desc)
+
+
+def refadapt_mx_linear_grad_packed(desc, args, stream):
+    """``refadapt_mx_linear_grad`` on bytes of LINEAR_DESC_PACK and LINEAR_GRAD_ARGS_PACK."""
+    return _check(_mx_linear_grad_packed(desc, args, stream))
 
 
 def refadapt_kv_drift_workspace_size(batch, heads, n_rows, head_dim):

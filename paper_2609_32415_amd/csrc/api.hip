@@ -838,6 +838,433 @@ ra_status refadapt_joint_attn_mx(const ra_attn_desc* desc, const ra_attn_args* a
 
 }  // extern "C"
 
+// ---- layer norm and products of microscaled operands
+
+namespace {
+
+// Rows of a [batch, rows, width] tensor (stride_h is not read) at any alignment of its elements.
+ra_status check_rows(const char* who, const char* name, const ra_tensor& t, int dtype, int32_t rows, int32_t width) {
+  if (t.data == nullptr) return fail(RA_EINVAL, "%s: null %s", who, name);
+  if (t.stride_b < 0 || t.stride_s < 0) return fail(RA_EINVAL, "%s: negative stride of %s", who, name);
+  if (rows > 1 && t.stride_s < width)
+    return fail(RA_EINVAL, "%s: row stride %lld of %s is smaller than its %d elements", who, (long long)t.stride_s, name,
+                width);
+  if (reinterpret_cast<uintptr_t>(t.data) % (dtype == RA_BF16 ? 2 : 4) != 0)
+    return fail(RA_EUNSUPPORTED, "%s: %s is not aligned to its elements", who, name);
+  return RA_OK;
+}
+
+// A tensor that is written: its batch entries lie apart.
+ra_status check_rows_out(const char* who, const char* name, const ra_tensor& t, int dtype, int32_t batch, int32_t rows,
+                         int32_t width) {
+  const ra_status s = check_rows(who, name, t, dtype, rows, width);
+  if (s != RA_OK) return s;
+  if (batch > 1 && t.stride_b < width)
+    return fail(RA_EINVAL, "%s: batch entries of %s overlap", who, name);
+  return RA_OK;
+}
+
+ra_status check_vector(const char* who, const char* name, const void* p, int dtype) {
+  if (reinterpret_cast<uintptr_t>(p) % (dtype == RA_BF16 ? 2 : 4) != 0)
+    return fail(RA_EUNSUPPORTED, "%s: %s is not aligned to its elements", who, name);
+  return RA_OK;
+}
+
+// Whole 16-byte units throughout.
+bool in_units(const ra_tensor& t, int dtype) {
+  const int64_t unit = dtype == RA_BF16 ? 8 : 4;
+  return (reinterpret_cast<uintptr_t>(t.data) & 15) == 0 && t.stride_b % unit == 0 && t.stride_s % unit == 0;
+}
+bool vector_in_units(const void* p, int64_t stride, int dtype) {
+  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride % (dtype == RA_BF16 ? 8 : 4) == 0;
+}
+
+ra_status check_norm_desc(const char* who, const ra_norm_desc* desc) {
+  if (!desc) return fail(RA_EINVAL, "%s: null desc", who);
+  const ra_norm_desc& d = *desc;
+  if (d.batch < 1 || d.rows < 0 || d.width < 1) return fail(RA_EINVAL, "%s: bad sizes", who);
+  if (d.dtype != RA_BF16 && d.dtype != RA_F32) return fail(RA_EINVAL, "%s: unknown dtype %d", who, d.dtype);
+  if (d.param_dtype != RA_F32 && d.param_dtype != d.dtype)
+    return fail(RA_EINVAL, "%s: parameters are of the rows' dtype or fp32 (got %d)", who, d.param_dtype);
+  if (!(d.eps >= 0.f) || !std::isfinite(d.eps)) return fail(RA_EINVAL, "%s: eps must be finite and not negative", who);
+  if (d.width > kNormMaxWidth) return fail(RA_EUNSUPPORTED, "%s: width %d above %d", who, d.width, kNormMaxWidth);
+  // 64, 256 or 1024 threads a row, and fewer than 2^32 in a launch
+  const int64_t most = int64_t(1) << (d.width <= 1024 ? 26 : d.width <= 8192 ? 24 : 22);
+  if (d.batch > 65535 || (int64_t)d.batch * d.rows >= most)
+    return fail(RA_EUNSUPPORTED, "%s: %d x %d rows are too many for one launch", who, d.batch, d.rows);
+  return RA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+ra_status refadapt_layer_norm(const ra_norm_desc* desc, const ra_norm_args* args, void* stream) {
+  ra_status s;
+  if ((s = check_norm_desc("layer_norm", desc)) != RA_OK) return s;
+  if (!args) return fail(RA_EINVAL, "layer_norm: null args");
+  const ra_norm_desc& d = *desc;
+  const ra_norm_args& a = *args;
+  const bool mx = a.y_mx.codes != nullptr || a.y_mx.scales != nullptr;
+  if (mx) {
+    if (a.y.data != nullptr) return fail(RA_EINVAL, "layer_norm: both y and y_mx are given");
+    if (d.format != RA_MXFP4 && d.format != RA_MXFP8) return fail(RA_EINVAL, "layer_norm: unknown format %d", d.format);
+    if (d.width % 32 != 0)
+      return fail(RA_EUNSUPPORTED, "layer_norm: width %d must be a multiple of 32 for codes", d.width);
+  }
+  if (d.rows == 0) return ok();
+  if ((s = check_rows("layer_norm", "x", a.x, d.dtype, d.rows, d.width)) != RA_OK) return s;
+  if (mx) {
+    if ((s = check_mx("y_mx", a.y_mx, d.format, d.rows, d.width)) != RA_OK) return s;
+    if (d.batch > 1 && (a.y_mx.stride_b < d.width / 2 || a.y_mx.scale_stride_b < d.width / 32))
+      return fail(RA_EINVAL, "layer_norm: batch entries of y_mx overlap");
+  } else if ((s = check_rows_out("layer_norm", "y", a.y, d.dtype, d.batch, d.rows, d.width)) != RA_OK) {
+    return s;
+  }
+  if (a.y.data == a.x.data && d.batch > 1 && a.x.stride_b == 0)
+    return fail(RA_EINVAL, "layer_norm: x is broadcast and cannot be normalised in place");
+  if (a.scale_stride < 0 || a.shift_stride < 0) return fail(RA_EINVAL, "layer_norm: negative stride of scale or shift");
+  const void* const params[4] = {a.weight, a.bias, a.scale, a.shift};
+  const int64_t strides[4] = {0, 0, a.scale_stride, a.shift_stride};
+  const char* const names[4] = {"weight", "bias", "scale", "shift"};
+  NormParams p{};
+  p.vec = d.width % 8 == 0 && in_units(a.x, d.dtype) && (mx || in_units(a.y, d.dtype));
+  for (int i = 0; i < 4; ++i) {
+    if ((s = check_vector("layer_norm", names[i], params[i], d.param_dtype)) != RA_OK) return s;
+    p.vec = p.vec && vector_in_units(params[i], strides[i], d.param_dtype);
+  }
+  if ((reinterpret_cast<uintptr_t>(a.stats) & 7) != 0)
+    return fail(RA_EUNSUPPORTED, "layer_norm: stats must be 8-byte aligned");
+  p.x = view(a.x);
+  p.y = view(a.y);
+  p.y_mx = mx_view(a.y_mx);
+  p.format = d.format;
+  p.weight = a.weight;
+  p.bias = a.bias;
+  p.scale = a.scale;
+  p.shift = a.shift;
+  p.scale_sb = a.scale_stride;
+  p.shift_sb = a.shift_stride;
+  p.stats = a.stats;
+  p.B = d.batch;
+  p.S = d.rows;
+  p.C = d.width;
+  p.eps = d.eps;
+  p.param_f32 = d.param_dtype == RA_F32;
+  return launch_status(launch_norm(d.dtype, p, static_cast<hipStream_t>(stream)), "layer_norm");
+}
+
+size_t refadapt_layer_norm_grad_workspace_size(const ra_norm_desc* desc) {
+  if (check_norm_desc("layer_norm_grad_workspace_size", desc) != RA_OK) return 0;
+  return (size_t)desc->batch * norm_grad_chunks(desc->batch, desc->rows) * 2 * desc->width * sizeof(float);
+}
+
+ra_status refadapt_layer_norm_grad(const ra_norm_desc* desc, const ra_norm_grad_args* args, void* stream) {
+  ra_status s;
+  const char* const who = "layer_norm_grad";
+  if ((s = check_norm_desc(who, desc)) != RA_OK) return s;
+  if (!args) return fail(RA_EINVAL, "%s: null args", who);
+  const ra_norm_desc& d = *desc;
+  const ra_norm_grad_args& a = *args;
+  const bool sums = a.dweight || a.dbias || a.dscale || a.dshift;
+  if (!sums && a.dx.data == nullptr) return fail(RA_EINVAL, "%s: no gradient is wanted", who);
+  NormGradParams p{};
+  p.vec = d.width % 8 == 0;
+  if (d.rows > 0) {
+    if ((s = check_rows(who, "dy", a.dy, d.dtype, d.rows, d.width)) != RA_OK) return s;
+    if ((s = check_rows(who, "x", a.x, d.dtype, d.rows, d.width)) != RA_OK) return s;
+    if (a.dx.data && (s = check_rows_out(who, "dx", a.dx, d.dtype, d.batch, d.rows, d.width)) != RA_OK) return s;
+    if (d.batch > 1 && a.dx.data && ((a.dx.data == a.x.data && a.x.stride_b == 0) ||
+                                     (a.dx.data == a.dy.data && a.dy.stride_b == 0)))
+      return fail(RA_EINVAL, "%s: a broadcast tensor cannot be replaced by its gradient", who);
+    if (a.stats == nullptr) return fail(RA_EINVAL, "%s: null stats", who);
+    p.vec = p.vec && in_units(a.dy, d.dtype) && in_units(a.x, d.dtype) && (!a.dx.data || in_units(a.dx, d.dtype));
+  }
+  if (a.scale_stride < 0) return fail(RA_EINVAL, "%s: negative stride of scale", who);
+  const void* const params[7] = {a.weight, a.bias, a.scale, a.dweight, a.dbias, a.dscale, a.dshift};
+  const char* const names[7] = {"weight", "bias", "scale", "dweight", "dbias", "dscale", "dshift"};
+  for (int i = 0; i < 7; ++i) {
+    if ((s = check_vector(who, names[i], params[i], d.param_dtype)) != RA_OK) return s;
+    if (i == 0 || i == 2) p.vec = p.vec && vector_in_units(params[i], i == 2 ? a.scale_stride : 0, d.param_dtype);
+  }
+  if ((reinterpret_cast<uintptr_t>(a.stats) & 7) != 0)
+    return fail(RA_EUNSUPPORTED, "%s: stats must be 8-byte aligned", who);
+  if (sums) {
+    const size_t need = refadapt_layer_norm_grad_workspace_size(desc);
+    if (!a.workspace || a.workspace_bytes < need)
+      return fail(RA_EWORKSPACE, "%s: workspace of %zu bytes needed, got %zu", who, need,
+                  a.workspace ? a.workspace_bytes : (size_t)0);
+    if ((reinterpret_cast<uintptr_t>(a.workspace) & 15) != 0)
+      return fail(RA_EUNSUPPORTED, "%s: workspace must be 16-byte aligned", who);
+  }
+  if (d.rows == 0 && !sums) return ok();
+  p.dy = view(a.dy);
+  p.x = view(a.x);
+  p.dx = view(a.dx);
+  p.stats = a.stats;
+  p.weight = a.weight;
+  p.bias = a.bias;
+  p.scale = a.scale;
+  p.scale_sb = a.scale_stride;
+  p.dweight = a.dweight;
+  p.dbias = a.dbias;
+  p.dscale = a.dscale;
+  p.dshift = a.dshift;
+  p.part = sums ? static_cast<float*>(a.workspace) : nullptr;
+  p.B = d.batch;
+  p.S = d.rows;
+  p.C = d.width;
+  p.param_f32 = d.param_dtype == RA_F32;
+  return launch_status(launch_norm_grad(d.dtype, p, static_cast<hipStream_t>(stream)), who);
+}
+
+}  // extern "C"
+
+namespace {
+
+size_t padded(size_t bytes) { return (bytes + 255) & ~size_t(255); }
+int64_t mx_row(int32_t format, int64_t n) { return format == RA_MXFP4 ? n / 2 : n; }
+int64_t mx_scale_row(int64_t n) { return (n / 32 + 3) & ~int64_t(3); }  // whole words
+
+ra_status check_linear_desc(const char* who, const ra_linear_desc* desc) {
+  if (!desc) return fail(RA_EINVAL, "%s: null desc", who);
+  const ra_linear_desc& d = *desc;
+  if (d.batch < 1 || d.rows < 0 || d.n_in < 1 || d.n_out < 1) return fail(RA_EINVAL, "%s: bad sizes", who);
+  if (d.dtype != RA_BF16 && d.dtype != RA_F32) return fail(RA_EINVAL, "%s: unknown dtype %d", who, d.dtype);
+  if ((d.x_format != RA_MXFP4 && d.x_format != RA_MXFP8) || (d.w_format != RA_MXFP4 && d.w_format != RA_MXFP8))
+    return fail(RA_EINVAL, "%s: unknown formats %d, %d", who, d.x_format, d.w_format);
+  if (d.n_in % 32 != 0) return fail(RA_EUNSUPPORTED, "%s: n_in %d must be a multiple of 32", who, d.n_in);
+  if (2 * (int64_t)d.n_in > kLinearMaxStride || 2 * (int64_t)d.n_out + 16 > kLinearMaxStride)
+    return fail(RA_EUNSUPPORTED, "%s: n_in %d or n_out %d above %lld", who, d.n_in, d.n_out,
+                (long long)kLinearMaxStride / 2 - 8);
+  const int64_t M = (int64_t)d.batch * d.rows;
+  if (d.batch > 65535 || M * std::max(d.n_in, (d.n_out + 7) & ~7) >= (int64_t(1) << 32))
+    return fail(RA_EUNSUPPORTED, "%s: %lld rows of %d and %d elements are too many for one call", who, (long long)M,
+                d.n_in, d.n_out);
+  return RA_OK;
+}
+
+ra_status check_weights(const char* who, const ra_linear_desc& d, const ra_mx_tensor& w) {
+  ra_mx_tensor t = w;  // one matrix: its batch and head strides are not read
+  t.stride_b = t.stride_h = t.scale_stride_b = t.scale_stride_h = 0;
+  const ra_status s = check_mx("w", t, d.w_format, d.n_out, d.n_in);
+  if (s != RA_OK) return s;
+  if (d.n_out > 1 && (t.stride_s > kLinearMaxStride || t.scale_stride_s > kLinearMaxStride))
+    return fail(RA_EUNSUPPORTED, "%s: row stride of w above %lld bytes", who, (long long)kLinearMaxStride);
+  return RA_OK;
+}
+
+// fp32 results with an e4m3 side are formed from the values in bf16.
+bool linear_by_values(const ra_linear_desc& d) {
+  return d.dtype == RA_F32 && (d.x_format == RA_MXFP8 || d.w_format == RA_MXFP8);
+}
+struct LinearSpace {
+  size_t x_codes, x_scales, x_values, w_values;
+  size_t total() const { return x_codes + x_scales + x_values + w_values; }
+};
+LinearSpace linear_space(const ra_linear_desc& d, bool x_mx) {
+  const size_t M = (size_t)d.batch * d.rows;
+  LinearSpace s{};
+  if (!x_mx) {
+    s.x_codes = padded(M * mx_row(d.x_format, d.n_in));
+    s.x_scales = padded(M * mx_scale_row(d.n_in));
+  }
+  if (linear_by_values(d)) {
+    s.x_values = padded(M * d.n_in * 2);
+    s.w_values = padded((size_t)d.n_out * d.n_in * 2);
+  }
+  return s;
+}
+
+bool linear_split_dy(const ra_linear_desc& d) { return d.dtype == RA_F32 || d.n_out % 8 != 0; }
+struct LinearGradSpace {
+  size_t dy, w, sums;
+  size_t total() const { return dy + w + sums; }
+};
+LinearGradSpace linear_grad_space(const ra_linear_desc& d) {
+  const size_t M = (size_t)d.batch * d.rows, ld = ((size_t)d.n_out + 7) & ~size_t(7);
+  return LinearGradSpace{linear_split_dy(d) ? padded(M * ld * 2 * (d.dtype == RA_F32 ? 3 : 1)) : 0,
+                         padded((size_t)d.n_in * ld * 2),
+                         padded((size_t)column_sum_chunks((int64_t)M, d.n_out) * d.n_out * sizeof(float))};
+}
+
+ra_status check_workspace(const char* who, const void* ws, size_t bytes, size_t need) {
+  if (need == 0) return RA_OK;
+  if (!ws || bytes < need)
+    return fail(RA_EWORKSPACE, "%s: workspace of %zu bytes needed, got %zu", who, need, ws ? bytes : (size_t)0);
+  if ((reinterpret_cast<uintptr_t>(ws) & 15) != 0)
+    return fail(RA_EUNSUPPORTED, "%s: workspace must be 16-byte aligned", who);
+  return RA_OK;
+}
+
+// The distance of rows that follow each other at one, over batch entries too; -1 where they do not.
+int64_t even_stride(int32_t batch, int32_t rows, int64_t sb, int64_t ss) {
+  if (rows == 1) return batch == 1 ? 0 : sb;
+  return batch == 1 || sb == rows * ss ? ss : -1;
+}
+
+void set_y(LinearParams* p, const ra_tensor& y, int dtype) {
+  p->y = view(y);
+  p->f32 = dtype == RA_F32;
+  p->y_vec = reinterpret_cast<uintptr_t>(y.data) % (dtype == RA_F32 ? 16 : 8) == 0 && y.stride_b % 4 == 0 &&
+             y.stride_s % 4 == 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t refadapt_mx_linear_workspace_size(const ra_linear_desc* desc, int32_t x_mx) {
+  if (check_linear_desc("mx_linear_workspace_size", desc) != RA_OK) return 0;
+  return linear_space(*desc, x_mx != 0).total();
+}
+
+ra_status refadapt_mx_linear(const ra_linear_desc* desc, const ra_linear_args* args, void* stream) {
+  ra_status s;
+  const char* const who = "mx_linear";
+  if ((s = check_linear_desc(who, desc)) != RA_OK) return s;
+  if (!args) return fail(RA_EINVAL, "%s: null args", who);
+  const ra_linear_desc& d = *desc;
+  const ra_linear_args& a = *args;
+  if ((s = check_weights(who, d, a.w)) != RA_OK) return s;
+  if (d.rows == 0) return ok();
+  const bool x_mx = a.x_mx.codes != nullptr || a.x_mx.scales != nullptr;
+  if (x_mx && a.x.data != nullptr) return fail(RA_EINVAL, "%s: both x and x_mx are given", who);
+  const bool values = linear_by_values(d);
+  int64_t x_row = mx_row(d.x_format, d.n_in), xs_row = mx_scale_row(d.n_in);
+  if (x_mx) {
+    if ((s = check_mx("x_mx", a.x_mx, d.x_format, d.rows, d.n_in)) != RA_OK) return s;
+    x_row = even_stride(d.batch, d.rows, a.x_mx.stride_b, a.x_mx.stride_s);
+    xs_row = even_stride(d.batch, d.rows, a.x_mx.scale_stride_b, a.x_mx.scale_stride_s);
+    if (!values && (x_row < 0 || xs_row < 0))
+      return fail(RA_EUNSUPPORTED, "%s: rows of x_mx must be evenly spaced over the batch", who);
+    if (x_row > kLinearMaxStride || xs_row > kLinearMaxStride)
+      return fail(RA_EUNSUPPORTED, "%s: row stride of x_mx above %lld bytes", who, (long long)kLinearMaxStride);
+  } else {
+    if ((s = check_tensor("x", a.x, d.dtype, d.rows, d.n_in)) != RA_OK) return s;
+  }
+  if ((s = check_rows_out(who, "y", a.y, d.dtype, d.batch, d.rows, d.n_out)) != RA_OK) return s;
+  if ((s = check_vector(who, "bias", a.bias, d.dtype)) != RA_OK) return s;
+  const LinearSpace space = linear_space(d, x_mx);
+  if ((s = check_workspace(who, a.workspace, a.workspace_bytes, space.total())) != RA_OK) return s;
+
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  uint8_t* ws = static_cast<uint8_t*>(a.workspace);
+  MxView x = mx_view(a.x_mx);
+  x.sh = x.eh = 0;
+  hipError_t e;
+  if (!x_mx) {
+    x = MxView{ws, x_row * d.rows, 0, x_row, ws + space.x_codes, xs_row * d.rows, 0, xs_row};
+    MxSet set{};
+    set.n = 1;
+    set.plain[0] = view(a.x);
+    set.plain[0].sh = 0;
+    set.mx[0] = x;
+    e = launch_mx_commit(d.dtype, d.x_format, d.batch, 1, d.rows, d.n_in, set, nullptr, nullptr, 0, st);
+    if (e != hipSuccess) return launch_status(e, who);
+  }
+  LinearParams p{};
+  p.M = (int64_t)d.batch * d.rows;
+  p.N = d.n_out;
+  p.K = d.n_in;
+  p.rows = d.rows;
+  p.parts = 1;
+  p.bias = a.bias;
+  set_y(&p, a.y, d.dtype);
+  if (values) {
+    uint8_t* const xv = ws + space.x_codes + space.x_scales;
+    uint8_t* const wv = xv + space.x_values;
+    MxSet set{};
+    set.n = 1;
+    set.plain[0] = View{xv, (int64_t)d.rows * d.n_in, 0, d.n_in};
+    set.mx[0] = x;
+    e = launch_mx_read(RA_BF16, d.x_format, d.batch, 1, d.rows, d.n_in, set, nullptr, 1, st);
+    if (e != hipSuccess) return launch_status(e, who);
+    set.plain[0] = View{wv, 0, 0, d.n_in};
+    set.mx[0] = mx_view(a.w);
+    e = launch_mx_read(RA_BF16, d.w_format, 1, 1, d.n_out, d.n_in, set, nullptr, 1, st);
+    if (e != hipSuccess) return launch_status(e, who);
+    p.x = xv;
+    p.w = wv;
+    p.x_stride = p.w_stride = 2 * d.n_in;
+    return launch_status(launch_linear(kLinearBf16, kLinearBf16, p, st), who);
+  }
+  p.x = x.codes;
+  p.xs = x.scales;
+  p.x_stride = (int32_t)x_row;
+  p.xs_stride = (int32_t)xs_row;
+  p.w = static_cast<const uint8_t*>(a.w.codes);
+  p.ws = static_cast<const uint8_t*>(a.w.scales);
+  p.w_stride = (int32_t)a.w.stride_s;
+  p.ws_stride = (int32_t)a.w.scale_stride_s;
+  return launch_status(launch_linear(d.x_format, d.w_format, p, st), who);
+}
+
+size_t refadapt_mx_linear_grad_workspace_size(const ra_linear_desc* desc) {
+  if (check_linear_desc("mx_linear_grad_workspace_size", desc) != RA_OK) return 0;
+  return linear_grad_space(*desc).total();
+}
+
+ra_status refadapt_mx_linear_grad(const ra_linear_desc* desc, const ra_linear_grad_args* args, void* stream) {
+  ra_status s;
+  const char* const who = "mx_linear_grad";
+  if ((s = check_linear_desc(who, desc)) != RA_OK) return s;
+  if (!args) return fail(RA_EINVAL, "%s: null args", who);
+  const ra_linear_desc& d = *desc;
+  const ra_linear_grad_args& a = *args;
+  if (a.dx.data == nullptr && a.dbias == nullptr) return fail(RA_EINVAL, "%s: no gradient is wanted", who);
+  const int32_t ld = (d.n_out + 7) & ~7;
+  const bool split = linear_split_dy(d);
+  int64_t dy_row = 0;
+  if (a.dx.data && (s = check_weights(who, d, a.w)) != RA_OK) return s;
+  if (d.rows > 0) {
+    if ((s = check_rows(who, "dy", a.dy, d.dtype, d.rows, d.n_out)) != RA_OK) return s;
+    if (a.dx.data) {
+      if ((s = check_rows_out(who, "dx", a.dx, d.dtype, d.batch, d.rows, d.n_in)) != RA_OK) return s;
+      dy_row = 2 * even_stride(d.batch, d.rows, a.dy.stride_b, a.dy.stride_s);
+      if (!split && (!in_units(a.dy, d.dtype) || dy_row < 0))
+        return fail(RA_EUNSUPPORTED, "%s: rows of dy must be evenly spaced, in whole 16-byte units", who);
+      if (!split && dy_row > kLinearMaxStride)
+        return fail(RA_EUNSUPPORTED, "%s: row stride of dy above %lld bytes", who, (long long)kLinearMaxStride);
+    }
+  }
+  if ((s = check_vector(who, "dbias", a.dbias, d.dtype)) != RA_OK) return s;
+  const LinearGradSpace space = linear_grad_space(d);
+  if ((s = check_workspace(who, a.workspace, a.workspace_bytes, space.total())) != RA_OK) return s;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  uint8_t* const ws = static_cast<uint8_t*>(a.workspace);
+  const int64_t M = (int64_t)d.batch * d.rows;
+  View dy = view(a.dy);
+  hipError_t e = hipSuccess;
+  if (a.dbias)
+    e = launch_column_sum(d.dtype, dy, std::max(d.rows, 1), M, d.n_out,
+                          reinterpret_cast<float*>(ws + space.dy + space.w), a.dbias, st);
+  if (e != hipSuccess || a.dx.data == nullptr || M == 0) return launch_status(e, who);
+  LinearParams p{};
+  p.M = M;
+  p.N = d.n_in;
+  p.K = ld;
+  p.rows = d.rows;
+  p.parts = d.dtype == RA_F32 ? 3 : 1;
+  set_y(&p, a.dx, d.dtype);
+  e = launch_linear_transpose(d.w_format, mx_view(a.w), d.n_out, d.n_in, ld, ws + space.dy, st);
+  if (e != hipSuccess) return launch_status(e, who);
+  p.w = ws + space.dy;
+  p.w_stride = 2 * ld;
+  p.x = static_cast<const uint8_t*>(a.dy.data);
+  p.x_stride = (int32_t)dy_row;
+  if (split) {
+    e = launch_linear_split(d.dtype, dy, d.rows, M, d.n_out, ld, ws, st);
+    if (e != hipSuccess) return launch_status(e, who);
+    p.x = ws;
+    p.x_stride = 2 * ld;
+    p.x_part = 2 * M * ld;
+  }
+  return launch_status(launch_linear(kLinearBf16, kLinearBf16, p, st), who);
+}
+
+}  // extern "C"
+
 // ---- diagnostics sidecar
 
 namespace {

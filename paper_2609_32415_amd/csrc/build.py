@@ -18,7 +18,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 PKG = os.path.dirname(HERE)
 ROOT = os.path.dirname(PKG)
 SOURCES = ["api.hip", "attn_bf16.hip", "attn_f32.hip", "stats.hip", "diag.hip", "rope.hip", "mx.hip", "attn_mx.hip",
-           "probe.hip"]
+           "norm.hip", "linear.hip", "probe.hip"]
 LIB_NAME = "librefadapt.so"
 ARCH = "gfx950"
 

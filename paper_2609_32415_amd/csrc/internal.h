@@ -176,6 +176,58 @@ struct RopeParams {
 };
 hipError_t launch_rope(int dtype, bool half, int32_t head_dim, RopeParams p, hipStream_t stream);
 
+// Layer norm of the rows of [B, S, C] (View strides sb and ss), and its gradients.
+constexpr int kNormMaxWidth = 16384;
+struct NormParams {
+  View x, y;       // y.p null: codes go to y_mx
+  MxView y_mx;     // strides sb, ss, eb, es
+  int32_t format;  // of y_mx
+  const void *weight, *bias, *scale, *shift;  // [C], [C], [B, C], [B, C], each null where not given
+  int64_t scale_sb, shift_sb;                 // elements
+  float* stats;                               // [B, S, 2] mean and 1 / deviation, or null
+  int32_t B, S, C;
+  float eps;
+  bool param_f32, vec;  // vec: every row of every tensor is in whole, aligned 16-byte units
+};
+hipError_t launch_norm(int dtype, NormParams p, hipStream_t stream);
+struct NormGradParams {
+  View dy, x, dx;  // dx.p null: not wanted
+  const float* stats;
+  const void *weight, *bias, *scale;
+  int64_t scale_sb;
+  void *dweight, *dbias, *dscale, *dshift;  // [C], [C], [B, C], [B, C], each null where not wanted
+  float* part;                              // [B][chunks][2][C] column sums, or null: no parameter's gradient is wanted
+  int32_t chunks, rows_per;                 // set by the launcher
+  int32_t B, S, C;
+  bool param_f32, vec;
+};
+int norm_grad_chunks(int32_t B, int32_t S);
+hipError_t launch_norm_grad(int dtype, NormGradParams p, hipStream_t stream);
+
+// y [M, N] = x [M, K] w [N, K]^T + bias over codes (kinds MX_FP4, MX_FP8) with scale bytes, or over bf16 values (kind 2).
+constexpr int kLinearBf16 = 2;
+constexpr int64_t kLinearMaxStride = int64_t(1) << 22;  // bytes of a row: 256 rows stay within 32-bit offsets
+struct LinearParams {
+  const uint8_t *x, *xs, *w, *ws;                   // codes or bf16, and scales
+  int32_t x_stride, xs_stride, w_stride, ws_stride;  // bytes
+  View y;                                           // of M / rows batch entries (strides sb, ss)
+  const void* bias;                                 // [N] of y's type, or null
+  int64_t M;
+  int32_t N, K, rows;
+  int32_t parts;   // planes of x that add up to it (fp32 values as three bf16 terms)
+  int64_t x_part;  // bytes from one to the next
+  int32_t tiles_m;  // set by the launcher
+  bool f32, y_vec;  // type of y and bias; rows of y hold whole aligned fours
+};
+hipError_t launch_linear(int x_kind, int w_kind, const LinearParams& p, hipStream_t stream);
+hipError_t launch_linear_split(int dtype, View g, int32_t rows, int64_t M, int32_t N, int32_t ld, void* out,
+                               hipStream_t stream);
+hipError_t launch_linear_transpose(int format, MxView w, int32_t N, int32_t K, int32_t ld, void* out,
+                                   hipStream_t stream);
+int column_sum_chunks(int64_t M, int32_t N);
+hipError_t launch_column_sum(int dtype, View g, int32_t rows, int64_t M, int32_t N, float* part, void* out,
+                             hipStream_t stream);
+
 // Up to two [B, H, n, d] slice pairs whose relative change the diagnostics
 // reduce in one launch; chunks[] is filled by the launcher.
 struct PairSet {

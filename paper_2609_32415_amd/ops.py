@@ -823,6 +823,310 @@ def attn_mx_workspace(q_tgt, n_ref, fmt, qset="target", kvsrc="cache", q_cached=
     return torch.empty(nbytes, dtype=torch.uint8, device=q_tgt.device)
 
 
+# ---- around the attention: the layer norm of the hidden rows and the projections
+
+
+def _rows(name, t, dtype, shape, dev):
+    """(data pointer, batch stride, 0, row stride) of [B, S, C] rows (``shape``; [S, C] has one entry), checked."""
+    if t is None:
+        return _NO_TENSOR
+    if t.get_device() != dev:
+        _elsewhere(name, t, dev)
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} differs from {dtype} {tuple(shape)}")
+    st = t.stride()
+    if st[-1] != 1 and shape[-1] != 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous")
+    if not t.numel():
+        return _NO_TENSOR
+    return t.data_ptr(), st[0] if len(st) == 3 else 0, 0, st[-2]
+
+
+def _batch_rows(name, shape):
+    if len(shape) not in (2, 3):
+        raise ValueError(f"{name} must be [S, C] or [B, S, C], got {tuple(shape)}")
+    return (1, *shape) if len(shape) == 2 else tuple(shape)
+
+
+def _row_words(name, t, dtype, shape, dev):
+    """(data pointer, stride) of a parameter: [C], or one row of C a batch entry."""
+    if t is None:
+        return 0, 0
+    if t.get_device() != dev:
+        _elsewhere(name, t, dev)
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} differs from {dtype} {tuple(shape)}")
+    if t.stride(-1) != 1 and shape[-1] != 1:
+        raise ValueError(f"{name} must be contiguous along the width")
+    return t.data_ptr(), t.stride(0) if len(shape) == 2 and shape[0] > 1 else 0
+
+
+def _norm_desc(x, params, eps, fmt=0):
+    """(packed descriptor, parameters' dtype) of rows like ``x``."""
+    B, S, C = _batch_rows("x", x.shape)
+    dt = x.dtype
+    if dt not in _DTYPES:
+        raise ValueError(f"unsupported dtype {dt}")
+    pdt = next((t.dtype for t in params if t is not None), dt)
+    if pdt != dt and pdt != torch.float32:
+        raise ValueError(f"parameters of {pdt} for rows of {dt}: they are of the rows' dtype or float32")
+    return L.NORM_DESC_PACK.pack(B, S, C, _DTYPES[dt], _DTYPES[pdt], fmt, float(eps)), pdt
+
+
+def _norm(x, weight, bias, scale, shift, eps, y=None, y_mx=None, stats=None):
+    dev, shape = torch._C._cuda_getDevice(), x.shape
+    desc, pdt = _norm_desc(x, (weight, bias, scale, shift), eps, 0 if y_mx is None else _MX[y_mx.fmt])
+    B, S, C = _batch_rows("x", shape)
+    per = (C,) if len(shape) == 2 and scale is not None and scale.dim() == 1 else (B, C)
+    sc, sc_stride = _row_words("scale", scale, pdt, per, dev)
+    per = (C,) if len(shape) == 2 and shift is not None and shift.dim() == 1 else (B, C)
+    sh, sh_stride = _row_words("shift", shift, pdt, per, dev)
+    args = L.NORM_ARGS_PACK.pack(
+        *_rows("x", x, x.dtype, shape, dev), *_rows("out", y, x.dtype, shape, dev),
+        *(_NO_MX if y_mx is None else _mx_words("out", y_mx, y_mx.fmt, (B, 1, S, C), dev)),
+        _row_words("weight", weight, pdt, (C,), dev)[0], _row_words("bias", bias, pdt, (C,), dev)[0], sc, sh,
+        sc_stride, sh_stride, 0 if stats is None else stats.data_ptr())
+    L.refadapt_layer_norm_packed(desc, args, _stream())
+
+
+def layer_norm(x, weight=None, bias=None, *, scale=None, shift=None, eps=1e-6, out=None):
+    """Layer norm of rows ``x`` [B, S, C] or [S, C], through ``refadapt_layer_norm``:
+    (h * weight + bias) * (1 + scale) + shift with h the normalised rows.
+
+    ``weight``, ``bias`` [C] and the modulation ``scale``, ``shift`` [B, C] (for [S, C] rows [C] too; rows of a larger
+    tensor will do) are each optional, and all of ``x``'s dtype or all float32. ``out=x`` works in place.
+
+    Where gradients are recorded and a tensor requires them the result carries them; ``out`` is refused then.
+    """
+    if torch.is_grad_enabled() and (
+            x.requires_grad or weight is not None and weight.requires_grad or bias is not None and bias.requires_grad or
+            scale is not None and scale.requires_grad or shift is not None and shift.requires_grad or
+            out is not None and out.requires_grad):
+        if out is not None:
+            raise ValueError("out cannot be given where a tensor requires grad")
+        return _LayerNorm.apply(x, weight, bias, scale, shift, eps)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _norm(x, weight, bias, scale, shift, eps, y=out)
+    return out
+
+
+class _LayerNorm(torch.autograd.Function):
+    """``layer_norm`` with its gradients (which have none of their own)."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, scale, shift, eps):
+        _on_gpu("x", x)
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        stats = torch.empty((*x.shape[:-1], 2), dtype=torch.float32, device=x.device)
+        _norm(x, weight, bias, scale, shift, eps, y=y, stats=stats)
+        ctx.save_for_backward(x, weight, bias, scale, stats)
+        ctx.eps, ctx.shift = eps, None if shift is None else (shift.shape, shift.dtype)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, weight, bias, scale, stats = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        if dy.stride(-1) != 1 or dy.dim() > 1 and dy.shape[-2] > 1 and dy.stride(-2) < dy.shape[-1]:
+            dy = dy.clone(memory_format=torch.contiguous_format)  # a gradient comes in any layout
+        dx, dw, db, ds, dt = layer_norm_grad(dy, x, stats, weight, bias, scale=scale, eps=ctx.eps, wanted=need[:5],
+                                             param_dtype=None if ctx.shift is None else ctx.shift[1])
+        return (dx, dw, db, None if ds is None else ds.view(scale.shape),
+                None if dt is None else dt.view(ctx.shift[0]), None)
+
+
+def layer_norm_grad(dy, x, stats, weight=None, bias=None, *, scale=None, eps=1e-6, wanted=(True,) * 5,
+                    param_dtype=None, workspace=None):
+    """The gradients of ``layer_norm`` through ``refadapt_layer_norm_grad``: (dx, dweight, dbias, dscale, dshift), None
+    where ``wanted`` says so. ``stats`` [..., 2]: float32 mean and 1 / deviation of each row. Gradients of
+    parameters are of ``param_dtype`` (of the parameters given, or ``x``'s), dscale and dshift [B, C]."""
+    dev, shape, dt = torch._C._cuda_getDevice(), x.shape, x.dtype
+    B, S, C = _batch_rows("x", shape)
+    desc, pdt = _norm_desc(x, (weight, bias, scale), eps)
+    if param_dtype is not None and param_dtype != pdt:
+        if any(t is not None for t in (weight, bias, scale)) or param_dtype != torch.float32:
+            raise ValueError(f"gradients of {param_dtype} for parameters of {pdt}")
+        pdt = param_dtype
+        desc = L.NORM_DESC_PACK.pack(B, S, C, _DTYPES[dt], _DTYPES[pdt], 0, float(eps))
+    _on_gpu("x", x)
+    if stats.dtype != torch.float32 or stats.shape != (*shape[:-1], 2) or not stats.is_contiguous():
+        raise ValueError(f"stats must be contiguous float32 {(*shape[:-1], 2)}")
+    if stats.get_device() != dev:
+        _elsewhere("stats", stats, dev)
+    where = x.device
+    dx = torch.empty(shape, dtype=dt, device=where) if wanted[0] else None
+    sums = [torch.empty(s, dtype=pdt, device=where) if w else None
+            for w, s in zip(wanted[1:], ((C,), (C,), (B, C), (B, C)))]
+    nbytes = 0
+    if any(wanted[1:]):
+        if workspace is None:
+            workspace = torch.empty(L.refadapt_layer_norm_grad_workspace_size_packed(desc), dtype=torch.uint8,
+                                    device=where)
+        elif workspace.get_device() != dev:
+            _elsewhere("workspace", workspace, dev)
+        nbytes = _nbytes(workspace)
+    elif dx is None:
+        return (None,) * 5
+    per = (C,) if len(shape) == 2 and scale is not None and scale.dim() == 1 else (B, C)
+    sc, sc_stride = _row_words("scale", scale, pdt, per, dev)
+    args = L.NORM_GRAD_ARGS_PACK.pack(
+        *_rows("dy", dy, dt, shape, dev), *_rows("x", x, dt, shape, dev), *_rows("dx", dx, dt, shape, dev),
+        stats.data_ptr(), _row_words("weight", weight, pdt, (C,), dev)[0], _row_words("bias", bias, pdt, (C,), dev)[0],
+        sc, sc_stride, *(0 if t is None else t.data_ptr() for t in sums), workspace.data_ptr() if nbytes else 0, nbytes)
+    if B * S or nbytes:
+        L.refadapt_layer_norm_grad_packed(desc, args, _stream())
+    return dx, *sums
+
+
+def layer_norm_mx(x, fmt, weight=None, bias=None, *, scale=None, shift=None, eps=1e-6, out=None):
+    """``layer_norm`` whose result goes out as codes in ``fmt``: the ``MxTensor`` [B, 1, S, C] that quantising the
+    result of ``layer_norm`` gives, bit for bit, in one launch. Carries no gradients."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias, scale, shift)):
+        raise ValueError("codes carry no gradients: use layer_norm and mx_linear, or torch.no_grad()")
+    B, S, C = _batch_rows("x", x.shape)
+    _on_gpu("x", x)
+    if out is None:
+        out = mx_tensor((B, 1, S, C), fmt, x.device)
+    elif out.fmt != fmt:
+        raise ValueError(f"out: format {out.fmt} differs from {fmt}")
+    _norm(x, weight, bias, scale, shift, eps, y_mx=out)
+    return out
+
+
+def mx_weight(w, fmt):
+    """Weights ``w`` [n_out, n_in] quantised along n_in, as the ``MxTensor`` [1, 1, n_out, n_in] that ``mx_linear``
+    takes; n_in a multiple of 32."""
+    if w.dim() != 2:
+        raise ValueError(f"w must be [n_out, n_in], got {tuple(w.shape)}")
+    _on_gpu("w", w)
+    out = mx_tensor((1, 1, *w.shape), fmt, w.device)
+    mx_commit(_readable(w.detach()[None, None]), None, out, None)
+    return out
+
+
+def _linear_desc(B, S, w, dt, fmt):
+    if dt not in _DTYPES:
+        raise ValueError(f"unsupported dtype {dt}")
+    if fmt not in _MX:
+        raise ValueError(f"format must be one of {sorted(_MX)}")
+    one, heads, n_out, n_in = w.shape
+    if one != 1 or heads != 1:
+        raise ValueError(f"w must be an MxTensor [1, 1, n_out, n_in], got {tuple(w.shape)}")
+    return L.LINEAR_DESC_PACK.pack(B, S, n_in, n_out, _DTYPES[dt], _MX[fmt], _MX[_mx_format(w)]), n_out, n_in
+
+
+def _linear_workspace(nbytes, workspace, where, dev):
+    """(words of the workspace, the tensor that holds it)."""
+    if workspace is None:
+        if not nbytes:
+            return (0, 0), None
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=where)
+    elif workspace.get_device() != dev:
+        _elsewhere("workspace", workspace, dev)
+    return (workspace.data_ptr(), _nbytes(workspace)), workspace
+
+
+def mx_linear(x, w, bias=None, *, fmt=None, dtype=None, out=None, workspace=None):
+    """The projection Q(x) w^T + bias through ``refadapt_mx_linear``.
+
+    ``x``: rows [B, S, n_in] or [S, n_in], rounded to codes of ``fmt`` (default: ``w``'s) on the way, or an ``MxTensor``
+    [B, 1, S, n_in] (``layer_norm_mx``), whose result is [B, S, n_out] of ``dtype`` (default: bias's, or bfloat16).
+    ``w``: an ``MxTensor`` [1, 1, n_out, n_in] (``mx_weight``), or rows of one. ``bias`` [n_out] is of the result's
+    dtype. ``out`` may be any rows with contiguous elements, a slice of a larger tensor too.
+
+    Where gradients are recorded and ``x`` or ``bias`` requires them, the result carries them: to ``x`` through the
+    weights' values, its rounding left out. ``out`` is refused then.
+    """
+    if isinstance(x, MxTensor):
+        if bias is not None and torch.is_grad_enabled() and bias.requires_grad:
+            raise ValueError("codes carry no gradients: give mx_linear plain rows, or use torch.no_grad()")
+        B, one, S, K = x.shape
+        if one != 1:
+            raise ValueError(f"x must be an MxTensor [B, 1, S, n_in], got {tuple(x.shape)}")
+        if fmt is not None and fmt != x.fmt:
+            raise ValueError(f"x has format {x.fmt}, not {fmt}")
+        dt = dtype if dtype is not None else bias.dtype if bias is not None else torch.bfloat16
+        return _linear(x, w, bias, _mx_format(x), dt, (B, S, K), (B, S), out, workspace)
+    if dtype is not None and dtype != x.dtype:
+        raise ValueError(f"plain rows of {x.dtype} give a result of that dtype, not {dtype}")
+    fmt = w.fmt if fmt is None else fmt
+    if torch.is_grad_enabled() and (x.requires_grad or bias is not None and bias.requires_grad or
+                                    out is not None and out.requires_grad):
+        if out is not None:
+            raise ValueError("out cannot be given where a tensor requires grad")
+        return _MxLinear.apply(x, w, bias, fmt, workspace)
+    return _linear(x, w, bias, fmt, x.dtype, _batch_rows("x", x.shape), x.shape[:-1], out, workspace)
+
+
+def _linear(x, w, bias, fmt, dt, sizes, lead, out=None, workspace=None):
+    dev = torch._C._cuda_getDevice()
+    B, S, K = sizes
+    desc, n_out, n_in = _linear_desc(B, S, w, dt, fmt)
+    if K != n_in:
+        raise ValueError(f"rows of {K} elements and weights of {n_in}")
+    mx = isinstance(x, MxTensor)
+    where = x.codes.device if mx else x.device
+    if not where.type == "cuda":
+        _on_gpu("x", x.codes if mx else x)
+    if out is None:
+        out = torch.empty((*lead, n_out), dtype=dt, device=where)
+    ws, held = _linear_workspace(L.refadapt_mx_linear_workspace_size_packed(desc, mx), workspace, where, dev)
+    args = L.LINEAR_ARGS_PACK.pack(
+        *(_NO_TENSOR if mx else _rows("x", x, dt, x.shape, dev)),
+        *(_mx_words("x", x, fmt, (B, 1, S, K), dev) if mx else _NO_MX),
+        *_mx_words("w", w, w.fmt, (1, 1, n_out, n_in), dev), _row_words("bias", bias, dt, (n_out,), dev)[0],
+        *_rows("out", out, dt, (*lead, n_out), dev), *ws)
+    L.refadapt_mx_linear_packed(desc, args, _stream())
+    return out
+
+
+class _MxLinear(torch.autograd.Function):
+    """``mx_linear`` with the gradients of its rows and its bias (which have none of their own)."""
+
+    @staticmethod
+    def forward(ctx, x, w, bias, fmt, workspace):
+        ctx.save_for_backward(w.codes, w.scales)
+        ctx.w_fmt, ctx.has_bias = w.fmt, bias is not None
+        return _linear(x, w, bias, fmt, x.dtype, _batch_rows("x", x.shape), x.shape[:-1], None, workspace)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        w = MxTensor(*ctx.saved_tensors, ctx.w_fmt)
+        dx, db = mx_linear_grad(dy, w, wanted=(ctx.needs_input_grad[0], ctx.has_bias and ctx.needs_input_grad[2]))
+        return dx, None, db, None, None
+
+
+def mx_linear_grad(dy, w, *, wanted=(True, True), workspace=None):
+    """The gradients of ``mx_linear`` through ``refadapt_mx_linear_grad``: (dx, dbias) of ``dy`` [B, S, n_out] or
+    [S, n_out], None where ``wanted`` says so."""
+    dev, shape, dt = torch._C._cuda_getDevice(), dy.shape, dy.dtype
+    B, S, N = _batch_rows("dy", shape)
+    desc, n_out, n_in = _linear_desc(B, S, w, dt, w.fmt)
+    if N != n_out:
+        raise ValueError(f"gradients of {N} outputs and weights of {n_out}")
+    if not any(wanted):
+        return None, None
+    _on_gpu("dy", dy)
+    st, whole = dy.stride(), n_out % 8 == 0 and dt == torch.bfloat16
+    if st[-1] != 1 or S > 1 and st[-2] < N or whole and (
+            dy.data_ptr() % 16 or any(s % 8 for s in st[:-1]) or len(st) == 3 and B > 1 and S > 1 and st[0] != S * st[1]):
+        dy = dy.clone(memory_format=torch.contiguous_format)  # a gradient comes in any layout
+    where = dy.device
+    dx = torch.empty((*shape[:-1], n_in), dtype=dt, device=where) if wanted[0] else None
+    db = torch.empty((n_out,), dtype=dt, device=where) if wanted[1] else None
+    ws, held = _linear_workspace(L.refadapt_mx_linear_grad_workspace_size_packed(desc), workspace, where, dev)
+    args = L.LINEAR_GRAD_ARGS_PACK.pack(
+        *_rows("dy", dy, dt, shape, dev), *_mx_words("w", w, w.fmt, (1, 1, n_out, n_in), dev),
+        *(_NO_TENSOR if dx is None else _rows("dx", dx, dt, (*shape[:-1], n_in), dev)),
+        0 if db is None else db.data_ptr(), *ws)
+    if B * S or db is not None:
+        L.refadapt_mx_linear_grad_packed(desc, args, _stream())
+    return dx, db
+
+
 def mfma_rate_probe(kind, operands, steps, workgroups=None, sink=None, clock_probe=None):
     """Runs ``refadapt_mfma_rate_probe`` (``kind`` "dense" or "mix") on the current stream and
     returns the sink. ``operands``: a device tensor of at least ``RA_PROBE_OPERAND_BYTES``
