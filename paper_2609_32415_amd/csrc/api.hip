@@ -1058,18 +1058,26 @@ ra_status check_weights(const char* who, const ra_linear_desc& d, const ra_mx_te
 bool linear_by_values(const ra_linear_desc& d) {
   return d.dtype == RA_F32 && (d.x_format == RA_MXFP8 || d.w_format == RA_MXFP8);
 }
+// Few rows are rounded by the product's own launch.
+bool linear_takes_plain(const ra_linear_desc& d) {
+  return !linear_by_values(d) && linear_is_few(d.x_format, (int64_t)d.batch * d.rows, d.n_out, d.n_in);
+}
+// Scale rows that do not start at whole words are copied: where a row is not in whole words, room for that is asked for.
+bool in_words(const ra_mx_tensor& t, int64_t row) {
+  return (reinterpret_cast<uintptr_t>(t.scales) & 3) == 0 && (row & 3) == 0;
+}
 struct LinearSpace {
-  size_t x_codes, x_scales, x_values, w_values;
-  size_t total() const { return x_codes + x_scales + x_values + w_values; }
+  size_t x_codes, x_scales, w_scales, x_values, w_values;
+  size_t total() const { return x_codes + x_scales + w_scales + x_values + w_values; }
 };
 LinearSpace linear_space(const ra_linear_desc& d, bool x_mx) {
   const size_t M = (size_t)d.batch * d.rows;
   LinearSpace s{};
-  if (!x_mx) {
-    s.x_codes = padded(M * mx_row(d.x_format, d.n_in));
-    s.x_scales = padded(M * mx_scale_row(d.n_in));
-  }
-  if (linear_by_values(d)) {
+  const bool values = linear_by_values(d), odd = d.n_in % 128 != 0, round = !x_mx && !linear_takes_plain(d);
+  if (round) s.x_codes = padded(M * mx_row(d.x_format, d.n_in));
+  if (round || (x_mx && odd && !values)) s.x_scales = padded(M * mx_scale_row(d.n_in));
+  if (odd && !values) s.w_scales = padded((size_t)d.n_out * mx_scale_row(d.n_in));
+  if (values) {
     s.x_values = padded(M * d.n_in * 2);
     s.w_values = padded((size_t)d.n_out * d.n_in * 2);
   }
@@ -1103,11 +1111,18 @@ int64_t even_stride(int32_t batch, int32_t rows, int64_t sb, int64_t ss) {
   return batch == 1 || sb == rows * ss ? ss : -1;
 }
 
-void set_y(LinearParams* p, const ra_tensor& y, int dtype) {
+void set_y(LinearParams* p, const ra_tensor& y, const ra_linear_desc& d) {
+  const int32_t dtype = d.dtype;
+  const int64_t even = even_stride(d.batch, d.rows, y.stride_b, y.stride_s);
+  p->M = (int64_t)d.batch * d.rows;
   p->y = view(y);
+  p->rows = d.rows;
+  if (even >= 0) {
+    p->rows = (int32_t)p->M;
+    p->y.ss = even;
+  }
   p->f32 = dtype == RA_F32;
-  p->y_vec = reinterpret_cast<uintptr_t>(y.data) % (dtype == RA_F32 ? 16 : 8) == 0 && y.stride_b % 4 == 0 &&
-             y.stride_s % 4 == 0;
+  p->y_vec = in_units(y, dtype);
 }
 
 }  // namespace
@@ -1153,7 +1168,8 @@ ra_status refadapt_mx_linear(const ra_linear_desc* desc, const ra_linear_args* a
   MxView x = mx_view(a.x_mx);
   x.sh = x.eh = 0;
   hipError_t e;
-  if (!x_mx) {
+  const bool rounds = !x_mx && linear_takes_plain(d);
+  if (!x_mx && !rounds) {
     x = MxView{ws, x_row * d.rows, 0, x_row, ws + space.x_codes, xs_row * d.rows, 0, xs_row};
     MxSet set{};
     set.n = 1;
@@ -1164,15 +1180,13 @@ ra_status refadapt_mx_linear(const ra_linear_desc* desc, const ra_linear_args* a
     if (e != hipSuccess) return launch_status(e, who);
   }
   LinearParams p{};
-  p.M = (int64_t)d.batch * d.rows;
+  set_y(&p, a.y, d);
   p.N = d.n_out;
   p.K = d.n_in;
-  p.rows = d.rows;
   p.parts = 1;
   p.bias = a.bias;
-  set_y(&p, a.y, d.dtype);
   if (values) {
-    uint8_t* const xv = ws + space.x_codes + space.x_scales;
+    uint8_t* const xv = ws + space.x_codes + space.x_scales + space.w_scales;
     uint8_t* const wv = xv + space.x_values;
     MxSet set{};
     set.n = 1;
@@ -1191,12 +1205,32 @@ ra_status refadapt_mx_linear(const ra_linear_desc* desc, const ra_linear_args* a
   }
   p.x = x.codes;
   p.xs = x.scales;
+  if (rounds) {
+    p.x_plain = view(a.x);
+    p.x_rows = d.rows;
+    p.x_f32 = d.dtype == RA_F32;
+  }
   p.x_stride = (int32_t)x_row;
   p.xs_stride = (int32_t)xs_row;
   p.w = static_cast<const uint8_t*>(a.w.codes);
   p.ws = static_cast<const uint8_t*>(a.w.scales);
-  p.w_stride = (int32_t)a.w.stride_s;
-  p.ws_stride = (int32_t)a.w.scale_stride_s;
+  p.w_stride = d.n_out > 1 ? (int32_t)a.w.stride_s : 0;  // a single row's stride may be anything
+  p.ws_stride = d.n_out > 1 ? (int32_t)a.w.scale_stride_s : 0;
+  const int32_t row = (int32_t)mx_scale_row(d.n_in);
+  if (x_mx && !in_words(a.x_mx, xs_row) && !linear_is_few(d.x_format, p.M, d.n_out, d.n_in)) {
+    uint8_t* const to = ws + space.x_codes;
+    e = launch_scale_rows(x.scales, x.es, x.eb, d.rows, p.M, d.n_in / 32, row / 4, to, st);
+    if (e != hipSuccess) return launch_status(e, who);
+    p.xs = to;
+    p.xs_stride = row;
+  }
+  if (!in_words(a.w, p.ws_stride)) {
+    uint8_t* const to = ws + space.x_codes + space.x_scales;
+    e = launch_scale_rows(p.ws, p.ws_stride, 0, d.n_out, d.n_out, d.n_in / 32, row / 4, to, st);
+    if (e != hipSuccess) return launch_status(e, who);
+    p.ws = to;
+    p.ws_stride = row;
+  }
   return launch_status(launch_linear(d.x_format, d.w_format, p, st), who);
 }
 
@@ -1241,12 +1275,10 @@ ra_status refadapt_mx_linear_grad(const ra_linear_desc* desc, const ra_linear_gr
                           reinterpret_cast<float*>(ws + space.dy + space.w), a.dbias, st);
   if (e != hipSuccess || a.dx.data == nullptr || M == 0) return launch_status(e, who);
   LinearParams p{};
-  p.M = M;
+  set_y(&p, a.dx, d);
   p.N = d.n_in;
   p.K = ld;
-  p.rows = d.rows;
   p.parts = d.dtype == RA_F32 ? 3 : 1;
-  set_y(&p, a.dx, d.dtype);
   e = launch_linear_transpose(d.w_format, mx_view(a.w), d.n_out, d.n_in, ld, ws + space.dy, st);
   if (e != hipSuccess) return launch_status(e, who);
   p.w = ws + space.dy;

@@ -209,17 +209,25 @@ constexpr int kLinearBf16 = 2;
 constexpr int64_t kLinearMaxStride = int64_t(1) << 22;  // bytes of a row: 256 rows stay within 32-bit offsets
 struct LinearParams {
   const uint8_t *x, *xs, *w, *ws;                   // codes or bf16, and scales
-  int32_t x_stride, xs_stride, w_stride, ws_stride;  // bytes
-  View y;                                           // of M / rows batch entries (strides sb, ss)
+  int32_t x_stride, xs_stride, w_stride, ws_stride;  // bytes; the scales' in whole words
+  View y;                                           // of M / rows batch entries (strides sb, ss), or rows = M
   const void* bias;                                 // [N] of y's type, or null
   int64_t M;
   int32_t N, K, rows;
   int32_t parts;   // planes of x that add up to it (fp32 values as three bf16 terms)
   int64_t x_part;  // bytes from one to the next
   int32_t tiles_m;  // set by the launcher
-  bool f32, y_vec;  // type of y and bias; rows of y hold whole aligned fours
+  View x_plain;     // rows that the kernel for few rows rounds itself (batch entries of x_rows), or null p: x and xs
+  int32_t x_rows;
+  bool x_f32;
+  bool f32, y_vec;  // type of y and bias; rows of y start at 16-byte units
 };
+// Whether launch_linear takes plain rows too (x_plain), which it rounds to codes on the way.
+bool linear_is_few(int x_kind, int64_t M, int32_t N, int32_t K);
 hipError_t launch_linear(int x_kind, int w_kind, const LinearParams& p, hipStream_t stream);
+// M rows of n scale bytes (batch stride sb, row stride stride) to rows of `words` words, zeros behind them.
+hipError_t launch_scale_rows(const uint8_t* in, int64_t stride, int64_t sb, int32_t rows, int64_t M, int32_t n,
+                             int32_t words, void* out, hipStream_t stream);
 hipError_t launch_linear_split(int dtype, View g, int32_t rows, int64_t M, int32_t N, int32_t ld, void* out,
                                hipStream_t stream);
 hipError_t launch_linear_transpose(int format, MxView w, int32_t N, int32_t K, int32_t ld, void* out,

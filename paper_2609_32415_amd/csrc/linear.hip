@@ -11,6 +11,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "internal.h"
 #include "mxcodes.h"
@@ -59,14 +60,13 @@ struct Operand {
   __amdgpu_buffer_rsrc_t rs;
   uint32_t voff[2];    // of even and of odd instructions: their chunks are swizzled differently
   int chunk[2];
-  int stride, bytes;   // of a row
+  uint32_t soff[NI];
+  int bytes;           // of a row
   int first;           // of this wavefront
 
-  __device__ __forceinline__ void start(const uint8_t* base, int64_t row0, int rows, int row_stride, int k, int wave,
+  __device__ __forceinline__ void start(const uint8_t* base, int64_t row0, int valid, int row_stride, int k, int wave,
                                         int lane) {
-    stride = row_stride;
     bytes = row_bytes<KIND>(k);
-    const int valid = min(ROWS, rows);
     rs = rsrc(base + row0 * row_stride, (int64_t)(valid - 1) * row_stride + bytes);
     first = wave * NI;
 #pragma unroll
@@ -75,74 +75,50 @@ struct Operand {
       chunk[i] = 16 * ((lane % NC) ^ swizzle<NC>(row));
       voff[i] = (uint32_t)(lane / NC * row_stride + chunk[i]);
     }
+#pragma unroll
+    for (int i = 0; i < NI; ++i) soff[i] = __builtin_amdgcn_readfirstlane((uint32_t)((first + i) * RPI * row_stride));
   }
-  // k0: bytes of a row ahead of the stage; past a row's end the chunks read as zeros
-  __device__ __forceinline__ void load(uint8_t* lds, int k0) const {
-    const uint32_t v[2] = {chunk[0] < bytes - k0 ? voff[0] : OUTSIDE, chunk[1] < bytes - k0 ? voff[1] : OUTSIDE};
+  // k0: bytes of a row ahead of the stage; past a row's end, and of no stage, the chunks read as zeros
+  __device__ __forceinline__ void load(uint8_t* lds, int k0, bool any) const {
+    const int left = any ? bytes - k0 : 0;
+    const uint32_t v[2] = {chunk[0] < left ? voff[0] : OUTSIDE, chunk[1] < left ? voff[1] : OUTSIDE};
 #pragma unroll
     for (int i = 0; i < NI; ++i)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          rs, (__attribute__((address_space(3))) void*)(lds + (first + i) * 1024), 16, v[i & 1],
-          __builtin_amdgcn_readfirstlane((first + i) * RPI * stride + k0), 0, 0);
+          rs, (__attribute__((address_space(3))) void*)(lds + (first + i) * 1024), 16, v[i & 1], soff[i] + k0, 0, 0);
   }
 };
 
-// The scale bytes of the rows of NB blocks of 32 rows: KD / 32 bytes a stage and row, read as aligned words (two where
-// rows of scales are not in whole words).
-template <int NB, int ND>
-struct Scales {
-  uint32_t lo[NB][ND], hi[NB];
-};
+// The scale bytes of its rows go to LDS for two stages at a time: 16 bytes a row (of which stages of 128 elements use the
+// first 8), 64 rows an instruction. Rows of scales start at whole words (the host has others copied).
 struct ScaleRows {
   __amdgpu_buffer_rsrc_t rs;
-  uint32_t voff;  // of this lane's row in block 0, a whole word's
-  int shift;      // bytes past it (0 to 3): stride and block offsets keep it where `odd` is false
-  int stride, bytes;
-  bool odd;
-  uint32_t base_off, lane_row;
-
-  __device__ __forceinline__ void start(const uint8_t* base, int64_t row0, int rows, int tile_rows, int row_stride,
-                                        int k, int lane) {
-    const uint8_t* p = base + row0 * row_stride;
-    base_off = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 3);
-    bytes = k / 32;
-    stride = row_stride;
-    odd = base_off != 0 || (row_stride & 3) != 0 || (bytes & 3) != 0;
-    rs = rsrc(p - base_off, ((int64_t)(min(rows, tile_rows) - 1) * row_stride + bytes + base_off + 3) & ~int64_t(3));
-    lane_row = (uint32_t)(lane & 31);
+  uint32_t voff;
+  __device__ __forceinline__ void none() {  // a wavefront without rows
+    rs = rsrc(nullptr, 0);
+    voff = OUTSIDE;
   }
-  template <int NB, int ND>
-  __device__ __forceinline__ void load(Scales<NB, ND>& s, int block0, int k0) const {
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const uint32_t at = base_off + (uint32_t)((block0 + b) * 32 + lane_row) * stride + k0;
-#pragma unroll
-      for (int d = 0; d < ND; ++d)
-        s.lo[b][d] = __builtin_amdgcn_raw_buffer_load_b32(rs, (at & ~3u) + 4 * d, 0, 0);
-      s.hi[b] = odd ? __builtin_amdgcn_raw_buffer_load_b32(rs, (at & ~3u) + 4 * ND, 0, 0) : 0u;
-    }
+  __device__ __forceinline__ void start(const uint8_t* base, int64_t row0, int valid, int row_stride, int k, int row,
+                                        int lane) {
+    rs = rsrc(base + row0 * row_stride, (int64_t)(valid - 1) * row_stride + ((k / 32 + 3) & ~3));  // in whole words
+    voff = (uint32_t)((row + lane) * row_stride);
   }
-  // Word d of a block's stage with this lane half's bytes in 0 and 2; bytes past the row's end are zeros (they meet
-  // zero codes, and a byte of 255 there would make NaN of them).
-  template <int NB, int ND>
-  __device__ __forceinline__ uint32_t word(const Scales<NB, ND>& s, int block0, int b, int d, int k0, int half) const {
-    uint32_t v = s.lo[b][d];
-    if (odd) {
-      const uint32_t at = base_off + (uint32_t)((block0 + b) * 32 + lane_row) * stride + k0;
-      v = __builtin_amdgcn_alignbyte(d + 1 < ND ? s.lo[b][d + 1 < ND ? d + 1 : d] : s.hi[b], v, at & 3);
-      const int left = bytes - k0 - 4 * d;
-      if (left < 4) v = left > 0 ? v & ((1u << (8 * left)) - 1) : 0u;
-    } else if (bytes - k0 <= 4 * d) {
-      v = 0u;
-    }
-    return v >> (8 * half);
+  __device__ __forceinline__ void load(uint8_t* lds, int k0) const {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)lds, 16, voff, k0, 0, 0);
   }
 };
 
-template <int KIND, int RB>
+// Every wavefront's loads into LDS have arrived and its reads are done. (The barrier alone waits for the loads that this
+// wavefront reads itself, where the compiler sees such reads.)
+__device__ __forceinline__ void all_arrived() {
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+  __syncthreads();
+}
+
+template <int KIND>
 __device__ __forceinline__ i32x8 operand(const uint8_t* lds, uint32_t at, int step) {
   i32x8 r = {};
-  if constexpr (KIND == FP4) {
+  if constexpr (KIND != FP8) {  // the upper half is not read
     const i32x4 a = *reinterpret_cast<const i32x4*>(lds + (at ^ (step * 32)));
 #pragma unroll
     for (int i = 0; i < 4; ++i) r[i] = a[i];
@@ -158,6 +134,10 @@ __device__ __forceinline__ i32x8 operand(const uint8_t* lds, uint32_t at, int st
   return r;
 }
 
+__device__ __forceinline__ bf16x8 first_half(const i32x8& v) {
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v, v, 0, 1, 2, 3));
+}
+
 // BM rows x BN outputs a workgroup of WM x WN wavefronts.
 template <int KX, int KW, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearParams p) {
@@ -166,152 +146,423 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearParams p) {
   using X = Operand<KX, KD, BM, NW>;
   using W = Operand<KW, KD, BN, NW>;
   constexpr bool SCALED = KX != B16;
-  constexpr int ND = SCALED ? KD / 128 : 1;
+  constexpr int ND = KD / 128;  // scale words of a row and stage
+  constexpr int NS = (BM / 64 + BN / 64 + NW - 1) / NW;  // scale loads of a wavefront
   // separate arrays, so that a stage's loads are not waited for before the other stage's reads
-  __shared__ __attribute__((aligned(1024))) uint8_t x0[BM * X::RB], x1[BM * X::RB], w0[BN * W::RB], w1[BN * W::RB];
+  __shared__ __attribute__((aligned(1024))) uint8_t x0[BM * X::RB], x1[BM * X::RB],
+      w0[BN * W::RB > 4096 * NW ? BN * W::RB : 4096 * NW], w1[BN * W::RB];
+  __shared__ __attribute__((aligned(1024))) uint8_t scales[SCALED ? 2 * 1024 * NW * NS : 16];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5, r = lane & 31;
   const int tile = xcd_remap(blockIdx.x, gridDim.x);
   const int tn = tile / p.tiles_m, tm = tile - tn * p.tiles_m;
   const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+  const int rows = (int)min((int64_t)BM, p.M - m0), cols = (int)min((int64_t)BN, p.N - n0);
   const int wm = wave / WN, wn = wave % WN;
 
   X xo;
   W wo;
-  xo.start(p.x, m0, (int)min((int64_t)BM, p.M - m0), p.x_stride, p.K, wave, lane);
-  wo.start(p.w, n0, (int)min((int64_t)BN, p.N - n0), p.w_stride, p.K, wave, lane);
-  ScaleRows xr, wr;
-  if constexpr (SCALED) {
-    xr.start(p.xs, m0, (int)min((int64_t)BM, p.M - m0), BM, p.xs_stride, p.K, lane);
-    wr.start(p.ws, n0, (int)min((int64_t)BN, p.N - n0), BN, p.ws_stride, p.K, lane);
+  xo.start(p.x, m0, rows, p.x_stride, p.K, wave, lane);
+  wo.start(p.w, n0, cols, p.w_stride, p.K, wave, lane);
+  ScaleRows so[NS];
+  if constexpr (SCALED) {  // 64 rows each: first those of x, then those of w
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      const int q = wave * NS + i;
+      if (q < BM / 64)
+        so[i].start(p.xs, m0, rows, p.xs_stride, p.K, 64 * q, lane);
+      else if (q < BM / 64 + BN / 64)
+        so[i].start(p.ws, n0, cols, p.ws_stride, p.K, 64 * (q - BM / 64), lane);
+      else
+        so[i].none();
+    }
   }
   f32x16 acc[NB][MB] = {};
   const int per = (p.K + KD - 1) / KD, stages = per * p.parts;
-  Scales<MB, ND> xs0, xs1;
-  Scales<NB, ND> ws0, ws1;
-  int next = 0, part = 0;  // the stage of its part that is loaded next
-  const auto load = [&](uint8_t* xl, uint8_t* wl, Scales<MB, ND>& xs, Scales<NB, ND>& ws) {
-    xo.load(xl, next * X::RB);
-    wo.load(wl, next * W::RB);
+  int next = 0, loaded = 0;  // the stage that is loaded next, within its part and of all
+  const uint8_t* xbase = p.x + m0 * p.x_stride;
+  // Without branches: across one the compiler moves matrix instructions behind the next barrier.
+  const auto load = [&](uint8_t* xl, uint8_t* wl, bool even) {
+    const bool any = loaded < stages;
+    xo.load(xl, next * X::RB, any);
+    wo.load(wl, next * W::RB, any);
     if constexpr (SCALED) {
-      xr.load(xs, wm * MB, next * (KD / 32));
-      wr.load(ws, wn * NB, next * (KD / 32));
+      if (even) {
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+          so[i].load(scales + ((next & 2) * 512 * NW + 1024 * wave) * NS + 1024 * i, any ? next * (KD / 32) : 0);
+      }
     }
-    if (++next == per && ++part < p.parts) {
-      next = 0;
-      xo.start(p.x + part * p.x_part, m0, (int)min((int64_t)BM, p.M - m0), p.x_stride, p.K, wave, lane);
+    ++loaded;
+    const bool wrap = ++next == per;
+    if constexpr (!SCALED) {  // on to the next plane of x
+      xbase += wrap ? p.x_part : 0;
+      next = wrap ? 0 : next;
+      xo.rs = rsrc(xbase, (int64_t)(rows - 1) * p.x_stride + xo.bytes);
     }
   };
-  // where this lane's operands lie
+  // where this lane's operands and scales lie
   const uint32_t xat = (wm * MB * 32 + r) * X::RB + 16 * (half ^ swizzle<X::NC>(r));
   const uint32_t wat = (wn * NB * 32 + r) * W::RB + 16 * (half ^ swizzle<W::NC>(r));
-  const auto compute = [&](const uint8_t* xl, const uint8_t* wl, const Scales<MB, ND>& xs, const Scales<NB, ND>& ws,
-                           int stage) {
+  const uint8_t* const xsat = scales + 16 * (wm * MB * 32 + r);
+  const uint8_t* const wsat = scales + 16 * (BM + wn * NB * 32 + r);
+  // Loads the next stage once this one's scale words have been read, and forms this one's products.
+  const auto stage = [&](const uint8_t* xl, const uint8_t* wl, uint8_t* xn, uint8_t* wn_, int s, bool even) {
+    uint32_t xe[MB][ND], we[NB][ND];
     if constexpr (SCALED) {
-      const int k0 = stage * (KD / 32);
+      const int at = (s & 2) * 512 * NW * NS + (even ? 0 : 4 * ND);
 #pragma unroll
       for (int d = 0; d < ND; ++d) {
-        uint32_t xe[MB], we[NB];
-#pragma unroll
-        for (int b = 0; b < MB; ++b) xe[b] = xr.word(xs, wm * MB, b, d, k0, half);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) we[b] = wr.word(ws, wn * NB, b, d, k0, half);
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          i32x8 xv[MB], wv[NB];
-#pragma unroll
-          for (int b = 0; b < MB; ++b) xv[b] = operand<KX, X::RB>(xl + b * 32 * X::RB, xat, 2 * d + t);
-#pragma unroll
-          for (int b = 0; b < NB; ++b) wv[b] = operand<KW, W::RB>(wl + b * 32 * W::RB, wat, 2 * d + t);
-#pragma unroll
-          for (int i = 0; i < NB; ++i)
-#pragma unroll
-            for (int j = 0; j < MB; ++j) {
-              constexpr int FW = KW == FP4 ? 4 : 0, FX = KX == FP4 ? 4 : 0;
-              acc[i][j] = t == 0 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wv[i], xv[j], acc[i][j], FW, FX, 0,
-                                                                                   we[i], 0, xe[j])
-                                 : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wv[i], xv[j], acc[i][j], FW, FX, 2,
-                                                                                   we[i], 2, xe[j]);
-            }
-        }
-      }
-    } else {
-#pragma unroll
-      for (int t = 0; t < KD / 16; ++t) {
-        bf16x8 xv[MB], wv[NB];
+        // bytes past the end of K meet zero codes, but 255 would make NaN of them
+        const int left = p.K / 32 - s * (KD / 32) - 4 * d;
+        const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
 #pragma unroll
         for (int b = 0; b < MB; ++b)
-          xv[b] = *reinterpret_cast<const bf16x8*>(xl + b * 32 * X::RB + (xat ^ (t * 32)));
+          xe[b][d] = (*reinterpret_cast<const uint32_t*>(xsat + at + 512 * b + 4 * d) & keep) >> (8 * half);
 #pragma unroll
         for (int b = 0; b < NB; ++b)
-          wv[b] = *reinterpret_cast<const bf16x8*>(wl + b * 32 * W::RB + (wat ^ (t * 32)));
-#pragma unroll
-        for (int i = 0; i < NB; ++i)
-#pragma unroll
-          for (int j = 0; j < MB; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wv[i], xv[j], acc[i][j], 0, 0, 0);
+          we[b][d] = (*reinterpret_cast<const uint32_t*>(wsat + at + 512 * b + 4 * d) & keep) >> (8 * half);
       }
+    }
+    load(xn, wn_, !even);
+#pragma unroll
+    for (int t = 0; t < (SCALED ? 2 * ND : KD / 16); ++t) {
+      i32x8 xv[MB], wv[NB];
+#pragma unroll
+      for (int b = 0; b < MB; ++b) xv[b] = operand<KX>(xl + b * 32 * X::RB, xat, t);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) wv[b] = operand<KW>(wl + b * 32 * W::RB, wat, t);
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int j = 0; j < MB; ++j) {
+          if constexpr (SCALED) {
+            constexpr int FW = KW == FP4 ? 4 : 0, FX = KX == FP4 ? 4 : 0;
+            acc[i][j] = t % 2 == 0 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                                         wv[i], xv[j], acc[i][j], FW, FX, 0, we[i][t / 2 % ND], 0, xe[j][t / 2 % ND])
+                                   : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                                         wv[i], xv[j], acc[i][j], FW, FX, 2, we[i][t / 2 % ND], 2, xe[j][t / 2 % ND]);
+          } else {
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(first_half(wv[i]), first_half(xv[j]), acc[i][j], 0, 0, 0);
+          }
+        }
+      __builtin_amdgcn_sched_barrier(0);  // operands of one step at a time: those of all would not fit in registers
     }
   };
 
-  load(x0, w0, xs0, ws0);
-  for (int s = 0; s < stages; s += 2) {
-    __syncthreads();  // stage s has arrived, and every wavefront is done with the stage before it
-    if (s + 1 < stages) load(x1, w1, xs1, ws1);
-    compute(x0, w0, xs0, ws0, s);
-    if (s + 1 >= stages) break;
-    __syncthreads();
-    if (s + 2 < stages) load(x0, w0, xs0, ws0);
-    compute(x1, w1, xs1, ws1, s + 1);
+  load(x0, w0, true);
+  int s = 0;
+  for (; s + 1 < stages; s += 2) {
+    all_arrived();  // stage s is there, and every wavefront is done with the stage before it
+    stage(x0, w0, x1, w1, s, true);
+    all_arrived();
+    stage(x1, w1, x0, w0, s + 1, false);
+  }
+  if (s < stages) {
+    all_arrived();
+    stage(x0, w0, x1, w1, s, true);
   }
 
-  // a lane's column of a block is a row of y, its registers 4 g .. 4 g + 3 outputs 8 g + 4 half .. + 3
-#pragma unroll
-  for (int j = 0; j < MB; ++j) {
-    const int64_t m = m0 + (wm * MB + j) * 32 + r;
-    if (m >= p.M) continue;
-    const int64_t b = m / p.rows, at = b * p.y.sb + (m - b * p.rows) * p.y.ss;
+  // A lane's column of a block is a row of y, its registers 4 g .. 4 g + 3 outputs 8 g + 4 half .. + 3: written as they
+  // are, 16 bytes of a line at a time, they took as long as the products. Each wavefront puts 32 rows of 128 bytes into
+  // LDS (16-byte chunks swizzled as above) and stores whole lines.
+  all_arrived();
+  uint8_t* const mine = w0 + 4096 * wave;
+  const int64_t nw = n0 + wn * NB * 32;
+  f32x4 add[NB][4] = {};
+  if (p.bias) {
 #pragma unroll
     for (int i = 0; i < NB; ++i)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int64_t n = n0 + (wn * NB + i) * 32 + 8 * g + 4 * half;
-        if (n >= p.N) continue;
-        const int count = (int)min((int64_t)4, p.N - n);
-        f32x4 v;
+      for (int g = 0; g < 4; ++g)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * g + e];
-        if (p.bias) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (e < count)
-              v[e] += p.f32 ? static_cast<const float*>(p.bias)[n + e]
-                            : __uint_as_float((uint32_t) static_cast<const uint16_t*>(p.bias)[n + e] << 16);
+        for (int e = 0; e < 4; ++e) {
+          const int64_t n = nw + 32 * i + 8 * g + 4 * half + e;
+          if (n < p.N)
+            add[i][g][e] = p.f32 ? static_cast<const float*>(p.bias)[n]
+                                 : __uint_as_float((uint32_t) static_cast<const uint16_t*>(p.bias)[n] << 16);
         }
-        if (p.f32) {
-          float* y = static_cast<float*>(const_cast<void*>(p.y.p)) + at + n;
-          if (p.y_vec && count == 4) {
-            *reinterpret_cast<f32x4*>(y) = v;
-          } else {
+  }
+  // 8 rows of `mine` a round: lane / 8 of them, chunk lane % 8 of its row, `per_chunk` outputs from n on
+  const auto put = [&](int j, int64_t n_first, auto* y, int per_chunk) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (e < count) y[e] = v[e];
-          }
-        } else {
-          uint16_t* y = static_cast<uint16_t*>(const_cast<void*>(p.y.p)) + at + n;
-          uint16_t h[4];
+    for (int q = 0; q < 4; ++q) {
+      const int row = 8 * q + lane / 8;
+      const u32x4 v = *reinterpret_cast<const u32x4*>(mine + 128 * row + 16 * (lane % 8));
+      const int64_t m = m0 + (wm * MB + j) * 32 + row, n = n_first + per_chunk * ((lane % 8) ^ swizzle<8>(row));
+      if (m >= p.M || n >= p.N) continue;
+      int64_t at = m * p.y.ss;
+      if (p.rows < p.M) {  // rows of several batch entries that are not evenly spaced
+        const uint32_t b = (uint32_t)m / (uint32_t)p.rows;
+        at = b * p.y.sb + ((uint32_t)m - b * (uint32_t)p.rows) * p.y.ss;
+      }
+      auto* const to = y + at + n;
+      if (p.y_vec && n + per_chunk <= p.N) {
+        *reinterpret_cast<u32x4*>(to) = v;
+      } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) h[e] = __builtin_bit_cast(uint16_t, (__bf16)v[e]);
-          if (p.y_vec && count == 4) {
-            *reinterpret_cast<u32x2*>(y) = u32x2{h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16};
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (e < count) y[e] = h[e];
-          }
+        for (int e = 0; e < 8; ++e) {
+          if (e >= per_chunk || n + e >= p.N) break;
+          if constexpr (sizeof(*to) == 4)
+            to[e] = __uint_as_float(v[e & 3]);
+          else
+            to[e] = (uint16_t)(v[e / 2] >> (16 * (e & 1)));
         }
       }
+    }
+  };
+  static_assert(NB % 2 == 0, "rows of 64 outputs");
+#pragma unroll
+  for (int j = 0; j < MB; ++j) {
+    if (p.f32) {
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          f32x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * g + e] + add[i][g][e];
+          *reinterpret_cast<f32x4*>(mine + 128 * r + 16 * ((2 * g + half) ^ swizzle<8>(r))) = v;
+        }
+        put(j, nw + 32 * i, static_cast<float*>(const_cast<void*>(p.y.p)), 4);
+      }
+    } else {
+#pragma unroll
+      for (int pair = 0; pair < NB / 2; ++pair) {
+#pragma unroll
+        for (int o = 0; o < 2; ++o)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int i = 2 * pair + o;
+            uint32_t h[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              h[e] = __builtin_bit_cast(uint16_t, (__bf16)(acc[i][j][4 * g + e] + add[i][g][e]));
+            *reinterpret_cast<u32x2*>(mine + 128 * r + 16 * ((4 * o + g) ^ swizzle<8>(r)) + 8 * half) =
+                u32x2{h[0] | h[1] << 16, h[2] | h[3] << 16};
+          }
+        put(j, nw + 64 * pair, static_cast<uint16_t*>(const_cast<void*>(p.y.p)), 8);
+      }
+    }
+  }
+}
+
+// ---- few rows
+
+// Rows of x that the kernel for few rows reads: codes, or plain rows that it rounds itself.
+enum { X_CODES = 0, X_BF16 = 1, X_F32 = 2 };
+constexpr int FEW_WAVES = 8, FEW_ROWS = 32;
+constexpr int FEW_LDS = 65536, FEW_MORE_LDS = 131072;  // two workgroups a CU, or one
+
+// A row's codes and scale bytes in LDS, 16 bytes apart from the next (rows of whole kilobytes would share banks).
+template <int KX>
+__host__ __device__ constexpr int64_t few_pitch(int64_t K) {
+  return row_bytes<KX>((int)K) + 16;
+}
+__host__ __device__ constexpr int64_t few_scale_pitch(int64_t K) { return (K / 32 + 3) & ~int64_t(3); }
+
+// The rows of x as codes into LDS, a batch of pieces after the other: a wavefront works on a row, or several do where there
+// are fewer than 8 rows. A piece is 16 bytes of codes, or 8 elements that become codes.
+template <int KX, int XP>
+struct RowsIn {
+  static constexpr int THREADS = 64 * FEW_WAVES, UNROLL = 4;  // pieces of a thread in flight
+  static constexpr bool PLAIN = XP != X_CODES, BF = XP != X_F32;
+  struct Batch {
+    RawOct<BF> plain[PLAIN ? UNROLL : 1];
+    u32x4 codes[PLAIN ? 1 : UNROLL];
+    int m, c0;
+  };
+  const LinearParams& p;
+  int rows, pieces, shift, lane, turn;
+
+  // Every workgroup reads the same rows: each starts with another, so that they do not ask one line for the same rows at
+  // once.
+  __device__ __forceinline__ int row_of(int m) const { return m + turn < rows ? m + turn : m + turn - rows; }
+  __device__ __forceinline__ RowsIn(const LinearParams& p_, int rows_) : p(p_), rows(rows_) {
+    turn = (int)(blockIdx.x % (unsigned)rows);
+    shift = rows >= 8 ? 6 : rows >= 4 ? 7 : rows >= 2 ? 8 : 9;  // 2^shift threads on a row
+    lane = threadIdx.x & ((1 << shift) - 1);
+    pieces = PLAIN ? p.K / 8 : row_bytes<KX>(p.K) / 16;
+  }
+  __device__ __forceinline__ Batch first() const {
+    Batch b;
+    b.m = threadIdx.x >> shift;
+    b.c0 = 0;
+    load(b);
+    return b;
+  }
+  __device__ __forceinline__ Batch after(const Batch& now) const {
+    Batch b;
+    const int c0 = now.c0 + (UNROLL << shift);
+    b.c0 = c0 < pieces ? c0 : 0;
+    b.m = c0 < pieces ? now.m : now.m + (THREADS >> shift);
+    load(b);
+    return b;
+  }
+  __device__ __forceinline__ void load(Batch& b) const {
+    if (b.m >= rows) return;
+    const int m = row_of(b.m);
+    const uint8_t* from;
+    if constexpr (PLAIN) {
+      const int e = m / p.x_rows;
+      from = static_cast<const uint8_t*>(p.x_plain.p) +
+             ((int64_t)e * p.x_plain.sb + (int64_t)(m - e * p.x_rows) * p.x_plain.ss) * (BF ? 2 : 4);
+    } else {
+      from = p.x + (int64_t)m * p.x_stride;
+    }
+#pragma unroll
+    for (int i = 0; i < UNROLL; ++i) {
+      const int c = b.c0 + (i << shift) + lane;
+      if (c >= pieces) break;
+      if constexpr (PLAIN)
+        b.plain[i].load(reinterpret_cast<const char*>(from) + (int64_t)c * (BF ? 16 : 32));
+      else
+        b.codes[i] = *reinterpret_cast<const u32x4*>(from + 16 * c);
+    }
+  }
+  __device__ __forceinline__ void store(const Batch& b, uint8_t* codes, uint8_t* scales) const {
+    const int m = row_of(b.m);
+    uint8_t* const to = codes + m * (int)few_pitch<KX>(p.K);
+    uint8_t* const sto = scales + m * (int)few_scale_pitch(p.K);
+#pragma unroll
+    for (int i = 0; i < UNROLL; ++i) {
+      const int c = b.c0 + (i << shift) + lane;
+      if (c >= pieces) break;  // pieces are a multiple of 4: the four threads of a block leave together
+      if constexpr (PLAIN) {
+        const Oct o = b.plain[i].widen();
+        uint32_t top = max_bits(o);
+        top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+        const uint32_t e = scale_byte<KX == FP4>(top);
+        store_codes<KX == FP4>(to + (KX == FP4 ? 4 : 8) * c, o, e);
+        if ((c & 3) == 0) sto[c >> 2] = (uint8_t)e;
+      } else {
+        *reinterpret_cast<u32x4*>(to + 16 * c) = b.codes[i];
+      }
+    }
+    if (!PLAIN && b.c0 == 0)
+      for (int c = lane; c < p.K / 32; c += 1 << shift) sto[c] = p.xs[(int64_t)m * p.xs_stride + c];
+  }
+};
+
+// A workgroup forms 32 outputs of up to 32 rows, which it keeps in LDS whole; its wavefronts take chunks of K in turn, and
+// their sums are joined in order. Bound by the weights' bytes, which go from memory to registers two chunks ahead; a
+// row costs every workgroup its turn into LDS (about 0.1 ns an element). Measured: 1 row x 4096 -> 24576 in 8 and 4 bits
+// 12.9 us (4.1 TB/s; 17.4 with 64 outputs a workgroup), x 1536 -> 4608 3.9; 32 rows of that 9.0 (tiles, and the rounding
+// in a launch of its own: 13.3).
+template <int KX, int KW, int LDS, int XP>
+__global__ __launch_bounds__(64 * FEW_WAVES) void linear_few_kernel(LinearParams p) {
+  constexpr int KC = KW == FP4 ? 256 : 128, STEPS = KC / 64, ND = KC / 128;
+  static_assert(FEW_WAVES * 4096 <= LDS, "the partial sums take the rows' place");
+  __shared__ __attribute__((aligned(16))) uint8_t lds[LDS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int half = lane >> 5, r = lane & 31, rows = (int)p.M;
+  const int64_t n0 = (int64_t)blockIdx.x * 32;
+  const int cols = (int)min((int64_t)32, p.N - n0);
+  const int wbytes = row_bytes<KW>(p.K), xbytes = row_bytes<KX>(p.K);
+  const auto wr = rsrc(p.w + n0 * p.w_stride, (int64_t)(cols - 1) * p.w_stride + wbytes);
+  const auto wsr = rsrc(p.ws + n0 * p.ws_stride, (int64_t)(cols - 1) * p.ws_stride + ((p.K / 32 + 3) & ~3));
+  struct Chunk {
+    u32x4 w[STEPS][KW == FP4 ? 1 : 2];
+    uint32_t e[ND];
+  };
+  const uint32_t wrow = (uint32_t)(r * p.w_stride), wsrow = (uint32_t)(r * p.ws_stride);
+  const auto load = [&](Chunk& c, int k) {
+#pragma unroll
+    for (int t = 0; t < STEPS; ++t)
+#pragma unroll
+      for (int j = 0; j < (KW == FP4 ? 1 : 2); ++j) {
+        const int at = row_bytes<KW>(k + 64 * t) + 32 * j + 16 * half;
+        c.w[t][j] = __builtin_amdgcn_raw_buffer_load_b128(wr, at < wbytes ? wrow + at : OUTSIDE, 0, 0);
+      }
+    if constexpr (ND == 2) {
+      const u32x2 e = __builtin_amdgcn_raw_buffer_load_b64(wsr, wsrow + k / 32, 0, 0);
+      c.e[0] = e[0];
+      c.e[1] = e[1];
+    } else {
+      c.e[0] = __builtin_amdgcn_raw_buffer_load_b32(wsr, wsrow + k / 32, 0, 0);
+    }
+  };
+  f32x16 acc = {};
+  uint8_t* const scales = lds + rows * (int)few_pitch<KX>(p.K);
+  const uint8_t* const xrow = lds + min(r, rows - 1) * (int)few_pitch<KX>(p.K);  // rows past the last are not stored
+  const uint8_t* const srow = scales + min(r, rows - 1) * (int)few_scale_pitch(p.K);
+  const auto multiply = [&](const Chunk& c, int k) {
+#pragma unroll
+    for (int t = 0; t < STEPS; ++t) {
+      // Codes past the end of K are zeros on both sides, and so are scale bytes: what lies there might make NaN of them.
+      const int left = (p.K - k) / 32 - 4 * (t / 2);
+      const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
+      const int at = row_bytes<KX>(k + 64 * t) + 16 * half;
+      i32x8 xv = {}, wv = {};
+#pragma unroll
+      for (int j = 0; j < (KX == FP4 ? 1 : 2); ++j) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(xrow + min(at + 32 * j, xbytes));
+#pragma unroll
+        for (int q = 0; q < 4; ++q) xv[4 * j + q] = at + 32 * j < xbytes ? (int)v[q] : 0;
+      }
+      const uint32_t word =
+          *reinterpret_cast<const uint32_t*>(srow + min(k / 32 + 4 * (t / 2), (int)few_scale_pitch(p.K) - 4));
+      const uint32_t xe = (word & keep) >> (8 * half), we = (c.e[t / 2] & keep) >> (8 * half);
+#pragma unroll
+      for (int j = 0; j < (KW == FP4 ? 1 : 2); ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) wv[4 * j + q] = (int)c.w[t][j][q];
+      constexpr int FW = KW == FP4 ? 4 : 0, FX = KX == FP4 ? 4 : 0;
+      acc = t % 2 == 0 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wv, xv, acc, FW, FX, 0, we, 0, xe)
+                       : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wv, xv, acc, FW, FX, 2, we, 2, xe);
+    }
+  };
+  Chunk a, b;
+  int k = wave * KC;
+  constexpr int NEXT = FEW_WAVES * KC;
+  // the first rows ahead of the weights: loads come back in order, and the rows are turned while the weights are on
+  // their way
+  const RowsIn<KX, XP> in(p, rows);
+  auto batch = in.first();
+  if (k < p.K) load(a, k);
+  if (k + NEXT < p.K) load(b, k + NEXT);
+  while (batch.m < rows) {
+    const auto next = in.after(batch);
+    in.store(batch, lds, scales);
+    batch = next;
+  }
+  __syncthreads();
+  for (; k < p.K; k += 2 * NEXT) {
+    multiply(a, k);
+    if (k + 2 * NEXT < p.K) load(a, k + 2 * NEXT);
+    if (k + NEXT < p.K) multiply(b, k + NEXT);
+    if (k + 3 * NEXT < p.K) load(b, k + 3 * NEXT);
+  }
+  __syncthreads();  // the rows have been read
+  // Registers 4 g .. 4 g + 3 of lane l: outputs 8 g + 4 (l / 32) .. + 3 of row l % 32, a chunk of the row's 128 bytes
+  // (swizzled as in the tiles).
+  float* const part = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    f32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = acc[4 * g + e];
+    reinterpret_cast<f32x4*>(part)[(wave * 32 + r) * 8 + ((2 * g + half) ^ swizzle<8>(r))] = v;
+  }
+  __syncthreads();
+  for (int o = threadIdx.x; o < rows * 32; o += 64 * FEW_WAVES) {  // neighbouring threads: outputs of a row
+    const int n = o % 32, m = o / 32;
+    if (n >= cols) continue;
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < FEW_WAVES; ++w) v += part[(w * 32 + m) * 32 + 4 * (n / 4 ^ swizzle<8>(m)) + n % 4];
+    const int64_t col = n0 + n;
+    const int bt = m / p.rows;
+    const int64_t at = bt * p.y.sb + (m - bt * p.rows) * p.y.ss + col;
+    if (p.f32) {
+      if (p.bias) v += static_cast<const float*>(p.bias)[col];
+      static_cast<float*>(const_cast<void*>(p.y.p))[at] = v;
+    } else {
+      if (p.bias) v += __uint_as_float((uint32_t) static_cast<const uint16_t*>(p.bias)[col] << 16);
+      static_cast<uint16_t*>(const_cast<void*>(p.y.p))[at] = __builtin_bit_cast(uint16_t, (__bf16)v);
+    }
   }
 }
 
@@ -372,6 +623,22 @@ __global__ __launch_bounds__(256) void linear_transpose_kernel(MxView w, int32_t
   }
 }
 
+// Rows of n bytes, `stride` apart at any address, to rows of whole words with zeros behind them.
+__global__ __launch_bounds__(256) void scale_rows_kernel(const uint8_t* in, int64_t stride, int64_t sb, int32_t rows,
+                                                         int64_t M, int32_t n, int32_t words, uint32_t* out) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t m = i / words;
+  const int w = (int)(i - m * words);
+  if (m >= M) return;
+  const int64_t b = m / rows;
+  const uint8_t* p = in + b * sb + (m - b * rows) * stride + 4 * w;
+  uint32_t v = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (4 * w + j < n) v |= (uint32_t)p[j] << (8 * j);
+  out[i] = v;
+}
+
 // Column sums of g over chunks of rows, and over the chunks.
 template <bool BF16>
 __global__ __launch_bounds__(256) void column_sum_kernel(View g, int32_t rows, int64_t M, int32_t N, int64_t per,
@@ -408,20 +675,97 @@ __global__ __launch_bounds__(64) void column_sum_final_kernel(const float* part,
   }
 }
 
-template <int KX, int KW>
-hipError_t run_linear(LinearParams p, hipStream_t stream) {
-  constexpr int BM = 128, BN = 128;
+// Place in LDS that M rows take.
+int64_t few_bytes(int x_kind, int64_t M, int32_t K) {
+  return M * ((x_kind == FP4 ? few_pitch<FP4>(K) : few_pitch<FP8>(K)) + few_scale_pitch(K));
+}
+
+// Explicit: reached only through a launcher's kernel pointer, the host pass would leave their launch stubs out.
+#define RA_LINEAR_TILES(KX, KW)                                                \
+  template __global__ void linear_kernel<KX, KW, 256, 256, 2, 4>(LinearParams); \
+  template __global__ void linear_kernel<KX, KW, 128, 128, 2, 2>(LinearParams);
+RA_LINEAR_TILES(FP4, FP4)
+RA_LINEAR_TILES(FP4, FP8)
+RA_LINEAR_TILES(FP8, FP4)
+RA_LINEAR_TILES(FP8, FP8)
+RA_LINEAR_TILES(B16, B16)
+#undef RA_LINEAR_TILES
+#define RA_LINEAR_FEW_OF(KX, KW, LDS)                                             \
+  template __global__ void linear_few_kernel<KX, KW, LDS, X_CODES>(LinearParams); \
+  template __global__ void linear_few_kernel<KX, KW, LDS, X_BF16>(LinearParams);  \
+  template __global__ void linear_few_kernel<KX, KW, LDS, X_F32>(LinearParams);
+#define RA_LINEAR_FEW(KX, KW)        \
+  RA_LINEAR_FEW_OF(KX, KW, FEW_LDS) \
+  RA_LINEAR_FEW_OF(KX, KW, FEW_MORE_LDS)
+RA_LINEAR_FEW(FP4, FP4)
+RA_LINEAR_FEW(FP4, FP8)
+RA_LINEAR_FEW(FP8, FP4)
+RA_LINEAR_FEW(FP8, FP8)
+#undef RA_LINEAR_FEW
+#undef RA_LINEAR_FEW_OF
+
+template <int KX, int KW, int BM, int BN, int WM, int WN>
+hipError_t run_tiles(LinearParams p, hipStream_t stream) {
   p.tiles_m = (int32_t)((p.M + BM - 1) / BM);
   const int64_t tiles = (int64_t)p.tiles_m * ((p.N + BN - 1) / BN);
-  return launch_kernel(linear_kernel<KX, KW, BM, BN, 2, 2>, dim3((unsigned)tiles), dim3(256), 0, stream, p);
+  return launch_kernel(linear_kernel<KX, KW, BM, BN, WM, WN>, dim3((unsigned)tiles), dim3(64 * WM * WN), 0, stream, p);
+}
+
+template <int KX, int KW, int LDS>
+hipError_t run_few(const LinearParams& p, hipStream_t stream) {
+  const dim3 grid((unsigned)((p.N + 31) / 32));
+  const auto run = [&](auto* kernel) { return launch_kernel(kernel, grid, dim3(64 * FEW_WAVES), 0, stream, p); };
+  if (p.x_plain.p == nullptr) return run(linear_few_kernel<KX, KW, LDS, X_CODES>);
+  return p.x_f32 ? run(linear_few_kernel<KX, KW, LDS, X_F32>) : run(linear_few_kernel<KX, KW, LDS, X_BF16>);
+}
+template <int KX, int KW>
+hipError_t run_few(const LinearParams& p, hipStream_t stream) {
+  return few_bytes(KX, p.M, p.K) <= FEW_LDS ? run_few<KX, KW, FEW_LDS>(p, stream)
+                                            : run_few<KX, KW, FEW_MORE_LDS>(p, stream);
+}
+
+// Tiles of 256 x 256 on workgroups of 8 wavefronts, one a CU, move half the bytes a product needs with tiles of 128 x 128
+// on 4 wavefronts, two a CU, and a round of them does twice the work in 1.45 times the time; a last round that leaves the
+// CUs' second place empty takes less. Measured, in us, 256 against 128: 16384 x 2048 -> 8192 in 4 bits 180 / 243, in 8
+// and 4 262 / 370; 4352 x 4096 -> 12288 135 / 153; 2048 x 2048 -> 6144 in 8 and 4 28 / 33; 4352 x 2048 -> 4096 in 4 bits
+// 37 / 33, in 8 and 4 54 / 47; 1024 x 2048 -> 4096 18 / 10. (256 x 128 and 128 x 256 on 8 wavefronts lie between.)
+template <int KX, int KW>
+hipError_t run_linear(const LinearParams& p, hipStream_t stream) {
+  const double cus = std::max(1, attn_bf16_slots(128, kAttnBf16BM).cus);
+  const auto tiles = [&](int64_t t) { return (double)(((p.M + t - 1) / t) * ((p.N + t - 1) / t)); };
+  const double small = tiles(128) / (2 * cus), part = small - std::floor(small);
+  const double small_us = std::floor(small) + (part > 0 ? 0.6 + 0.4 * part : 0.0);
+  if (1.45 * std::ceil(tiles(256) / cus) < small_us) return run_tiles<KX, KW, 256, 256, 2, 4>(p, stream);
+  return run_tiles<KX, KW, 128, 128, 2, 2>(p, stream);
 }
 
 }  // namespace
 
+// Few rows go to the kernel that reads the weights once and turns the rows in every workgroup, at about 0.1 ns an element
+// and round of workgroups; tiles take a launch for the rounding and walk K in stages. Measured, in us, few against tiles
+// (rounding included), 8 and 4 bits: 1 row x 512 -> 512 3.3 / 7.5, x 4096 -> 24576 12.9 / 25; 16 rows x 1536 -> 4608 6.2 /
+// 13.2, x 4096 -> 4096 12.9 / 24.3, x 4096 -> 24576 38 / 27 (tiles are taken); 32 rows x 1536 -> 4608 9.0 / 13.3.
+bool linear_is_few(int x_kind, int64_t M, int32_t N, int32_t K) {
+  if (x_kind == B16 || M > FEW_ROWS || few_bytes(x_kind, M, K) > FEW_MORE_LDS) return false;
+  return (double)M * K * std::max(1.0, N / 8192.0) < 24000.0 + 31.0 * K;
+}
+
 hipError_t launch_linear(int x_kind, int w_kind, const LinearParams& p, hipStream_t stream) {
+  const bool w4 = w_kind == FP4;
   if (x_kind == B16) return run_linear<B16, B16>(p, stream);
-  if (x_kind == FP4) return w_kind == FP4 ? run_linear<FP4, FP4>(p, stream) : run_linear<FP4, FP8>(p, stream);
-  return w_kind == FP4 ? run_linear<FP8, FP4>(p, stream) : run_linear<FP8, FP8>(p, stream);
+  if (linear_is_few(x_kind, p.M, p.N, p.K)) {
+    if (x_kind == FP4) return w4 ? run_few<FP4, FP4>(p, stream) : run_few<FP4, FP8>(p, stream);
+    return w4 ? run_few<FP8, FP4>(p, stream) : run_few<FP8, FP8>(p, stream);
+  }
+  if (x_kind == FP4) return w4 ? run_linear<FP4, FP4>(p, stream) : run_linear<FP4, FP8>(p, stream);
+  return w4 ? run_linear<FP8, FP4>(p, stream) : run_linear<FP8, FP8>(p, stream);
+}
+
+hipError_t launch_scale_rows(const uint8_t* in, int64_t stride, int64_t sb, int32_t rows, int64_t M, int32_t n,
+                             int32_t words, void* out, hipStream_t stream) {
+  const dim3 grid((unsigned)((M * words + 255) / 256));
+  return launch_kernel(scale_rows_kernel, grid, dim3(256), 0, stream, in, stride, sb, rows, M, n, words,
+                       static_cast<uint32_t*>(out));
 }
 
 hipError_t launch_linear_split(int dtype, View g, int32_t rows, int64_t M, int32_t N, int32_t ld, void* out,

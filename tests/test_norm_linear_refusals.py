@@ -106,7 +106,7 @@ def test_layer_norm_grad(kw, status, msg):
 
 
 def _linear(x=_t(), x_mx=NO_MX, w=_m(0x4000), bias=None, y=_t(0x9000), workspace=0x10000, nbytes=BIG, **kw):
-    d = dict(batch=2, rows=10, n_in=256, n_out=100, dtype=L.RA_BF16, x_format=L.RA_MXFP8, w_format=L.RA_MXFP4)
+    d = dict(batch=2, rows=40, n_in=256, n_out=100, dtype=L.RA_BF16, x_format=L.RA_MXFP8, w_format=L.RA_MXFP4)
     d.update(kw)
     return _call("mx_linear", L.ra_linear_desc(**d), L.ra_linear_args(x, x_mx, w, bias, y, workspace, nbytes))
 
@@ -140,8 +140,8 @@ LINEAR_SIZES = [
     (dict(x=_t(0x1008)), L.RA_EUNSUPPORTED, "16-byte"),
     (dict(x=_t(ss=260)), L.RA_EUNSUPPORTED, "multiples"),
     (dict(x=_t(ss=128)), L.RA_EINVAL, "row stride"),
-    (dict(x=NONE, x_mx=_m(ss=256, sb=2560, es=8, eb=88)), L.RA_EUNSUPPORTED, "evenly"),
-    (dict(x=NONE, x_mx=_m(ss=256, sb=4096, es=8, eb=80)), L.RA_EUNSUPPORTED, "evenly"),
+    (dict(x=NONE, x_mx=_m(ss=256, sb=10240, es=8, eb=328)), L.RA_EUNSUPPORTED, "evenly"),
+    (dict(x=NONE, x_mx=_m(ss=256, sb=12288, es=8, eb=320)), L.RA_EUNSUPPORTED, "evenly"),
     (dict(x=NONE, x_mx=_m(ss=128)), L.RA_EINVAL, "row strides"),
     (dict(x=NONE, batch=1, x_mx=_m(ss=1 << 23)), L.RA_EUNSUPPORTED, "row stride of x_mx"),
     (dict(y=NONE), L.RA_EINVAL, "null y"),
@@ -156,7 +156,7 @@ def test_mx_linear(kw, status, msg):
 
 
 def _linear_grad(dy=_t(), w=_m(0x4000), dx=_t(0x9000), dbias=0x3000, workspace=0x10000, nbytes=BIG, **kw):
-    d = dict(batch=2, rows=10, n_in=256, n_out=104, dtype=L.RA_BF16, x_format=L.RA_MXFP8, w_format=L.RA_MXFP4)
+    d = dict(batch=2, rows=40, n_in=256, n_out=104, dtype=L.RA_BF16, x_format=L.RA_MXFP8, w_format=L.RA_MXFP4)
     d.update(kw)
     return _call("mx_linear_grad", L.ra_linear_desc(**d), L.ra_linear_grad_args(dy, w, dx, dbias, workspace, nbytes))
 
@@ -165,17 +165,17 @@ def _linear_grad(dy=_t(), w=_m(0x4000), dx=_t(0x9000), dbias=0x3000, workspace=0
     (dict(dx=NONE, dbias=None), L.RA_EINVAL, "no gradient"),
     (dict(dy=NONE), L.RA_EINVAL, "null dy"),
     (dict(dy=_t(0x1002)), L.RA_EUNSUPPORTED, "evenly"),
-    (dict(dy=_t(sb=2568)), L.RA_EUNSUPPORTED, "evenly"),
+    (dict(dy=_t(sb=10248)), L.RA_EUNSUPPORTED, "evenly"),
     (dict(dy=_t(ss=1 << 22), batch=1), L.RA_EUNSUPPORTED, "row stride of dy"),
     (dict(dx=_t(0x9001)), L.RA_EUNSUPPORTED, "aligned"),
     (dict(dx=_t(0x9000, ss=255)), L.RA_EINVAL, "row stride"),
-    (dict(dx=_t(0x9000, sb=0), dy=_t(sb=2560)), L.RA_EINVAL, "overlap"),
-    (dict(dbias=0x3001, dy=_t(sb=2560)), L.RA_EUNSUPPORTED, "dbias"),
+    (dict(dx=_t(0x9000, sb=0), dy=_t(sb=10240)), L.RA_EINVAL, "overlap"),
+    (dict(dbias=0x3001, dy=_t(sb=10240)), L.RA_EUNSUPPORTED, "dbias"),
 ])
 def test_mx_linear_grad(kw, status, msg):
     kw = dict(kw)
     if "dy" not in kw:
-        kw["dy"] = _t(sb=2560)
+        kw["dy"] = _t(sb=10240)
     st, err = _linear_grad(**kw)
     assert st == status and msg in err, (st, err)
 
@@ -190,14 +190,16 @@ def test_null_blocks_and_nothing_to_do():
 
 
 def test_workspace_sizes():
-    d = L.ra_linear_desc(2, 10, 256, 104, L.RA_BF16, L.RA_MXFP8, L.RA_MXFP4)
+    d = L.ra_linear_desc(2, 40, 256, 104, L.RA_BF16, L.RA_MXFP8, L.RA_MXFP4)
     size = L.LIB.refadapt_mx_linear_workspace_size
-    assert size(d, 0) >= 20 * (256 + 8) and size(d, 1) == 0
-    f = L.ra_linear_desc(2, 10, 256, 104, L.RA_F32, L.RA_MXFP8, L.RA_MXFP4)
-    assert size(f, 1) >= (20 + 104) * 512 and size(f, 0) > size(f, 1)
+    assert size(d, 0) >= 80 * (256 + 8) and size(d, 1) == 0
+    f = L.ra_linear_desc(2, 40, 256, 104, L.RA_F32, L.RA_MXFP8, L.RA_MXFP4)
+    assert size(f, 1) >= (80 + 104) * 512 and size(f, 0) > size(f, 1)
+    few = L.ra_linear_desc(2, 10, 256, 104, L.RA_BF16, L.RA_MXFP8, L.RA_MXFP4)
+    assert size(few, 0) == 0  # rounded on the way
     assert L.LIB.refadapt_mx_linear_grad_workspace_size(d) >= 256 * 104 * 2 + 104 * 4
-    assert L.LIB.refadapt_mx_linear_grad_workspace_size(f) >= 256 * 104 * 2 + 3 * 20 * 104 * 2
-    bad = L.ra_linear_desc(2, 10, 250, 104, L.RA_BF16, L.RA_MXFP8, L.RA_MXFP4)
+    assert L.LIB.refadapt_mx_linear_grad_workspace_size(f) >= 256 * 104 * 2 + 3 * 80 * 104 * 2
+    bad = L.ra_linear_desc(2, 40, 250, 104, L.RA_BF16, L.RA_MXFP8, L.RA_MXFP4)
     assert size(bad, 0) == 0 and L.LIB.refadapt_mx_linear_grad_workspace_size(bad) == 0
     n = L.ra_norm_desc(3, 100, 512, L.RA_BF16, L.RA_F32, 0, 1e-6)
     assert L.LIB.refadapt_layer_norm_grad_workspace_size(n) >= 3 * 2 * 512 * 4
