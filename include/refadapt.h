@@ -517,8 +517,7 @@ typedef struct {
  * Errors: RA_EINVAL (null desc, args or tensors, both of y and y_mx, sizes, dtypes,
  * eps, negative or overlapping strides, x broadcast over the batch and normalised in
  * place), RA_EUNSUPPORTED (width above 16384, or not a multiple of 32 with y_mx,
- * alignment, batch above 65535, 2^26 or more rows of up to 1024, 2^24 of up to 8192,
- * 2^22 of more elements).
+ * alignment, batch above 65535, 2^31 or more rows).
  */
 ra_status refadapt_layer_norm(const ra_norm_desc* desc, const ra_norm_args* args, void* stream);
 

@@ -879,6 +879,8 @@ bool vector_in_units(const void* p, int64_t stride, int dtype) {
   return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride % (dtype == RA_BF16 ? 8 : 4) == 0;
 }
 
+size_t padded(size_t bytes) { return (bytes + 255) & ~size_t(255); }
+
 ra_status check_norm_desc(const char* who, const ra_norm_desc* desc) {
   if (!desc) return fail(RA_EINVAL, "%s: null desc", who);
   const ra_norm_desc& d = *desc;
@@ -888,9 +890,7 @@ ra_status check_norm_desc(const char* who, const ra_norm_desc* desc) {
     return fail(RA_EINVAL, "%s: parameters are of the rows' dtype or fp32 (got %d)", who, d.param_dtype);
   if (!(d.eps >= 0.f) || !std::isfinite(d.eps)) return fail(RA_EINVAL, "%s: eps must be finite and not negative", who);
   if (d.width > kNormMaxWidth) return fail(RA_EUNSUPPORTED, "%s: width %d above %d", who, d.width, kNormMaxWidth);
-  // 64, 256 or 1024 threads a row, and fewer than 2^32 in a launch
-  const int64_t most = int64_t(1) << (d.width <= 1024 ? 26 : d.width <= 8192 ? 24 : 22);
-  if (d.batch > 65535 || (int64_t)d.batch * d.rows >= most)
+  if (d.batch > 65535 || (int64_t)d.batch * d.rows >= int64_t(1) << 31)
     return fail(RA_EUNSUPPORTED, "%s: %d x %d rows are too many for one launch", who, d.batch, d.rows);
   return RA_OK;
 }
@@ -956,7 +956,9 @@ ra_status refadapt_layer_norm(const ra_norm_desc* desc, const ra_norm_args* args
 
 size_t refadapt_layer_norm_grad_workspace_size(const ra_norm_desc* desc) {
   if (check_norm_desc("layer_norm_grad_workspace_size", desc) != RA_OK) return 0;
-  return (size_t)desc->batch * norm_grad_chunks(desc->batch, desc->rows) * 2 * desc->width * sizeof(float);
+  const size_t B = desc->batch, C = desc->width;
+  return (B > 1 ? padded(B * 2 * C * sizeof(double)) : 0) +
+         B * norm_grad_chunks(desc->batch, desc->rows, desc->width) * 2 * C * sizeof(float);
 }
 
 ra_status refadapt_layer_norm_grad(const ra_norm_desc* desc, const ra_norm_grad_args* args, void* stream) {
@@ -1010,7 +1012,11 @@ ra_status refadapt_layer_norm_grad(const ra_norm_desc* desc, const ra_norm_grad_
   p.dbias = a.dbias;
   p.dscale = a.dscale;
   p.dshift = a.dshift;
-  p.part = sums ? static_cast<float*>(a.workspace) : nullptr;
+  if (sums) {
+    p.entry = static_cast<double*>(a.workspace);
+    p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) +
+                                      (d.batch > 1 ? padded((size_t)d.batch * 2 * d.width * sizeof(double)) : 0));
+  }
   p.B = d.batch;
   p.S = d.rows;
   p.C = d.width;
@@ -1022,7 +1028,6 @@ ra_status refadapt_layer_norm_grad(const ra_norm_desc* desc, const ra_norm_grad_
 
 namespace {
 
-size_t padded(size_t bytes) { return (bytes + 255) & ~size_t(255); }
 int64_t mx_row(int32_t format, int64_t n) { return format == RA_MXFP4 ? n / 2 : n; }
 int64_t mx_scale_row(int64_t n) { return (n / 32 + 3) & ~int64_t(3); }  // whole words
 

@@ -186,8 +186,9 @@ struct NormParams {
   int64_t scale_sb, shift_sb;                 // elements
   float* stats;                               // [B, S, 2] mean and 1 / deviation, or null
   int32_t B, S, C;
+  int32_t rows_per;  // of a chunk, set by the launcher
   float eps;
-  bool param_f32, vec;  // vec: every row of every tensor is in whole, aligned 16-byte units
+  bool param_f32, vec;  // vec: every row of every plain tensor is in whole, aligned 16-byte units
 };
 hipError_t launch_norm(int dtype, NormParams p, hipStream_t stream);
 struct NormGradParams {
@@ -197,11 +198,12 @@ struct NormGradParams {
   int64_t scale_sb;
   void *dweight, *dbias, *dscale, *dshift;  // [C], [C], [B, C], [B, C], each null where not wanted
   float* part;                              // [B][chunks][2][C] column sums, or null: no parameter's gradient is wanted
+  double* entry;                            // [B][2][C] where B > 1
   int32_t chunks, rows_per;                 // set by the launcher
   int32_t B, S, C;
   bool param_f32, vec;
 };
-int norm_grad_chunks(int32_t B, int32_t S);
+int norm_grad_chunks(int32_t B, int32_t S, int32_t C);
 hipError_t launch_norm_grad(int dtype, NormGradParams p, hipStream_t stream);
 
 // y [M, N] = x [M, K] w [N, K]^T + bias over codes (kinds MX_FP4, MX_FP8) with scale bytes, or over bf16 values (kind 2).

@@ -8,6 +8,10 @@
 //
 // Statistics and sums are fp32, the variance from the differences to the mean (a second pass over registers), the sums
 // of row chunks fp64; results are rounded once. Sums run in a fixed order: outputs repeat bit for bit.
+//
+// Bound by memory: a row stays in registers between its passes, and each workgroup has the next one on its way. A large
+// copy moves 5.1 TB/s; measured in bf16: 4096 x 4096 with its modulation 16.4 us (4.1 TB/s), 16384 x 2048 with every
+// parameter 29.6 (4.5 TB/s); dx alone there 42 (4.8 TB/s), with the four sums 55.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -38,54 +42,61 @@ __device__ __forceinline__ float row_sum(float v, float* slot) {
   return v;
 }
 
-// Eight elements at p + 8 * piece of a row of C, zeros past its end. `vec`: rows are in whole 16-byte units.
-template <bool BF16>
-__device__ __forceinline__ Oct load_piece(const char* p, int piece, int C, bool vec) {
-  Oct o;
-  const int c0 = 8 * piece;
-  if (vec) {
-    if (c0 < C) {
-      RawOct<BF16> raw;
-      raw.load(p + c0 * (BF16 ? 2 : 4));
-      return raw.widen();
+// The elements of a row that a lane holds, 8 a piece: piece lane + L k of the row's (`pieces`), or every L-th element, so
+// that neighbouring lanes read neighbouring elements where rows are not in whole 16-byte units (`vec` false).
+template <int L>
+struct Lane {
+  int lane, C;
+  bool vec, pieces;
+  __device__ __forceinline__ int at(int k, int i) const {
+    return pieces ? 8 * (lane + L * k) + i : 8 * L * k + L * i + lane;
+  }
+  // zeros past the row's end
+  template <bool BF16>
+  __device__ __forceinline__ RawOct<BF16> raw(const char* p, int k) const {
+    RawOct<BF16> o = {};
+    if (vec) {
+      if (at(k, 0) < C) o.load(p + at(k, 0) * (BF16 ? 2 : 4));
+      return o;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o.f[i] = 0.f;
-    return o;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    o.f[i] = 0.f;
-    if (c0 + i < C) {
-      if constexpr (BF16) {
-        o.f[i] = __uint_as_float((uint32_t) reinterpret_cast<const uint16_t*>(p)[c0 + i] << 16);
-      } else {
-        o.f[i] = reinterpret_cast<const float*>(p)[c0 + i];
+    for (int i = 0; i < 8; ++i) {
+      if (at(k, i) < C) {
+        if constexpr (BF16)
+          o.w[0][i / 2] |= (uint32_t) reinterpret_cast<const uint16_t*>(p)[at(k, i)] << (16 * (i % 2));
+        else
+          o.w[i / 4][i % 4] = reinterpret_cast<const uint32_t*>(p)[at(k, i)];
       }
     }
-  }
-  return o;
-}
-
-// The same of a parameter, whose type is known at run time; `none` where it is not given.
-__device__ __forceinline__ Oct load_param(const void* p, bool f32, int piece, int C, bool vec, float none) {
-  if (p == nullptr) {
-    Oct o;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) o.f[i] = none;
     return o;
   }
-  const char* q = static_cast<const char*>(p);
-  return f32 ? load_piece<false>(q, piece, C, vec) : load_piece<true>(q, piece, C, vec);
-}
+  template <bool BF16>
+  __device__ __forceinline__ Oct load(const char* p, int k) const {
+    return raw<BF16>(p, k).widen();
+  }
+  // A parameter, whose type is known at run time; `none` where it is not given.
+  __device__ __forceinline__ Oct param(const void* p, bool f32, int k, float none) const {
+    if (p == nullptr) {
+      Oct o;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o.f[i] = none;
+      return o;
+    }
+    const char* q = static_cast<const char*>(p);
+    return f32 ? load<false>(q, k) : load<true>(q, k);
+  }
+  // Rounds to nearest even and stores.
+  template <bool BF16>
+  __device__ __forceinline__ void store(char* p, const Oct& o, int k) const;
+};
 
 __device__ __forceinline__ uint16_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 
-// Rounds to nearest even and stores.
+template <int L>
 template <bool BF16>
-__device__ __forceinline__ void store_piece(char* p, const Oct& o, int piece, int C, bool vec) {
-  const int c0 = 8 * piece;
+__device__ __forceinline__ void Lane<L>::store(char* p, const Oct& o, int k) const {
   if (vec) {
+    const int c0 = at(k, 0);
     if (c0 >= C) return;
     if constexpr (BF16) {
       u32x4 w;
@@ -106,138 +117,171 @@ __device__ __forceinline__ void store_piece(char* p, const Oct& o, int piece, in
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    if (c0 + i >= C) return;
-    if constexpr (BF16) {
-      reinterpret_cast<uint16_t*>(p)[c0 + i] = bf16_bits(o.f[i]);
-    } else {
-      reinterpret_cast<float*>(p)[c0 + i] = o.f[i];
-    }
+    if (at(k, i) >= C) return;
+    if constexpr (BF16)
+      reinterpret_cast<uint16_t*>(p)[at(k, i)] = bf16_bits(o.f[i]);
+    else
+      reinterpret_cast<float*>(p)[at(k, i)] = o.f[i];
   }
 }
 
-// W wavefronts on a row, NP pieces of 8 elements a lane: piece lane + 64 W k of the row's. y goes out as it is or, with
-// FMT 0 or 1, as e2m1 or e4m3 codes of the values rounded to the rows' type (the bits that quantising y itself gives).
+// blockIdx.y: batch entry, x: chunk of its rows. W wavefronts work on a row, with W = 1 each wavefront of the workgroup on
+// rows of its own; NP pieces a lane. The parameters, folded to y = h p + q, stay in registers over the chunk, and the next
+// row is on its way while one is worked on. y goes out as it is or, with a format, as codes of the values
+// rounded to the rows' type (the bits that quantising y itself gives).
 template <bool BF16, int W, int NP>
-__global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS) void norm_kernel(NormParams p) {
-  constexpr int ROWS = W >= 4 ? 1 : NORM_THREADS / 64 / W;  // rows of a workgroup
+__global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS, 4) void norm_kernel(NormParams p) {
+  constexpr int ROWS = W >= 4 ? 1 : NORM_THREADS / 64 / W;  // rows of a workgroup at a time
   constexpr int L = 64 * W;
-  __shared__ float slots[2][W];
-  const int lane = threadIdx.x % L;
-  const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / L;
-  if (row >= (int64_t)p.B * p.S) return;  // W > 1: one row a workgroup, so all of it leaves
-  const int b = (int)(row / p.S), s = (int)(row - (int64_t)b * p.S), C = p.C;
-  const bool vec = p.vec, pf32 = p.param_f32;
+  __shared__ float slots[2][2][W];
+  const int b = blockIdx.y, C = p.C;
+  const int s0 = blockIdx.x * p.rows_per, s1 = min(p.S, s0 + p.rows_per);
+  const bool pf32 = p.param_f32;
+  // codes need a block of 32 elements on four neighbouring lanes, whatever the alignment
+  const Lane<L> ln{(int)(threadIdx.x % L), C, p.vec, p.vec || p.y.p == nullptr};
   constexpr int esz = BF16 ? 2 : 4;
-  const char* x = static_cast<const char*>(p.x.p) + (b * p.x.sb + s * p.x.ss) * esz;
+  const char* const x = static_cast<const char*>(p.x.p) + b * p.x.sb * esz;
+  int s = s0 + (int)threadIdx.x / L;
   Oct v[NP];
-  float sum = 0.f;
+  RawOct<BF16> next[NP];
+  if (s < s1) {
 #pragma unroll
-  for (int k = 0; k < NP; ++k) {
-    v[k] = load_piece<BF16>(x, lane + L * k, C, vec);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) sum += v[k].f[i];
+    for (int k = 0; k < NP; ++k) next[k] = ln.template raw<BF16>(x + s * p.x.ss * esz, k);
   }
-  const float mean = row_sum<W>(sum, slots[0]) / (float)C;
-  float sq = 0.f;
-#pragma unroll
-  for (int k = 0; k < NP; ++k)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float d = v[k].f[i] - mean;
-      v[k].f[i] = d;
-      if (8 * (lane + L * k) + i < C) sq += d * d;
-    }
-  const float var = row_sum<W>(sq, slots[1]) / (float)C;
-  const float r = 1.f / sqrtf(var + p.eps);
-  if (p.stats && lane == 0) reinterpret_cast<float2*>(p.stats)[row] = make_float2(mean, r);
   const int psz = pf32 ? 4 : 2;
   const char* sc = static_cast<const char*>(p.scale);
   const char* sh = static_cast<const char*>(p.shift);
   if (sc) sc += b * p.scale_sb * psz;
   if (sh) sh += b * p.shift_sb * psz;
-  char* y = static_cast<char*>(const_cast<void*>(p.y.p));
-  if (y) y += (b * p.y.sb + s * p.y.ss) * esz;
+  Oct mul[NP], add[NP];
 #pragma unroll
   for (int k = 0; k < NP; ++k) {
-    const int piece = lane + L * k;
-    const Oct w = load_param(p.weight, pf32, piece, C, vec, 1.f), a = load_param(p.bias, pf32, piece, C, vec, 0.f);
-    const Oct m = load_param(sc, pf32, piece, C, vec, 0.f), t = load_param(sh, pf32, piece, C, vec, 0.f);
+    const Oct w = ln.param(p.weight, pf32, k, 1.f), a = ln.param(p.bias, pf32, k, 0.f);
+    const Oct m = ln.param(sc, pf32, k, 0.f), t = ln.param(sh, pf32, k, 0.f);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[k].f[i] = (v[k].f[i] * r * w.f[i] + a.f[i]) * (1.f + m.f[i]) + t.f[i];
-    if (y) {
-      store_piece<BF16>(y, v[k], piece, C, vec);
-    } else {
+    for (int i = 0; i < 8; ++i) {
+      mul[k].f[i] = w.f[i] * (1.f + m.f[i]);
+      add[k].f[i] = fmaf(a.f[i], 1.f + m.f[i], t.f[i]);
+    }
+  }
+  for (int turn = 0; s < s1; s += ROWS, turn ^= 1) {
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < NP; ++k) {
+      v[k] = next[k].widen();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += v[k].f[i];
+    }
+    if (s + ROWS < s1) {
+#pragma unroll
+      for (int k = 0; k < NP; ++k) next[k] = ln.template raw<BF16>(x + (s + ROWS) * p.x.ss * esz, k);
+    }
+    const float mean = row_sum<W>(sum, slots[turn][0]) / (float)C;
+    float sq = 0.f;
+#pragma unroll
+    for (int k = 0; k < NP; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v[k].f[i] -= mean;
+        if (ln.at(k, i) < C) sq += v[k].f[i] * v[k].f[i];
+      }
+    const float var = row_sum<W>(sq, slots[turn][1]) / (float)C;
+    const float r = 1.f / sqrtf(var + p.eps);
+    if (p.stats && ln.lane == 0) reinterpret_cast<float2*>(p.stats)[(int64_t)b * p.S + s] = make_float2(mean, r);
+#pragma unroll
+    for (int k = 0; k < NP; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[k].f[i] = fmaf(v[k].f[i] * r, mul[k].f[i], add[k].f[i]);
+    if (p.y.p) {
+      char* const y = static_cast<char*>(const_cast<void*>(p.y.p)) + (b * p.y.sb + s * p.y.ss) * esz;
+#pragma unroll
+      for (int k = 0; k < NP; ++k) ln.template store<BF16>(y, v[k], k);
+      continue;
+    }
+    uint8_t* const codes = p.y_mx.codes + b * p.y_mx.sb + s * p.y_mx.ss;
+    uint8_t* const scales = p.y_mx.scales + b * p.y_mx.eb + s * p.y_mx.es;
+#pragma unroll
+    for (int k = 0; k < NP; ++k) {
       // C is a multiple of 32: the four lanes of a block are in the row together or not at all
+      const int piece = ln.lane + L * k;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         if constexpr (BF16) v[k].f[i] = __uint_as_float((uint32_t)bf16_bits(v[k].f[i]) << 16);
       uint32_t mb = max_bits(v[k]);
       mb = max(mb, (uint32_t)__shfl_xor((int)mb, 1));
       mb = max(mb, (uint32_t)__shfl_xor((int)mb, 2));
-      if (8 * piece < C) {
-        uint8_t* codes = p.y_mx.codes + b * p.y_mx.sb + s * p.y_mx.ss;
-        uint8_t* scales = p.y_mx.scales + b * p.y_mx.eb + s * p.y_mx.es;
-        uint32_t e;
-        if (p.format == MX_FP4) {
-          e = scale_byte<true>(mb);
-          store_codes<true>(codes + 4 * piece, v[k], e);
-        } else {
-          e = scale_byte<false>(mb);
-          store_codes<false>(codes + 8 * piece, v[k], e);
-        }
-        if ((piece & 3) == 0) scales[piece >> 2] = (uint8_t)e;
+      if (8 * piece >= C) continue;
+      uint32_t e;
+      if (p.format == MX_FP4) {
+        e = scale_byte<true>(mb);
+        store_codes<true>(codes + 4 * piece, v[k], e);
+      } else {
+        e = scale_byte<false>(mb);
+        store_codes<false>(codes + 8 * piece, v[k], e);
       }
+      if ((piece & 3) == 0) scales[piece >> 2] = (uint8_t)e;
     }
   }
 }
 
-// blockIdx.y: batch entry, x: chunk of its rows. W wavefronts on a row; with W < 4 the workgroup's other wavefronts
-// take rows of their own and the column sums are joined in shared memory.
+// The same chunks. With W = 1 the workgroup's wavefronts join their column sums in shared memory.
 template <bool BF16, int W, int NP>
 __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS) void norm_grad_kernel(NormGradParams p) {
   constexpr int ROWS = W >= 4 ? 1 : NORM_THREADS / 64 / W;
   constexpr int L = 64 * W;
   __shared__ float slots[2][2][W];
-  const int lane = threadIdx.x % L, group = threadIdx.x / L;
+  const int group = threadIdx.x / L;
   const int b = blockIdx.y, C = p.C;
   const int s0 = blockIdx.x * p.rows_per, s1 = min(p.S, s0 + p.rows_per);
-  const bool vec = p.vec, pf32 = p.param_f32;
+  const bool pf32 = p.param_f32;
+  const Lane<L> ln{(int)(threadIdx.x % L), C, p.vec, p.vec};
   constexpr int esz = BF16 ? 2 : 4;
+  const char* const xb = static_cast<const char*>(p.x.p) + b * p.x.sb * esz;
+  const char* const gb = static_cast<const char*>(p.dy.p) + b * p.dy.sb * esz;
+  const float2* const st = reinterpret_cast<const float2*>(p.stats) + (int64_t)b * p.S;
   const char* sc = static_cast<const char*>(p.scale);
   if (sc) sc += b * p.scale_sb * (pf32 ? 4 : 2);
   Oct ws[NP], P[NP], D[NP];
+  RawOct<BF16> xn[NP], gn[NP];
+  float2 stn = make_float2(0.f, 0.f);
+  const auto fetch = [&](int s) {
+    stn = st[s];
+#pragma unroll
+    for (int k = 0; k < NP; ++k) {
+      xn[k] = ln.template raw<BF16>(xb + s * p.x.ss * esz, k);
+      gn[k] = ln.template raw<BF16>(gb + s * p.dy.ss * esz, k);
+    }
+  };
+  int s = s0 + group;
+  if (s < s1) fetch(s);
 #pragma unroll
   for (int k = 0; k < NP; ++k) {
-    const Oct w = load_param(p.weight, pf32, lane + L * k, C, vec, 1.f);
-    const Oct m = load_param(sc, pf32, lane + L * k, C, vec, 0.f);
+    const Oct w = ln.param(p.weight, pf32, k, 1.f), m = ln.param(sc, pf32, k, 0.f);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       ws[k].f[i] = w.f[i] * (1.f + m.f[i]);
       P[k].f[i] = D[k].f[i] = 0.f;
     }
   }
-  int turn = 0;
-  for (int s = s0 + group; s < s1; s += ROWS, turn ^= 1) {
-    const char* x = static_cast<const char*>(p.x.p) + (b * p.x.sb + s * p.x.ss) * esz;
-    const char* g = static_cast<const char*>(p.dy.p) + (b * p.dy.sb + s * p.dy.ss) * esz;
-    const float2 st = reinterpret_cast<const float2*>(p.stats)[(int64_t)b * p.S + s];
+  for (int turn = 0; s < s1; s += ROWS, turn ^= 1) {
     Oct h[NP], e[NP];
+    const float2 now = stn;
     float a0 = 0.f, a1 = 0.f;
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
-      const int piece = lane + L * k;
-      h[k] = load_piece<BF16>(x, piece, C, vec);
-      e[k] = load_piece<BF16>(g, piece, C, vec);
+      const Oct xw = xn[k].widen(), gw = gn[k].widen();
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        h[k].f[i] = 8 * piece + i < C ? (h[k].f[i] - st.x) * st.y : 0.f;
-        P[k].f[i] = fmaf(e[k].f[i], h[k].f[i], P[k].f[i]);
-        D[k].f[i] += e[k].f[i];
-        e[k].f[i] *= ws[k].f[i];
+        const float g = gw.f[i];
+        h[k].f[i] = ln.at(k, i) < C ? (xw.f[i] - now.x) * now.y : 0.f;
+        P[k].f[i] = fmaf(g, h[k].f[i], P[k].f[i]);
+        D[k].f[i] += g;
+        e[k].f[i] = g * ws[k].f[i];
         a0 += e[k].f[i];
         a1 = fmaf(e[k].f[i], h[k].f[i], a1);
       }
     }
+    if (s + ROWS < s1) fetch(s + ROWS);
     // both sums behind one barrier; the slots of the row before stay readable (two sets in turn)
 #pragma unroll
     for (int m = 32; m > 0; m >>= 1) {
@@ -258,15 +302,14 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS) void norm_grad_kerne
         a1 += slots[turn][1][i];
       }
     }
-    const float m0 = a0 / (float)C, m1 = a1 / (float)C;
-    char* dx = static_cast<char*>(const_cast<void*>(p.dx.p));
-    if (dx) {
-      dx += (b * p.dx.sb + s * p.dx.ss) * esz;
+    if (p.dx.p) {
+      const float m0 = a0 / (float)C, m1 = a1 / (float)C;
+      char* const dx = static_cast<char*>(const_cast<void*>(p.dx.p)) + (b * p.dx.sb + s * p.dx.ss) * esz;
 #pragma unroll
       for (int k = 0; k < NP; ++k) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[k].f[i] = st.y * (e[k].f[i] - m0 - h[k].f[i] * m1);
-        store_piece<BF16>(dx, e[k], lane + L * k, C, vec);
+        for (int i = 0; i < 8; ++i) e[k].f[i] = now.y * (e[k].f[i] - m0 - h[k].f[i] * m1);
+        ln.template store<BF16>(dx, e[k], k);
       }
     }
   }
@@ -279,8 +322,8 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS) void norm_grad_kerne
       for (int k = 0; k < NP; ++k)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          joined[group - 1][0][8 * (lane + L * k) + i] = P[k].f[i];
-          joined[group - 1][1][8 * (lane + L * k) + i] = D[k].f[i];
+          joined[group - 1][0][64 * (8 * k + i) + ln.lane] = P[k].f[i];
+          joined[group - 1][1][64 * (8 * k + i) + ln.lane] = D[k].f[i];
         }
     }
     __syncthreads();
@@ -291,14 +334,14 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS) void norm_grad_kerne
       for (int k = 0; k < NP; ++k)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          P[k].f[i] += joined[j][0][8 * (lane + L * k) + i];
-          D[k].f[i] += joined[j][1][8 * (lane + L * k) + i];
+          P[k].f[i] += joined[j][0][64 * (8 * k + i) + ln.lane];
+          D[k].f[i] += joined[j][1][64 * (8 * k + i) + ln.lane];
         }
   }
 #pragma unroll
   for (int k = 0; k < NP; ++k) {
-    store_piece<false>(reinterpret_cast<char*>(out), P[k], lane + L * k, C, vec);
-    store_piece<false>(reinterpret_cast<char*>(out + C), D[k], lane + L * k, C, vec);
+    ln.template store<false>(reinterpret_cast<char*>(out), P[k], k);
+    ln.template store<false>(reinterpret_cast<char*>(out + C), D[k], k);
   }
 }
 
@@ -316,45 +359,68 @@ __device__ __forceinline__ void put_param(void* p, bool f32, int64_t i, double v
   }
 }
 
-// Joins the chunks' column sums: FIN_COLS columns a workgroup, its groups of threads take chunks in turn.
-constexpr int FIN_COLS = 32, FIN_GROUPS = 16;
+// Joins the chunks' column sums of batch entry blockIdx.y: FIN_COLS columns a workgroup, its groups of threads take chunks
+// in turn. With several entries the terms of dw and db go to `entry` [B][2][C], which a second launch adds up.
+constexpr int FIN_COLS = 32, FIN_GROUPS = 32, FIN_UNROLL = 4;
 __global__ __launch_bounds__(FIN_COLS * FIN_GROUPS) void norm_grad_final_kernel(NormGradParams p) {
   __shared__ double held[2][FIN_GROUPS][FIN_COLS];
   const int col = threadIdx.x % FIN_COLS, group = threadIdx.x / FIN_COLS;
-  const int c = blockIdx.x * FIN_COLS + col;
-  const bool pf32 = p.param_f32;
-  double dw = 0.0, db = 0.0;
-  for (int b = 0; b < p.B; ++b) {
-    double P = 0.0, D = 0.0;
-    if (c < p.C) {
-      const float* q = p.part + (int64_t)b * p.chunks * 2 * p.C + c;
-      for (int j = group; j < p.chunks; j += FIN_GROUPS) {
-        P += q[(int64_t)j * 2 * p.C];
-        D += q[(int64_t)j * 2 * p.C + p.C];
+  const int c = blockIdx.x * FIN_COLS + col, b = blockIdx.y;
+  double P = 0.0, D = 0.0;
+  if (c < p.C) {
+    const float* q = p.part + (int64_t)b * p.chunks * 2 * p.C + c;
+    for (int j0 = group; j0 < p.chunks; j0 += FIN_UNROLL * FIN_GROUPS) {
+      float u[FIN_UNROLL], v[FIN_UNROLL];
+#pragma unroll
+      for (int i = 0; i < FIN_UNROLL; ++i) {
+        const int j = j0 + i * FIN_GROUPS;
+        u[i] = j < p.chunks ? q[(int64_t)j * 2 * p.C] : 0.f;
+        v[i] = j < p.chunks ? q[(int64_t)j * 2 * p.C + p.C] : 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < FIN_UNROLL; ++i) {
+        P += u[i];
+        D += v[i];
       }
     }
-    __syncthreads();  // the sums of the entry before have been read
-    held[0][group][col] = P;
-    held[1][group][col] = D;
+  }
+  held[0][group][col] = P;
+  held[1][group][col] = D;
+#pragma unroll
+  for (int n = FIN_GROUPS / 2; n > 0; n /= 2) {
     __syncthreads();
-    if (group == 0 && c < p.C) {
-      P = D = 0.0;
-      for (int i = 0; i < FIN_GROUPS; ++i) {
-        P += held[0][i][col];
-        D += held[1][i][col];
-      }
-      const double s1 = 1.0 + param_at(p.scale, pf32, b * p.scale_sb + c, 0.f);
-      dw += s1 * P;
-      db += s1 * D;
-      put_param(p.dscale, pf32, (int64_t)b * p.C + c,
-                param_at(p.weight, pf32, c, 1.f) * P + param_at(p.bias, pf32, c, 0.f) * D);
-      put_param(p.dshift, pf32, (int64_t)b * p.C + c, D);
+    if (group < n) {
+      held[0][group][col] += held[0][group + n][col];
+      held[1][group][col] += held[1][group + n][col];
     }
   }
-  if (group == 0 && c < p.C) {
-    put_param(p.dweight, pf32, c, dw);
-    put_param(p.dbias, pf32, c, db);
+  if (group > 0 || c >= p.C) return;
+  P = held[0][0][col];
+  D = held[1][0][col];
+  const bool pf32 = p.param_f32;
+  const double s1 = 1.0 + param_at(p.scale, pf32, b * p.scale_sb + c, 0.f);
+  put_param(p.dscale, pf32, (int64_t)b * p.C + c,
+            param_at(p.weight, pf32, c, 1.f) * P + param_at(p.bias, pf32, c, 0.f) * D);
+  put_param(p.dshift, pf32, (int64_t)b * p.C + c, D);
+  if (p.B == 1) {
+    put_param(p.dweight, pf32, c, s1 * P);
+    put_param(p.dbias, pf32, c, s1 * D);
+  } else {
+    p.entry[(int64_t)b * 2 * p.C + c] = s1 * P;
+    p.entry[((int64_t)b * 2 + 1) * p.C + c] = s1 * D;
   }
+}
+__global__ __launch_bounds__(64) void norm_grad_entries_kernel(NormGradParams p) {
+  const int c = blockIdx.x * 64 + threadIdx.x;
+  if (c >= p.C) return;
+  double dw = 0.0, db = 0.0;
+#pragma unroll 8
+  for (int b = 0; b < p.B; ++b) {
+    dw += p.entry[(int64_t)b * 2 * p.C + c];
+    db += p.entry[((int64_t)b * 2 + 1) * p.C + c];
+  }
+  put_param(p.dweight, p.param_f32, c, dw);
+  put_param(p.dbias, p.param_f32, c, db);
 }
 
 // Calls f with the wavefronts on a row and the pieces of a lane for rows of C elements.
@@ -365,7 +431,7 @@ hipError_t with_shape(int32_t C, F f) {
   if (pieces <= 128) return f(std::integral_constant<int, 1>{}, std::integral_constant<int, 2>{});
   if (pieces <= 256) return f(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
   if (pieces <= 512) return f(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
-  if (pieces <= 1024) return f(std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{});
+  if (pieces <= 1024) return f(std::integral_constant<int, 8>{}, std::integral_constant<int, 2>{});
   return f(std::integral_constant<int, 16>{}, std::integral_constant<int, 2>{});
 }
 
@@ -375,20 +441,28 @@ hipError_t launch_norm(int dtype, NormParams p, hipStream_t stream) {
   return with_shape(p.C, [&](auto w, auto np) {
     constexpr int W = decltype(w)::value, NP = decltype(np)::value;
     constexpr int rows = W >= 4 ? 1 : NORM_THREADS / 64 / W, threads = W > 4 ? 64 * W : NORM_THREADS;
-    const dim3 grid((unsigned)(((int64_t)p.B * p.S + rows - 1) / rows));
+    // Workgroups that are at work at once, about: the parameters are read once a chunk and the next row is on its way.
+    // 4096 x 4096 16.4 us (18.9 with 2048 chunks), 2048 x 8192 22.0 (26.3), 16384 x 2048 in one piece a lane 29.6 (29.8
+    // with 1024; 38 with a workgroup a row).
+    const int64_t most = W == 4 && NP == 1 ? 2048 : 1024;
+    const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>(most / p.B, (p.S + rows - 1) / rows));
+    p.rows_per = (int32_t)((p.S + chunks - 1) / chunks);
+    const dim3 grid((unsigned)((p.S + p.rows_per - 1) / p.rows_per), (unsigned)p.B);
     return dtype == 0 ? launch_kernel(norm_kernel<true, W, NP>, grid, dim3(threads), 0, stream, p)
                       : launch_kernel(norm_kernel<false, W, NP>, grid, dim3(threads), 0, stream, p);
   });
 }
 
-int norm_grad_chunks(int32_t B, int32_t S) {
-  // two workgroups a CU, and two rows a workgroup at least
-  const int64_t most = std::max<int64_t>(1, 512 / B);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(most, (S + 1) / 2));
+// A chunk's column sums cost a store and a load of 2 C values, a launch of few chunks leaves loads unhidden: 512 chunks, two
+// rows each at least, and 256 of wide rows. Measured with every gradient, 256 / 512 / 1024 chunks: 16384 x 2048 bf16
+// 76 / 55 / 63 us, 4096 x 4096 35 / 33 / 46, 2048 x 8192 31 / 43 / 62.
+int norm_grad_chunks(int32_t B, int32_t S, int32_t C) {
+  const int64_t most = std::max<int64_t>(1, (C > 4096 ? 256 : 512) / B);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(most, ((int64_t)S + 1) / 2));
 }
 
 hipError_t launch_norm_grad(int dtype, NormGradParams p, hipStream_t stream) {
-  p.chunks = norm_grad_chunks(p.B, p.S);
+  p.chunks = norm_grad_chunks(p.B, p.S, p.C);
   p.rows_per = std::max(1, (p.S + p.chunks - 1) / p.chunks);
   p.chunks = (p.S + p.rows_per - 1) / p.rows_per;  // 0 without rows: the sums are zeros
   const hipError_t e = p.chunks == 0 ? hipSuccess : with_shape(p.C, [&](auto w, auto np) {
@@ -399,8 +473,11 @@ hipError_t launch_norm_grad(int dtype, NormGradParams p, hipStream_t stream) {
                       : launch_kernel(norm_grad_kernel<false, W, NP>, grid, dim3(threads), 0, stream, p);
   });
   if (e != hipSuccess || p.part == nullptr) return e;
-  return launch_kernel(norm_grad_final_kernel, dim3((unsigned)((p.C + FIN_COLS - 1) / FIN_COLS)),
-                       dim3(FIN_COLS * FIN_GROUPS), 0, stream, p);
+  const hipError_t f = launch_kernel(norm_grad_final_kernel,
+                                     dim3((unsigned)((p.C + FIN_COLS - 1) / FIN_COLS), (unsigned)p.B),
+                                     dim3(FIN_COLS * FIN_GROUPS), 0, stream, p);
+  if (f != hipSuccess || p.B == 1 || (p.dweight == nullptr && p.dbias == nullptr)) return f;
+  return launch_kernel(norm_grad_entries_kernel, dim3((unsigned)((p.C + 63) / 64)), dim3(64), 0, stream, p);
 }
 
 }  // namespace refadapt

@@ -887,6 +887,7 @@ def _norm(x, weight, bias, scale, shift, eps, y=None, y_mx=None, stats=None):
         _row_words("weight", weight, pdt, (C,), dev)[0], _row_words("bias", bias, pdt, (C,), dev)[0], sc, sh,
         sc_stride, sh_stride, 0 if stats is None else stats.data_ptr())
     L.refadapt_layer_norm_packed(desc, args, _stream())
+    return desc, pdt
 
 
 def layer_norm(x, weight=None, bias=None, *, scale=None, shift=None, eps=1e-6, out=None):
@@ -919,22 +920,20 @@ class _LayerNorm(torch.autograd.Function):
         _on_gpu("x", x)
         y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         stats = torch.empty((*x.shape[:-1], 2), dtype=torch.float32, device=x.device)
-        _norm(x, weight, bias, scale, shift, eps, y=y, stats=stats)
+        ctx.desc, ctx.param_dtype = _norm(x, weight, bias, scale, shift, eps, y=y, stats=stats)
         ctx.save_for_backward(x, weight, bias, scale, stats)
-        ctx.eps, ctx.shift = eps, None if shift is None else (shift.shape, shift.dtype)
+        ctx.shapes = None if scale is None else scale.shape, None if shift is None else shift.shape
         return y
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         x, weight, bias, scale, stats = ctx.saved_tensors
-        need = ctx.needs_input_grad
-        if dy.stride(-1) != 1 or dy.dim() > 1 and dy.shape[-2] > 1 and dy.stride(-2) < dy.shape[-1]:
+        st = dy.stride()
+        if st[-1] != 1 or dy.shape[-2] > 1 and st[-2] < dy.shape[-1]:
             dy = dy.clone(memory_format=torch.contiguous_format)  # a gradient comes in any layout
-        dx, dw, db, ds, dt = layer_norm_grad(dy, x, stats, weight, bias, scale=scale, eps=ctx.eps, wanted=need[:5],
-                                             param_dtype=None if ctx.shift is None else ctx.shift[1])
-        return (dx, dw, db, None if ds is None else ds.view(scale.shape),
-                None if dt is None else dt.view(ctx.shift[0]), None)
+        return (*_norm_grad(ctx.desc, ctx.param_dtype, dy, x, stats, weight, bias, scale, ctx.needs_input_grad[:5],
+                            ctx.shapes), None)
 
 
 def layer_norm_grad(dy, x, stats, weight=None, bias=None, *, scale=None, eps=1e-6, wanted=(True,) * 5,
@@ -955,12 +954,17 @@ def layer_norm_grad(dy, x, stats, weight=None, bias=None, *, scale=None, eps=1e-
         raise ValueError(f"stats must be contiguous float32 {(*shape[:-1], 2)}")
     if stats.get_device() != dev:
         _elsewhere("stats", stats, dev)
-    where = x.device
-    dx = torch.empty(shape, dtype=dt, device=where) if wanted[0] else None
-    sums = [torch.empty(s, dtype=pdt, device=where) if w else None
-            for w, s in zip(wanted[1:], ((C,), (C,), (B, C), (B, C)))]
+    return _norm_grad(desc, pdt, dy, x, stats, weight, bias, scale, wanted, ((B, C), (B, C)), workspace)
+
+
+def _norm_grad(desc, pdt, dy, x, stats, weight, bias, scale, wanted, shapes, workspace=None):
+    dev, shape, dt, where = torch._C._cuda_getDevice(), x.shape, x.dtype, x.device
+    C, B = shape[-1], shape[0] if len(shape) == 3 else 1
+    w_x, *w_params = wanted
+    dx = torch.empty(shape, dtype=dt, device=where) if w_x else None
+    sums = [torch.empty(s, dtype=pdt, device=where) if w else None for w, s in zip(w_params, ((C,), (C,), *shapes))]
     nbytes = 0
-    if any(wanted[1:]):
+    if True in w_params:
         if workspace is None:
             workspace = torch.empty(L.refadapt_layer_norm_grad_workspace_size_packed(desc), dtype=torch.uint8,
                                     device=where)
@@ -969,13 +973,13 @@ def layer_norm_grad(dy, x, stats, weight=None, bias=None, *, scale=None, eps=1e-
         nbytes = _nbytes(workspace)
     elif dx is None:
         return (None,) * 5
-    per = (C,) if len(shape) == 2 and scale is not None and scale.dim() == 1 else (B, C)
-    sc, sc_stride = _row_words("scale", scale, pdt, per, dev)
+    sc, sc_stride = (0, 0) if scale is None else _row_words(
+        "scale", scale, pdt, (C,) if len(shape) == 2 and scale.dim() == 1 else (B, C), dev)
     args = L.NORM_GRAD_ARGS_PACK.pack(
         *_rows("dy", dy, dt, shape, dev), *_rows("x", x, dt, shape, dev), *_rows("dx", dx, dt, shape, dev),
         stats.data_ptr(), _row_words("weight", weight, pdt, (C,), dev)[0], _row_words("bias", bias, pdt, (C,), dev)[0],
-        sc, sc_stride, *(0 if t is None else t.data_ptr() for t in sums), workspace.data_ptr() if nbytes else 0, nbytes)
-    if B * S or nbytes:
+        sc, sc_stride, *[0 if t is None else t.data_ptr() for t in sums], workspace.data_ptr() if nbytes else 0, nbytes)
+    if nbytes or x.numel():
         L.refadapt_layer_norm_grad_packed(desc, args, _stream())
     return dx, *sums
 
