@@ -218,7 +218,7 @@ struct LinearParams {
   int32_t N, K, rows;
   int32_t parts;   // planes of x that add up to it (fp32 values as three bf16 terms)
   int64_t x_part;  // bytes from one to the next
-  int32_t tiles_m;  // set by the launcher
+  int32_t tiles_m, tiles_n;  // set by the launcher
   View x_plain;     // rows that the kernel for few rows rounds itself (batch entries of x_rows), or null p: x and xs
   int32_t x_rows;
   bool x_f32;
