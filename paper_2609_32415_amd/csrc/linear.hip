@@ -464,7 +464,7 @@ struct RowsIn {
 // their sums are joined in order. Bound by the weights' bytes, which go from memory to registers two chunks ahead; a
 // row costs every workgroup its turn into LDS (about 0.1 ns an element). Measured: 1 row x 4096 -> 24576 in 8 and 4 bits
 // 12.9 us (4.1 TB/s; 17.4 with 64 outputs a workgroup), x 1536 -> 4608 3.9; 32 rows of that 9.0 (tiles, and the rounding
-// in a launch of its own: 13.3).
+// in a launch of its own: 11.2).
 template <int KX, int KW, int LDS, int XP>
 __global__ __launch_bounds__(64 * FEW_WAVES) void linear_few_kernel(LinearParams p) {
   constexpr int KC = KW == FP4 ? 256 : 128, STEPS = KC / 64, ND = KC / 128;
@@ -740,7 +740,8 @@ int64_t few_bytes(int x_kind, int64_t M, int32_t K) {
 // Explicit: reached only through a launcher's kernel pointer, the host pass would leave their launch stubs out.
 #define RA_LINEAR_TILES(KX, KW)                                                \
   template __global__ void linear_kernel<KX, KW, 256, 256, 2, 4>(LinearParams); \
-  template __global__ void linear_kernel<KX, KW, 128, 128, 2, 2>(LinearParams);
+  template __global__ void linear_kernel<KX, KW, 128, 128, 2, 2>(LinearParams); \
+  template __global__ void linear_kernel<KX, KW, 64, 64, 2, 1>(LinearParams);
 RA_LINEAR_TILES(FP4, FP4)
 RA_LINEAR_TILES(FP4, FP8)
 RA_LINEAR_TILES(FP8, FP4)
@@ -784,13 +785,17 @@ hipError_t run_few(const LinearParams& p, hipStream_t stream) {
 
 // Tiles of 256 x 256 on workgroups of 8 wavefronts, one a CU, move half the bytes a product needs with tiles of 128 x 128
 // on 4 wavefronts, two a CU, and a round of them does twice the work in 1.45 times the time; a last round that leaves the
-// CUs' second place empty takes less. Measured, in us, 256 against 128: 16384 x 2048 -> 8192 in 4 bits 180 / 243, in 8
-// and 4 262 / 370; 4352 x 4096 -> 12288 135 / 153; 2048 x 2048 -> 6144 in 8 and 4 28 / 33; 4352 x 2048 -> 4096 in 4 bits
-// 37 / 33, in 8 and 4 54 / 47; 1024 x 2048 -> 4096 18 / 10. (256 x 128 and 128 x 256 on 8 wavefronts lie between.)
+// CUs' second place empty takes less. Measured, in us, 256 against 128: 16384 x 2048 -> 8192 in 4 bits 166 / 197, in 8
+// and 4 241 / 277; 4352 x 4096 -> 12288 131 / 145; 2048 x 2048 -> 6144 in 8 and 4 26 / 30; 4352 x 2048 -> 4096 in 4 bits
+// 38 / 31, in 8 and 4 54 / 45; 1024 x 2048 -> 4096 25 / 12. (256 x 128 and 128 x 256 on 8 wavefronts lie between.)
+// Tiles of 64 x 64 on 2 wavefronts where no CU has more than three: less work a stage, and more CUs read the weights. 64
+// against 128, 8 and 4 bits: 61 x 1536 -> 4608 7.1 / 10.5, 131 x 1536 -> 1152 6.1 / 8.9, 64 x 8192 -> 2048 21 / 32, 512 x
+// 2048 -> 4096 9.5 / 11.2, 768 rows of that 10.7 / 11.8, 896 13.2 / 12.0.
 template <int KX, int KW>
 hipError_t run_linear(const LinearParams& p, hipStream_t stream) {
   const double cus = std::max(1, attn_bf16_slots(128, kAttnBf16BM).cus);
   const auto tiles = [&](int64_t t) { return (double)(((p.M + t - 1) / t) * ((p.N + t - 1) / t)); };
+  if (tiles(64) <= 3 * cus) return run_tiles<KX, KW, 64, 64, 2, 1>(p, stream);
   const double small = tiles(128) / (2 * cus), part = small - std::floor(small);
   const double small_us = std::floor(small) + (part > 0 ? 0.6 + 0.4 * part : 0.0);
   if (1.45 * std::ceil(tiles(256) / cus) < small_us) return run_tiles<KX, KW, 256, 256, 2, 4>(p, stream);
@@ -801,8 +806,9 @@ hipError_t run_linear(const LinearParams& p, hipStream_t stream) {
 
 // Few rows go to the kernel that reads the weights once and turns the rows in every workgroup, at about 0.1 ns an element
 // and round of workgroups; tiles take a launch for the rounding and walk K in stages. Measured, in us, few against tiles
-// (rounding included), 8 and 4 bits: 1 row x 512 -> 512 3.3 / 7.5, x 4096 -> 24576 12.9 / 25; 16 rows x 1536 -> 4608 6.2 /
-// 13.2, x 4096 -> 4096 12.9 / 24.3, x 4096 -> 24576 38 / 27 (tiles are taken); 32 rows x 1536 -> 4608 9.0 / 13.3.
+// (rounding included), 8 and 4 bits: 1 row x 512 -> 512 3.3 / 6.2, x 4096 -> 24576 13.1 / 20; 16 rows x 1536 -> 4608 6.3 /
+// 10.9, x 4096 -> 4096 12.0 / 18.9, x 4096 -> 24576 35 / 22 (tiles are taken); 32 rows x 1536 -> 4608 9.0 / 11.2, x 4096
+// -> 4096 19.2 / 19.3.
 bool linear_is_few(int x_kind, int64_t M, int32_t N, int32_t K) {
   if (x_kind == B16 || M > FEW_ROWS || few_bytes(x_kind, M, K) > FEW_MORE_LDS) return false;
   return (double)M * K * std::max(1.0, N / 8192.0) < 24000.0 + 31.0 * K;
