@@ -826,6 +826,9 @@ def attn_mx_workspace(q_tgt, n_ref, fmt, qset="target", kvsrc="cache", q_cached=
 # ---- around the attention: the layer norm of the hidden rows and the projections
 
 
+_DENSE = torch.contiguous_format
+
+
 def _rows(name, t, dtype, shape, dev):
     """(data pointer, batch stride, 0, row stride) of [B, S, C] rows (``shape``; [S, C] has one entry), checked."""
     if t is None:
@@ -861,22 +864,21 @@ def _row_words(name, t, dtype, shape, dev):
     return t.data_ptr(), t.stride(0) if len(shape) == 2 and shape[0] > 1 else 0
 
 
-def _norm_desc(x, params, eps, fmt=0):
-    """(packed descriptor, parameters' dtype) of rows like ``x``."""
-    B, S, C = _batch_rows("x", x.shape)
+def _norm_desc(x, sizes, params, eps, fmt=0):
+    """(packed descriptor, parameters' dtype) of rows like ``x``, whose sizes are [B, S, C]."""
     dt = x.dtype
     if dt not in _DTYPES:
         raise ValueError(f"unsupported dtype {dt}")
     pdt = next((t.dtype for t in params if t is not None), dt)
     if pdt != dt and pdt != torch.float32:
         raise ValueError(f"parameters of {pdt} for rows of {dt}: they are of the rows' dtype or float32")
-    return L.NORM_DESC_PACK.pack(B, S, C, _DTYPES[dt], _DTYPES[pdt], fmt, float(eps)), pdt
+    return L.NORM_DESC_PACK.pack(*sizes, _DTYPES[dt], _DTYPES[pdt], fmt, float(eps)), pdt
 
 
 def _norm(x, weight, bias, scale, shift, eps, y=None, y_mx=None, stats=None):
     dev, shape = torch._C._cuda_getDevice(), x.shape
-    desc, pdt = _norm_desc(x, (weight, bias, scale, shift), eps, 0 if y_mx is None else _MX[y_mx.fmt])
-    B, S, C = _batch_rows("x", shape)
+    B, S, C = sizes = _batch_rows("x", shape)
+    desc, pdt = _norm_desc(x, sizes, (weight, bias, scale, shift), eps, 0 if y_mx is None else _MX[y_mx.fmt])
     per = (C,) if len(shape) == 2 and scale is not None and scale.dim() == 1 else (B, C)
     sc, sc_stride = _row_words("scale", scale, pdt, per, dev)
     per = (C,) if len(shape) == 2 and shift is not None and shift.dim() == 1 else (B, C)
@@ -907,7 +909,7 @@ def layer_norm(x, weight=None, bias=None, *, scale=None, shift=None, eps=1e-6, o
             raise ValueError("out cannot be given where a tensor requires grad")
         return _LayerNorm.apply(x, weight, bias, scale, shift, eps)
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = torch.empty_like(x, memory_format=_DENSE)
     _norm(x, weight, bias, scale, shift, eps, y=out)
     return out
 
@@ -918,7 +920,7 @@ class _LayerNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, scale, shift, eps):
         _on_gpu("x", x)
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        y = torch.empty_like(x, memory_format=_DENSE)
         stats = torch.empty((*x.shape[:-1], 2), dtype=torch.float32, device=x.device)
         ctx.desc, ctx.param_dtype = _norm(x, weight, bias, scale, shift, eps, y=y, stats=stats)
         ctx.save_for_backward(x, weight, bias, scale, stats)
@@ -942,8 +944,8 @@ def layer_norm_grad(dy, x, stats, weight=None, bias=None, *, scale=None, eps=1e-
     where ``wanted`` says so. ``stats`` [..., 2]: float32 mean and 1 / deviation of each row. Gradients of
     parameters are of ``param_dtype`` (of the parameters given, or ``x``'s), dscale and dshift [B, C]."""
     dev, shape, dt = torch._C._cuda_getDevice(), x.shape, x.dtype
-    B, S, C = _batch_rows("x", shape)
-    desc, pdt = _norm_desc(x, (weight, bias, scale), eps)
+    B, S, C = sizes = _batch_rows("x", shape)
+    desc, pdt = _norm_desc(x, sizes, (weight, bias, scale), eps)
     if param_dtype is not None and param_dtype != pdt:
         if any(t is not None for t in (weight, bias, scale)) or param_dtype != torch.float32:
             raise ValueError(f"gradients of {param_dtype} for parameters of {pdt}")
@@ -961,8 +963,10 @@ def _norm_grad(desc, pdt, dy, x, stats, weight, bias, scale, wanted, shapes, wor
     dev, shape, dt, where = torch._C._cuda_getDevice(), x.shape, x.dtype, x.device
     C, B = shape[-1], shape[0] if len(shape) == 3 else 1
     w_x, *w_params = wanted
-    dx = torch.empty(shape, dtype=dt, device=where) if w_x else None
-    sums = [torch.empty(s, dtype=pdt, device=where) if w else None for w, s in zip(w_params, ((C,), (C,), *shapes))]
+    dx = torch.empty_like(x, memory_format=_DENSE) if w_x else None
+    sums = [None if not w else torch.empty_like(t, memory_format=_DENSE) if t is not None and t.shape == s else
+            torch.empty(s, dtype=pdt, device=where)
+            for w, t, s in zip(w_params, (weight, bias, scale, scale), ((C,), (C,), *shapes))]
     nbytes = 0
     if True in w_params:
         if workspace is None:
@@ -1008,6 +1012,9 @@ def mx_weight(w, fmt):
     out = mx_tensor((1, 1, *w.shape), fmt, w.device)
     mx_commit(_readable(w.detach()[None, None]), None, out, None)
     return out
+
+
+_MAX_ROW = 1 << 21  # bf16 elements from one row to the next that a product takes
 
 
 def _linear_desc(B, S, w, dt, fmt):
@@ -1116,7 +1123,8 @@ def mx_linear_grad(dy, w, *, wanted=(True, True), workspace=None):
     _on_gpu("dy", dy)
     st, whole = dy.stride(), n_out % 8 == 0 and dt == torch.bfloat16
     if st[-1] != 1 or S > 1 and st[-2] < N or whole and (
-            dy.data_ptr() % 16 or any(s % 8 for s in st[:-1]) or len(st) == 3 and B > 1 and S > 1 and st[0] != S * st[1]):
+            dy.data_ptr() % 16 or any(s % 8 for s in st[:-1]) or (st[-2] if S > 1 else st[0]) > _MAX_ROW or
+            len(st) == 3 and B > 1 and S > 1 and st[0] != S * st[1]):
         dy = dy.clone(memory_format=torch.contiguous_format)  # a gradient comes in any layout
     where = dy.device
     dx = torch.empty((*shape[:-1], n_in), dtype=dt, device=where) if wanted[0] else None
