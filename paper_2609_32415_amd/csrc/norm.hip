@@ -102,7 +102,7 @@ __device__ __forceinline__ void Lane<L>::store(char* p, const Oct& o, int k) con
       u32x4 w;
 #pragma unroll
       for (int i = 0; i < 4; ++i) w[i] = bf16_bits(o.f[2 * i]) | (uint32_t)bf16_bits(o.f[2 * i + 1]) << 16;
-      *reinterpret_cast<u32x4*>(p + c0 * 2) = w;
+      __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p + c0 * 2));
     } else {
       u32x4 a, b;
 #pragma unroll
@@ -361,7 +361,7 @@ __device__ __forceinline__ void put_param(void* p, bool f32, int64_t i, double v
 
 // Joins the chunks' column sums of batch entry blockIdx.y: FIN_COLS columns a workgroup, its groups of threads take chunks
 // in turn. With several entries the terms of dw and db go to `entry` [B][2][C], which a second launch adds up.
-constexpr int FIN_COLS = 32, FIN_GROUPS = 32, FIN_UNROLL = 4;
+constexpr int FIN_COLS = 16, FIN_GROUPS = 64, FIN_UNROLL = 4;
 __global__ __launch_bounds__(FIN_COLS * FIN_GROUPS) void norm_grad_final_kernel(NormGradParams p) {
   __shared__ double held[2][FIN_GROUPS][FIN_COLS];
   const int col = threadIdx.x % FIN_COLS, group = threadIdx.x / FIN_COLS;
