@@ -10,8 +10,10 @@
 // of row chunks fp64; results are rounded once. Sums run in a fixed order: outputs repeat bit for bit.
 //
 // Bound by memory: a row stays in registers between its passes, and each workgroup has the next one on its way. A large
-// copy moves 5.1 TB/s; measured in bf16: 4096 x 4096 with its modulation 16.4 us (4.1 TB/s), 16384 x 2048 with every
-// parameter 29.6 (4.5 TB/s); dx alone there 42 (4.8 TB/s), with the four sums 55.
+// copy moves 5.1 TB/s; measured in bf16, replayed from a graph: 4096 x 4096 with its modulation 14.2 us (4.7 TB/s), 16384 x
+// 2048 with every parameter 24.5 (5.5 TB/s; the rows partly in the last-level cache; 29 without); dx alone there 41.5 (4.8
+// TB/s), with the four sums 51. Rows in whole 16-byte units have kernels of their own (VEC): one kernel for both takes 16.1
+// and 28.6 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -43,25 +45,26 @@ __device__ __forceinline__ float row_sum(float v, float* slot) {
 }
 
 // The elements of a row that a lane holds, 8 a piece: piece lane + L k of the row's (`pieces`), or every L-th element, so
-// that neighbouring lanes read neighbouring elements where rows are not in whole 16-byte units (`vec` false).
-template <int L>
+// that neighbouring lanes read neighbouring elements where rows are not in whole 16-byte units (VEC false).
+template <int L, bool VEC>
 struct Lane {
   int lane, C;
-  bool vec, pieces;
+  bool pieces;
   __device__ __forceinline__ int at(int k, int i) const {
-    return pieces ? 8 * (lane + L * k) + i : 8 * L * k + L * i + lane;
+    return VEC || pieces ? 8 * (lane + L * k) + i : 8 * L * k + L * i + lane;
   }
+  __device__ __forceinline__ bool in(int k, int i) const { return at(k, VEC ? 0 : i) < C; }  // pieces are whole with VEC
   // zeros past the row's end
   template <bool BF16>
   __device__ __forceinline__ RawOct<BF16> raw(const char* p, int k) const {
     RawOct<BF16> o = {};
-    if (vec) {
-      if (at(k, 0) < C) o.load(p + at(k, 0) * (BF16 ? 2 : 4));
+    if constexpr (VEC) {
+      if (in(k, 0)) o.load(p + at(k, 0) * (BF16 ? 2 : 4));
       return o;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      if (at(k, i) < C) {
+      if (in(k, i)) {
         if constexpr (BF16)
           o.w[0][i / 2] |= (uint32_t) reinterpret_cast<const uint16_t*>(p)[at(k, i)] << (16 * (i % 2));
         else
@@ -92,11 +95,11 @@ struct Lane {
 
 __device__ __forceinline__ uint16_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 
-template <int L>
+template <int L, bool VEC>
 template <bool BF16>
-__device__ __forceinline__ void Lane<L>::store(char* p, const Oct& o, int k) const {
-  if (vec) {
-    const int c0 = at(k, 0);
+__device__ __forceinline__ void Lane<L, VEC>::store(char* p, const Oct& o, int k) const {
+  if constexpr (VEC) {  // bf16 rows past the caches (16384 x 2048: gradient 46.5 us, past them 44.7); fp32 ones are sums
+    const int c0 = at(k, 0);  // too, which are read next
     if (c0 >= C) return;
     if constexpr (BF16) {
       u32x4 w;
@@ -117,7 +120,7 @@ __device__ __forceinline__ void Lane<L>::store(char* p, const Oct& o, int k) con
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    if (at(k, i) >= C) return;
+    if (!in(k, i)) return;
     if constexpr (BF16)
       reinterpret_cast<uint16_t*>(p)[at(k, i)] = bf16_bits(o.f[i]);
     else
@@ -129,8 +132,8 @@ __device__ __forceinline__ void Lane<L>::store(char* p, const Oct& o, int k) con
 // rows of its own; NP pieces a lane. The parameters, folded to y = h p + q, stay in registers over the chunk, and the next
 // row is on its way while one is worked on. y goes out as it is or, with a format, as codes of the values
 // rounded to the rows' type (the bits that quantising y itself gives).
-template <bool BF16, int W, int NP>
-__global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS, 4) void norm_kernel(NormParams p) {
+template <bool BF16, int W, int NP, bool VEC>
+__global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS, VEC ? 4 : 2) void norm_kernel(NormParams p) {
   constexpr int ROWS = W >= 4 ? 1 : NORM_THREADS / 64 / W;  // rows of a workgroup at a time
   constexpr int L = 64 * W;
   __shared__ float slots[2][2][W];
@@ -138,7 +141,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS, 4) void norm_kernel(
   const int s0 = blockIdx.x * p.rows_per, s1 = min(p.S, s0 + p.rows_per);
   const bool pf32 = p.param_f32;
   // codes need a block of 32 elements on four neighbouring lanes, whatever the alignment
-  const Lane<L> ln{(int)(threadIdx.x % L), C, p.vec, p.vec || p.y.p == nullptr};
+  const Lane<L, VEC> ln{(int)(threadIdx.x % L), C, p.y.p == nullptr};
   constexpr int esz = BF16 ? 2 : 4;
   const char* const x = static_cast<const char*>(p.x.p) + b * p.x.sb * esz;
   int s = s0 + (int)threadIdx.x / L;
@@ -183,7 +186,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS, 4) void norm_kernel(
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         v[k].f[i] -= mean;
-        if (ln.at(k, i) < C) sq += v[k].f[i] * v[k].f[i];
+        if (ln.in(k, i)) sq += v[k].f[i] * v[k].f[i];
       }
     const float var = row_sum<W>(sq, slots[turn][1]) / (float)C;
     const float r = 1.f / sqrtf(var + p.eps);
@@ -225,7 +228,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS, 4) void norm_kernel(
 }
 
 // The same chunks. With W = 1 the workgroup's wavefronts join their column sums in shared memory.
-template <bool BF16, int W, int NP>
+template <bool BF16, int W, int NP, bool VEC>
 __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS) void norm_grad_kernel(NormGradParams p) {
   constexpr int ROWS = W >= 4 ? 1 : NORM_THREADS / 64 / W;
   constexpr int L = 64 * W;
@@ -234,7 +237,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS) void norm_grad_kerne
   const int b = blockIdx.y, C = p.C;
   const int s0 = blockIdx.x * p.rows_per, s1 = min(p.S, s0 + p.rows_per);
   const bool pf32 = p.param_f32;
-  const Lane<L> ln{(int)(threadIdx.x % L), C, p.vec, p.vec};
+  const Lane<L, VEC> ln{(int)(threadIdx.x % L), C, false};
   constexpr int esz = BF16 ? 2 : 4;
   const char* const xb = static_cast<const char*>(p.x.p) + b * p.x.sb * esz;
   const char* const gb = static_cast<const char*>(p.dy.p) + b * p.dy.sb * esz;
@@ -273,7 +276,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS) void norm_grad_kerne
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float g = gw.f[i];
-        h[k].f[i] = ln.at(k, i) < C ? (xw.f[i] - now.x) * now.y : 0.f;
+        h[k].f[i] = ln.in(k, i) ? (xw.f[i] - now.x) * now.y : 0.f;
         P[k].f[i] = fmaf(g, h[k].f[i], P[k].f[i]);
         D[k].f[i] += g;
         e[k].f[i] = g * ws[k].f[i];
@@ -360,7 +363,7 @@ __device__ __forceinline__ void put_param(void* p, bool f32, int64_t i, double v
 }
 
 // Joins the chunks' column sums of batch entry blockIdx.y: FIN_COLS columns a workgroup, its groups of threads take chunks
-// in turn. With several entries the terms of dw and db go to `entry` [B][2][C], which a second launch adds up.
+// in turn (2048 columns of 512 chunks 7.4 us; 10.8 with 32 columns, 8.6 with 8). With several entries the terms of dw and db go to `entry` [B][2][C], which a second launch adds up.
 constexpr int FIN_COLS = 16, FIN_GROUPS = 64, FIN_UNROLL = 4;
 __global__ __launch_bounds__(FIN_COLS * FIN_GROUPS) void norm_grad_final_kernel(NormGradParams p) {
   __shared__ double held[2][FIN_GROUPS][FIN_COLS];
@@ -442,20 +445,21 @@ hipError_t launch_norm(int dtype, NormParams p, hipStream_t stream) {
     constexpr int W = decltype(w)::value, NP = decltype(np)::value;
     constexpr int rows = W >= 4 ? 1 : NORM_THREADS / 64 / W, threads = W > 4 ? 64 * W : NORM_THREADS;
     // Workgroups that are at work at once, about: the parameters are read once a chunk and the next row is on its way.
-    // 4096 x 4096 16.4 us (18.9 with 2048 chunks), 2048 x 8192 22.0 (26.3), 16384 x 2048 in one piece a lane 29.6 (29.8
-    // with 1024; 38 with a workgroup a row).
-    const int64_t most = W == 4 && NP == 1 ? 2048 : 1024;
+    // bf16, us, 512 / 1024 / 2048 / 4096 chunks: 4096 x 4096 16.8 / 14.1 / 15.6 / 19.6, 2048 x 8192 15.6 / 16.9 / 20.7 /
+    // 20.7, 16384 x 2048 38.6 / 25.7 / 24.5 / 24.4, 16384 x 512 10.8 / 8.8 / 8.4 / 10.3.
+    const int64_t most = W > 4 ? 512 : W == 4 && NP == 1 ? 2048 : 1024;
     const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>(most / p.B, (p.S + rows - 1) / rows));
     p.rows_per = (int32_t)((p.S + chunks - 1) / chunks);
     const dim3 grid((unsigned)((p.S + p.rows_per - 1) / p.rows_per), (unsigned)p.B);
-    return dtype == 0 ? launch_kernel(norm_kernel<true, W, NP>, grid, dim3(threads), 0, stream, p)
-                      : launch_kernel(norm_kernel<false, W, NP>, grid, dim3(threads), 0, stream, p);
+    const auto run = [&](auto* kernel) { return launch_kernel(kernel, grid, dim3(threads), 0, stream, p); };
+    if (dtype == 0) return p.vec ? run(norm_kernel<true, W, NP, true>) : run(norm_kernel<true, W, NP, false>);
+    return p.vec ? run(norm_kernel<false, W, NP, true>) : run(norm_kernel<false, W, NP, false>);
   });
 }
 
 // A chunk's column sums cost a store and a load of 2 C values, a launch of few chunks leaves loads unhidden: 512 chunks, two
 // rows each at least, and 256 of wide rows. Measured with every gradient, 256 / 512 / 1024 chunks: 16384 x 2048 bf16
-// 76 / 55 / 63 us, 4096 x 4096 35 / 33 / 46, 2048 x 8192 31 / 43 / 62.
+// 66 / 51 / 57 us, 4096 x 4096 31 / 31 / 39, 2048 x 8192 30 / 39 / 57.
 int norm_grad_chunks(int32_t B, int32_t S, int32_t C) {
   const int64_t most = std::max<int64_t>(1, (C > 4096 ? 256 : 512) / B);
   return (int)std::max<int64_t>(1, std::min<int64_t>(most, ((int64_t)S + 1) / 2));
@@ -469,8 +473,9 @@ hipError_t launch_norm_grad(int dtype, NormGradParams p, hipStream_t stream) {
     constexpr int W = decltype(w)::value, NP = decltype(np)::value;
     constexpr int threads = W > 4 ? 64 * W : NORM_THREADS;
     const dim3 grid((unsigned)p.chunks, (unsigned)p.B);
-    return dtype == 0 ? launch_kernel(norm_grad_kernel<true, W, NP>, grid, dim3(threads), 0, stream, p)
-                      : launch_kernel(norm_grad_kernel<false, W, NP>, grid, dim3(threads), 0, stream, p);
+    const auto run = [&](auto* kernel) { return launch_kernel(kernel, grid, dim3(threads), 0, stream, p); };
+    if (dtype == 0) return p.vec ? run(norm_grad_kernel<true, W, NP, true>) : run(norm_grad_kernel<true, W, NP, false>);
+    return p.vec ? run(norm_grad_kernel<false, W, NP, true>) : run(norm_grad_kernel<false, W, NP, false>);
   });
   if (e != hipSuccess || p.part == nullptr) return e;
   const hipError_t f = launch_kernel(norm_grad_final_kernel,
