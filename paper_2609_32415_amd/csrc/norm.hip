@@ -44,31 +44,39 @@ __device__ __forceinline__ float row_sum(float v, float* slot) {
   return v;
 }
 
-// The elements of a row that a lane holds, 8 a piece: piece lane + L k of the row's (`pieces`), or every L-th element, so
-// that neighbouring lanes read neighbouring elements where rows are not in whole 16-byte units (VEC false).
+// A row's elements at any alignment of theirs: the hardware takes wide loads and stores there too.
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+
+// The elements of a row that a lane holds, 8 a piece: piece lane + L k of the row's. With VEC rows are in whole 16-byte units;
+// without, they lie at any alignment and their last piece may be a part (2 x 1009 x 1001 fp32: 8.6 us; element by element
+// 10.3).
 template <int L, bool VEC>
 struct Lane {
   int lane, C;
-  bool pieces;
-  __device__ __forceinline__ int at(int k, int i) const {
-    return VEC || pieces ? 8 * (lane + L * k) + i : 8 * L * k + L * i + lane;
-  }
-  __device__ __forceinline__ bool in(int k, int i) const { return at(k, VEC ? 0 : i) < C; }  // pieces are whole with VEC
+  __device__ __forceinline__ int at(int k, int i) const { return 8 * (lane + L * k) + i; }
+  __device__ __forceinline__ bool in(int k, int i) const { return at(k, VEC ? 0 : i) < C; }
   // zeros past the row's end
   template <bool BF16>
   __device__ __forceinline__ RawOct<BF16> raw(const char* p, int k) const {
     RawOct<BF16> o = {};
+    const int c0 = at(k, 0);
+    p += c0 * (BF16 ? 2 : 4);
     if constexpr (VEC) {
-      if (in(k, 0)) o.load(p + at(k, 0) * (BF16 ? 2 : 4));
+      if (c0 < C) o.load(p);
+      return o;
+    }
+    if (c0 + 8 <= C) {
+      o.w[0] = reinterpret_cast<const u32x4_any*>(p)[0];
+      if constexpr (!BF16) o.w[1] = reinterpret_cast<const u32x4_any*>(p)[1];
       return o;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (in(k, i)) {
+    for (int i = 0; i < 7; ++i) {
+      if (c0 + i < C) {
         if constexpr (BF16)
-          o.w[0][i / 2] |= (uint32_t) reinterpret_cast<const uint16_t*>(p)[at(k, i)] << (16 * (i % 2));
+          o.w[0][i / 2] |= (uint32_t) reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i % 2));
         else
-          o.w[i / 4][i % 4] = reinterpret_cast<const uint32_t*>(p)[at(k, i)];
+          o.w[i / 4][i % 4] = reinterpret_cast<const uint32_t*>(p)[i];
       }
     }
     return o;
@@ -98,33 +106,33 @@ __device__ __forceinline__ uint16_t bf16_bits(float x) { return __builtin_bit_ca
 template <int L, bool VEC>
 template <bool BF16>
 __device__ __forceinline__ void Lane<L, VEC>::store(char* p, const Oct& o, int k) const {
-  if constexpr (VEC) {  // bf16 rows past the caches (16384 x 2048: gradient 46.5 us, past them 44.7); fp32 ones are sums
-    const int c0 = at(k, 0);  // too, which are read next
-    if (c0 >= C) return;
-    if constexpr (BF16) {
-      u32x4 w;
+  const int c0 = at(k, 0);
+  p += c0 * (BF16 ? 2 : 4);
+  if (VEC ? c0 < C : c0 + 8 <= C) {
+    u32x4 w[BF16 ? 1 : 2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = bf16_bits(o.f[2 * i]) | (uint32_t)bf16_bits(o.f[2 * i + 1]) << 16;
-      __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p + c0 * 2));
+    for (int i = 0; i < (BF16 ? 4 : 8); ++i) {
+      if constexpr (BF16)
+        w[0][i] = bf16_bits(o.f[2 * i]) | (uint32_t)bf16_bits(o.f[2 * i + 1]) << 16;
+      else
+        w[i / 4][i % 4] = __float_as_uint(o.f[i]);
+    }
+    if constexpr (BF16 && VEC) {  // past the caches (gradient of 16384 x 2048 46.5 us, past them 44.7); fp32 rows are sums
+      __builtin_nontemporal_store(w[0], reinterpret_cast<u32x4*>(p));  // too, which are read next
     } else {
-      u32x4 a, b;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        a[i] = __float_as_uint(o.f[i]);
-        b[i] = __float_as_uint(o.f[4 + i]);
-      }
-      reinterpret_cast<u32x4*>(p + c0 * 4)[0] = a;
-      reinterpret_cast<u32x4*>(p + c0 * 4)[1] = b;
+      reinterpret_cast<u32x4_any*>(p)[0] = w[0];
+      if constexpr (!BF16) reinterpret_cast<u32x4_any*>(p)[1] = w[1];
     }
     return;
   }
+  if constexpr (VEC) return;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (!in(k, i)) return;
+  for (int i = 0; i < 7; ++i) {
+    if (c0 + i >= C) return;
     if constexpr (BF16)
-      reinterpret_cast<uint16_t*>(p)[at(k, i)] = bf16_bits(o.f[i]);
+      reinterpret_cast<uint16_t*>(p)[i] = bf16_bits(o.f[i]);
     else
-      reinterpret_cast<float*>(p)[at(k, i)] = o.f[i];
+      reinterpret_cast<float*>(p)[i] = o.f[i];
   }
 }
 
@@ -133,15 +141,14 @@ __device__ __forceinline__ void Lane<L, VEC>::store(char* p, const Oct& o, int k
 // row is on its way while one is worked on. y goes out as it is or, with a format, as codes of the values
 // rounded to the rows' type (the bits that quantising y itself gives).
 template <bool BF16, int W, int NP, bool VEC>
-__global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS, VEC ? 4 : 2) void norm_kernel(NormParams p) {
+__global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS, 4) void norm_kernel(NormParams p) {
   constexpr int ROWS = W >= 4 ? 1 : NORM_THREADS / 64 / W;  // rows of a workgroup at a time
   constexpr int L = 64 * W;
   __shared__ float slots[2][2][W];
   const int b = blockIdx.y, C = p.C;
   const int s0 = blockIdx.x * p.rows_per, s1 = min(p.S, s0 + p.rows_per);
   const bool pf32 = p.param_f32;
-  // codes need a block of 32 elements on four neighbouring lanes, whatever the alignment
-  const Lane<L, VEC> ln{(int)(threadIdx.x % L), C, p.y.p == nullptr};
+  const Lane<L, VEC> ln{(int)(threadIdx.x % L), C};
   constexpr int esz = BF16 ? 2 : 4;
   const char* const x = static_cast<const char*>(p.x.p) + b * p.x.sb * esz;
   int s = s0 + (int)threadIdx.x / L;
@@ -237,7 +244,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS) void norm_grad_kerne
   const int b = blockIdx.y, C = p.C;
   const int s0 = blockIdx.x * p.rows_per, s1 = min(p.S, s0 + p.rows_per);
   const bool pf32 = p.param_f32;
-  const Lane<L, VEC> ln{(int)(threadIdx.x % L), C, false};
+  const Lane<L, VEC> ln{(int)(threadIdx.x % L), C};
   constexpr int esz = BF16 ? 2 : 4;
   const char* const xb = static_cast<const char*>(p.x.p) + b * p.x.sb * esz;
   const char* const gb = static_cast<const char*>(p.dy.p) + b * p.dy.sb * esz;

@@ -166,3 +166,36 @@ def test_two_calls_at_once():
     torch.cuda.synchronize()
     for i in range(2):
         assert all(torch.equal(a, want[i]) and torch.equal(b, n[i]) for a, b in got[i])
+
+
+@pytest.mark.parametrize("dtype,pdtype", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("C", [9, 511, 513, 1023, 1999, 3001, 5003, 9001, 16383])
+def test_norm_of_odd_widths(C, dtype, pdtype):
+    """Rows at every alignment that end inside a lane's piece; what lies between and around them stays."""
+    x, p, dy = _case(C, 2, 5, C, dtype, pdtype, True, True)
+    for pad in (1, 2):
+        around = torch.full((2, 7, C + pad), 7.0, dtype=x.dtype, device="cuda:0")
+        out = around[:, 1:-1, :-pad]
+        print("odd width", C, dtype, pdtype, pad, flush=True)
+        with torch.no_grad():
+            _check_norm(ops.layer_norm(x, **p, out=out), x, p)
+        out.fill_(7.0)
+        assert (around == 7.0).all()
+    leaves = [t.requires_grad_() for t in (x, *p.values())]
+    got = torch.autograd.grad(ops.layer_norm(x, **p), leaves, dy)
+    d = [t.detach().double().requires_grad_() for t in leaves]
+    h = (d[0] - d[0].mean(-1, keepdim=True)) / (d[0].var(-1, correction=0, keepdim=True) + 1e-6).sqrt()
+    y = (h * d[1] + d[2]) * (1 + d[3][:, None]) + d[4][:, None]
+    for a, b in zip(got, torch.autograd.grad(y, d, dy.double())):
+        # rms: the roundings of h (64 u of a few times its size), of the sums' terms and of the result
+        assert float((a.double() - b).norm() / b.norm()) <= 64 * U + HALF[a.dtype]
+
+
+def test_codes_of_rows_at_odd_addresses():
+    for dtype, pad in (("bf16", 1), ("f32", 3)):
+        x, p, _ = _case(8, 2, 5, 2080, dtype, dtype, True, True)
+        odd = torch.empty((2, 5, 2080 + pad), dtype=x.dtype, device="cuda:0")[..., pad:]
+        odd.copy_(x)
+        for fmt in ("mxfp4", "mxfp8"):
+            a, b = ops.layer_norm_mx(odd, fmt, **p), ops.layer_norm_mx(x, fmt, **p)
+            assert torch.equal(a.codes, b.codes) and torch.equal(a.scales, b.scales)
