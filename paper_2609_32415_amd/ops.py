@@ -1042,8 +1042,9 @@ def _linear_workspace(nbytes, workspace, where, dev):
 def mx_linear(x, w, bias=None, *, fmt=None, dtype=None, out=None, workspace=None):
     """The projection Q(x) w^T + bias through ``refadapt_mx_linear``.
 
-    ``x``: rows [B, S, n_in] or [S, n_in], rounded to codes of ``fmt`` (default: ``w``'s) on the way, or an ``MxTensor``
-    [B, 1, S, n_in] (``layer_norm_mx``), whose result is [B, S, n_out] of ``dtype`` (default: bias's, or bfloat16).
+    ``x``: rows [B, S, n_in] or [S, n_in] in whole 16-byte units, rounded to codes of ``fmt`` (default: ``w``'s) on the
+    way, or an ``MxTensor`` [B, 1, S, n_in] (``layer_norm_mx``), whose result is [B, S, n_out] of ``dtype`` (default:
+    bias's, or bfloat16).
     ``w``: an ``MxTensor`` [1, 1, n_out, n_in] (``mx_weight``), or rows of one. ``bias`` [n_out] is of the result's
     dtype. ``out`` may be any rows with contiguous elements, a slice of a larger tensor too.
 
@@ -1082,7 +1083,7 @@ def _linear(x, w, bias, fmt, dt, sizes, lead, out=None, workspace=None):
     if not where.type == "cuda":
         _on_gpu("x", x.codes if mx else x)
     if out is None:
-        out = torch.empty((*lead, n_out), dtype=dt, device=where)
+        out = x.codes.new_empty((*lead, n_out), dtype=dt) if mx else x.new_empty((*lead, n_out))
     ws, held = _linear_workspace(L.refadapt_mx_linear_workspace_size_packed(desc, mx), workspace, where, dev)
     args = L.LINEAR_ARGS_PACK.pack(
         *(_NO_TENSOR if mx else _rows("x", x, dt, x.shape, dev)),
