@@ -515,8 +515,8 @@ typedef struct {
  * strides, batch entries apart); otherwise what is written overlaps nothing else.
  * A row with a NaN or an infinity is NaN throughout and touches no other row.
  * Errors: RA_EINVAL (null desc, args or tensors, both of y and y_mx, sizes, dtypes,
- * eps, negative or overlapping strides, x broadcast over the batch and normalised in
- * place), RA_EUNSUPPORTED (width above 16384, or not a multiple of 32 with y_mx,
+ * eps, negative or overlapping strides, y over a part of x, x broadcast over the batch
+ * and normalised in place), RA_EUNSUPPORTED (width above 16384, or not a multiple of 32 with y_mx,
  * alignment, batch above 65535, 2^31 or more rows).
  */
 ra_status refadapt_layer_norm(const ra_norm_desc* desc, const ra_norm_args* args, void* stream);
@@ -546,7 +546,8 @@ typedef struct {
  * itself. Without rows the sums are zeros. A scale shared over the batch
  * (scale_stride 0) still has one gradient per entry. The workspace needs no
  * initialisation and must not be used by another call that runs concurrently.
- * Errors: as refadapt_layer_norm; RA_EINVAL (no gradient wanted, null stats);
+ * Errors: as refadapt_layer_norm; RA_EINVAL (no gradient wanted, null stats, dx over a
+ * part of x or dy);
  * RA_EWORKSPACE (missing or smaller workspace).
  */
 size_t refadapt_layer_norm_grad_workspace_size(const ra_norm_desc* desc);
@@ -586,7 +587,7 @@ typedef struct {
  * The workspace needs no initialisation and must not be used by another call that runs
  * concurrently; y overlaps nothing.
  * Errors: RA_EINVAL (null desc, args or tensors, both of x and x_mx, sizes, enums,
- * strides), RA_EUNSUPPORTED (n_in not a multiple of 32, alignment, rows of x_mx not
+ * strides, y over x), RA_EUNSUPPORTED (n_in not a multiple of 32, alignment, rows of x_mx not
  * evenly spaced over the batch, rows longer or further apart than 4 MiB, batch above
  * 65535, 2^32 or more elements of x or of y in rows of whole eights), RA_EWORKSPACE.
  */
@@ -612,7 +613,7 @@ typedef struct {
  * to dtype, and deterministic. Where dtype is RA_BF16 and n_out a multiple of 8, rows
  * of dy lie in whole 16-byte units and evenly over the batch. Without rows dbias is
  * zeros. desc->x_format is not read beyond its check.
- * Errors: as refadapt_mx_linear; RA_EINVAL (no gradient wanted).
+ * Errors: as refadapt_mx_linear; RA_EINVAL (no gradient wanted, dx over dy).
  */
 size_t refadapt_mx_linear_grad_workspace_size(const ra_linear_desc* desc);
 ra_status refadapt_mx_linear_grad(const ra_linear_desc* desc, const ra_linear_grad_args* args, void* stream);

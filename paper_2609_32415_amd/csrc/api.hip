@@ -864,6 +864,41 @@ ra_status check_rows_out(const char* who, const char* name, const ra_tensor& t, 
   return RA_OK;
 }
 
+// Whether rows y of wy elements share elements with rows x of wx of the same type: slices of one buffer whose rows or
+// entries lie between each other's do not, rows at other strides do where their entries' ranges meet.
+bool rows_overlap(const ra_tensor& y, int32_t wy, const ra_tensor& x, int32_t wx, int dtype, int32_t batch,
+                  int32_t rows) {
+  const int64_t size = dtype == RA_BF16 ? 2 : 4;
+  const int64_t span_y = (rows - 1) * y.stride_s + wy, span_x = (rows - 1) * x.stride_s + wx;
+  const int64_t apart = (reinterpret_cast<intptr_t>(y.data) - reinterpret_cast<intptr_t>(x.data)) / size;
+  const int64_t last_y = apart + (batch > 1 ? (batch - 1) * y.stride_b : 0), last_x = batch > 1 ? (batch - 1) * x.stride_b : 0;
+  if (last_y + span_y <= 0 || apart >= last_x + span_x) return false;
+  const auto floor_div = [](int64_t a, int64_t b) { return a / b - (a % b < 0 ? 1 : 0); };
+  for (int32_t by = 0; by < batch; ++by) {
+    const int64_t y0 = apart + by * y.stride_b;
+    int64_t first = 0, last = batch - 1;  // the entries of x that start ahead of y's end and end behind its start
+    if (batch == 1 || x.stride_b == 0) {
+      last = 0;
+    } else {
+      first = std::max(first, floor_div(y0 - span_x, x.stride_b) + 1);
+      last = std::min(last, floor_div(y0 + span_y - 1, x.stride_b));
+    }
+    for (int64_t bx = first; bx <= last; ++bx) {
+      const int64_t d = y0 - (batch > 1 ? bx * x.stride_b : 0);
+      if (d + span_y <= 0 || d >= span_x) continue;
+      if (rows == 1 || y.stride_s != x.stride_s) return true;
+      const int64_t k = floor_div(d, y.stride_s), r = d - k * y.stride_s;  // y's row 0 starts r elements into x's row k
+      if ((r < wx && std::abs(k) < rows) || (r + wy > y.stride_s && std::abs(k + 1) < rows)) return true;
+    }
+  }
+  return false;
+}
+
+// y takes x's own place.
+bool in_place(const ra_tensor& y, const ra_tensor& x, int32_t batch, int32_t rows) {
+  return y.data == x.data && (batch == 1 || y.stride_b == x.stride_b) && (rows == 1 || y.stride_s == x.stride_s);
+}
+
 ra_status check_vector(const char* who, const char* name, const void* p, int dtype) {
   if (reinterpret_cast<uintptr_t>(p) % (dtype == RA_BF16 ? 2 : 4) != 0)
     return fail(RA_EUNSUPPORTED, "%s: %s is not aligned to its elements", who, name);
@@ -923,6 +958,9 @@ ra_status refadapt_layer_norm(const ra_norm_desc* desc, const ra_norm_args* args
   }
   if (a.y.data == a.x.data && d.batch > 1 && a.x.stride_b == 0)
     return fail(RA_EINVAL, "layer_norm: x is broadcast and cannot be normalised in place");
+  if (!mx && !in_place(a.y, a.x, d.batch, d.rows) &&
+      rows_overlap(a.y, d.width, a.x, d.width, d.dtype, d.batch, d.rows))
+    return fail(RA_EINVAL, "layer_norm: y overlaps x and is not in its place");
   if (a.scale_stride < 0 || a.shift_stride < 0) return fail(RA_EINVAL, "layer_norm: negative stride of scale or shift");
   const void* const params[4] = {a.weight, a.bias, a.scale, a.shift};
   const int64_t strides[4] = {0, 0, a.scale_stride, a.shift_stride};
@@ -979,6 +1017,10 @@ ra_status refadapt_layer_norm_grad(const ra_norm_desc* desc, const ra_norm_grad_
     if (d.batch > 1 && a.dx.data && ((a.dx.data == a.x.data && a.x.stride_b == 0) ||
                                      (a.dx.data == a.dy.data && a.dy.stride_b == 0)))
       return fail(RA_EINVAL, "%s: a broadcast tensor cannot be replaced by its gradient", who);
+    for (const ra_tensor* t : {&a.x, &a.dy})
+      if (a.dx.data && !in_place(a.dx, *t, d.batch, d.rows) &&
+          rows_overlap(a.dx, d.width, *t, d.width, d.dtype, d.batch, d.rows))
+        return fail(RA_EINVAL, "%s: dx overlaps %s and is not in its place", who, t == &a.x ? "x" : "dy");
     if (a.stats == nullptr) return fail(RA_EINVAL, "%s: null stats", who);
     p.vec = p.vec && in_units(a.dy, d.dtype) && in_units(a.x, d.dtype) && (!a.dx.data || in_units(a.dx, d.dtype));
   }
@@ -1167,6 +1209,8 @@ ra_status refadapt_mx_linear(const ra_linear_desc* desc, const ra_linear_args* a
   if ((s = check_vector(who, "bias", a.bias, d.dtype)) != RA_OK) return s;
   const LinearSpace space = linear_space(d, x_mx);
   if ((s = check_workspace(who, a.workspace, a.workspace_bytes, space.total())) != RA_OK) return s;
+  if (!x_mx && rows_overlap(a.y, d.n_out, a.x, d.n_in, d.dtype, d.batch, d.rows))
+    return fail(RA_EINVAL, "%s: y overlaps x", who);
 
   hipStream_t st = static_cast<hipStream_t>(stream);
   uint8_t* ws = static_cast<uint8_t*>(a.workspace);
@@ -1270,6 +1314,8 @@ ra_status refadapt_mx_linear_grad(const ra_linear_desc* desc, const ra_linear_gr
   if ((s = check_vector(who, "dbias", a.dbias, d.dtype)) != RA_OK) return s;
   const LinearGradSpace space = linear_grad_space(d);
   if ((s = check_workspace(who, a.workspace, a.workspace_bytes, space.total())) != RA_OK) return s;
+  if (a.dx.data && d.rows > 0 && rows_overlap(a.dx, d.n_in, a.dy, d.n_out, d.dtype, d.batch, d.rows))
+    return fail(RA_EINVAL, "%s: dx overlaps dy", who);
   hipStream_t st = static_cast<hipStream_t>(stream);
   uint8_t* const ws = static_cast<uint8_t*>(a.workspace);
   const int64_t M = (int64_t)d.batch * d.rows;

@@ -199,3 +199,24 @@ def test_codes_of_rows_at_odd_addresses():
         for fmt in ("mxfp4", "mxfp8"):
             a, b = ops.layer_norm_mx(odd, fmt, **p), ops.layer_norm_mx(x, fmt, **p)
             assert torch.equal(a.codes, b.codes) and torch.equal(a.scales, b.scales)
+
+
+def test_slices_of_one_buffer():
+    """Rows, columns and entries of one buffer that lie between each other's, as rows and as results."""
+    x, p, dy = _case(11, 2, 6, 128, "bf16", "bf16", True, True)
+    want, w = ops.layer_norm(x, **p), _weights(np.random.default_rng(1), 128, 128, "mxfp4")[0]
+    product = ops.mx_linear(x, w)
+    shapes = [lambda b: (b[..., :128], b[..., 128:256]), lambda b: (b[:, :6, :128], b[:, 6:, :128]),
+              lambda b: (b[:, ::2, :128], b[:, 1::2, :128]), lambda b: (b[:, 1::2, 128:256], b[:, ::2, :128])]
+    for cut in shapes:
+        for call, result in ((lambda i, o: ops.layer_norm(i, **p, out=o), want), (lambda i, o: ops.mx_linear(i, w, out=o), product)):
+            buf = torch.zeros((2, 12, 256), dtype=torch.bfloat16, device="cuda:0")
+            src, dst = cut(buf)
+            src, dst = src[:, :6], dst[:, :6]
+            src.copy_(x)
+            call(src, dst)
+            assert torch.equal(dst, result) and torch.equal(src, x)
+    with pytest.raises(RuntimeError, match="overlaps"):
+        ops.layer_norm(x[:, :5], **p, out=x[:, 1:])
+    with pytest.raises(RuntimeError, match="overlaps"):
+        ops.mx_linear(x, w, out=x)
