@@ -854,44 +854,58 @@ ra_status check_rows(const char* who, const char* name, const ra_tensor& t, int 
   return RA_OK;
 }
 
+int64_t floor_div(int64_t a, int64_t b) { return a / b - (a % b < 0 ? 1 : 0); }
+
+// Whether rows of wy elements, the first of them d elements behind that of rows of wx elements, share elements with those.
+// Rows at other strides do where the ranges meet.
+bool entries_overlap(int64_t d, int32_t wy, int64_t y_s, int32_t wx, int64_t x_s, int32_t rows) {
+  if (d + (rows - 1) * y_s + wy <= 0 || d >= (rows - 1) * x_s + wx) return false;
+  if (y_s != x_s) return true;
+  const int64_t k = floor_div(d, y_s), r = d - k * y_s;  // the first row starts r elements into the other's row k
+  return (r < wx && std::abs(k) < rows) || (r + wy > y_s && std::abs(k + 1) < rows);
+}
+
+// Whether rows y of wy elements share elements with rows x of wx of the same type. Slices of one buffer, at the same
+// strides, whose rows or entries lie between each other's do not; rows at other strides do where their entries' ranges meet.
+bool rows_overlap(const ra_tensor& y, int32_t wy, const ra_tensor& x, int32_t wx, int dtype, int32_t batch,
+                  int32_t rows) {
+  const int64_t apart = (reinterpret_cast<intptr_t>(y.data) - reinterpret_cast<intptr_t>(x.data)) / (dtype == RA_BF16 ? 2 : 4);
+  const int64_t y_b = batch > 1 ? y.stride_b : 0, x_b = batch > 1 ? x.stride_b : 0;
+  const int64_t y_s = rows > 1 ? y.stride_s : wy + wx, x_s = rows > 1 ? x.stride_s : y_s;
+  const int64_t span_y = (rows - 1) * y_s + wy, span_x = (rows - 1) * x_s + wx;
+  const auto entries = [&](int64_t d) { return entries_overlap(d, wy, y_s, wx, x_s, rows); };
+  if (apart + (batch - 1) * y_b + span_y <= 0 || apart >= (batch - 1) * x_b + span_x) return false;
+  if (y_b == x_b) {
+    for (int64_t b = 1 - batch; b < batch; ++b)
+      if (entries(apart + b * y_b)) return true;
+    return false;
+  }
+  for (int64_t b = 0; b < batch; ++b) {
+    const int64_t y0 = apart + b * y_b;  // the entries of x that start ahead of y's end and end behind its start
+    const int64_t first = x_b == 0 ? 0 : std::max<int64_t>(0, floor_div(y0 - span_x, x_b) + 1);
+    const int64_t last = x_b == 0 ? 0 : std::min<int64_t>(batch - 1, floor_div(y0 + span_y - 1, x_b));
+    if (last - first > 64) return true;  // entries inside each other at two strides
+    for (int64_t i = first; i <= last; ++i)
+      if (entries(y0 - i * x_b)) return true;
+  }
+  return false;
+}
+
+bool entries_apart(int64_t stride_b, int64_t stride_s, int32_t width, int32_t batch, int32_t rows) {
+  const int64_t row = rows > 1 ? stride_s : 2 * (int64_t)width, span = (rows - 1) * row + width;
+  for (int64_t b = 1; b < batch && b * stride_b < span; ++b)
+    if (stride_b < width || entries_overlap(b * stride_b, width, row, width, row, rows)) return false;
+  return true;
+}
+
 // A tensor that is written: its batch entries lie apart.
 ra_status check_rows_out(const char* who, const char* name, const ra_tensor& t, int dtype, int32_t batch, int32_t rows,
                          int32_t width) {
   const ra_status s = check_rows(who, name, t, dtype, rows, width);
   if (s != RA_OK) return s;
-  if (batch > 1 && t.stride_b < width)
+  if (!entries_apart(t.stride_b, t.stride_s, width, batch, rows))
     return fail(RA_EINVAL, "%s: batch entries of %s overlap", who, name);
   return RA_OK;
-}
-
-// Whether rows y of wy elements share elements with rows x of wx of the same type: slices of one buffer whose rows or
-// entries lie between each other's do not, rows at other strides do where their entries' ranges meet.
-bool rows_overlap(const ra_tensor& y, int32_t wy, const ra_tensor& x, int32_t wx, int dtype, int32_t batch,
-                  int32_t rows) {
-  const int64_t size = dtype == RA_BF16 ? 2 : 4;
-  const int64_t span_y = (rows - 1) * y.stride_s + wy, span_x = (rows - 1) * x.stride_s + wx;
-  const int64_t apart = (reinterpret_cast<intptr_t>(y.data) - reinterpret_cast<intptr_t>(x.data)) / size;
-  const int64_t last_y = apart + (batch > 1 ? (batch - 1) * y.stride_b : 0), last_x = batch > 1 ? (batch - 1) * x.stride_b : 0;
-  if (last_y + span_y <= 0 || apart >= last_x + span_x) return false;
-  const auto floor_div = [](int64_t a, int64_t b) { return a / b - (a % b < 0 ? 1 : 0); };
-  for (int32_t by = 0; by < batch; ++by) {
-    const int64_t y0 = apart + by * y.stride_b;
-    int64_t first = 0, last = batch - 1;  // the entries of x that start ahead of y's end and end behind its start
-    if (batch == 1 || x.stride_b == 0) {
-      last = 0;
-    } else {
-      first = std::max(first, floor_div(y0 - span_x, x.stride_b) + 1);
-      last = std::min(last, floor_div(y0 + span_y - 1, x.stride_b));
-    }
-    for (int64_t bx = first; bx <= last; ++bx) {
-      const int64_t d = y0 - (batch > 1 ? bx * x.stride_b : 0);
-      if (d + span_y <= 0 || d >= span_x) continue;
-      if (rows == 1 || y.stride_s != x.stride_s) return true;
-      const int64_t k = floor_div(d, y.stride_s), r = d - k * y.stride_s;  // y's row 0 starts r elements into x's row k
-      if ((r < wx && std::abs(k) < rows) || (r + wy > y.stride_s && std::abs(k + 1) < rows)) return true;
-    }
-  }
-  return false;
 }
 
 // y takes x's own place.
@@ -951,7 +965,8 @@ ra_status refadapt_layer_norm(const ra_norm_desc* desc, const ra_norm_args* args
   if ((s = check_rows("layer_norm", "x", a.x, d.dtype, d.rows, d.width)) != RA_OK) return s;
   if (mx) {
     if ((s = check_mx("y_mx", a.y_mx, d.format, d.rows, d.width)) != RA_OK) return s;
-    if (d.batch > 1 && (a.y_mx.stride_b < d.width / 2 || a.y_mx.scale_stride_b < d.width / 32))
+    if (!entries_apart(a.y_mx.stride_b, a.y_mx.stride_s, d.width / (d.format == RA_MXFP4 ? 2 : 1), d.batch, d.rows) ||
+        !entries_apart(a.y_mx.scale_stride_b, a.y_mx.scale_stride_s, d.width / 32, d.batch, d.rows))
       return fail(RA_EINVAL, "layer_norm: batch entries of y_mx overlap");
   } else if ((s = check_rows_out("layer_norm", "y", a.y, d.dtype, d.batch, d.rows, d.width)) != RA_OK) {
     return s;

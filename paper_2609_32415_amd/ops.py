@@ -899,7 +899,8 @@ def layer_norm(x, weight=None, bias=None, *, scale=None, shift=None, eps=1e-6, o
     ``weight``, ``bias`` [C] and the modulation ``scale``, ``shift`` [B, C] (for [S, C] rows [C] too; rows of a larger
     tensor will do) are each optional, and all of ``x``'s dtype or all float32. ``out=x`` works in place.
 
-    Where gradients are recorded and a tensor requires them the result carries them; ``out`` is refused then.
+    Where gradients are recorded and a tensor requires them the result carries them; ``out`` is refused then. A backward
+    pass is captured into a graph with no eager graph of the same leaves alive.
     """
     if torch.is_grad_enabled() and (
             x.requires_grad or weight is not None and weight.requires_grad or bias is not None and bias.requires_grad or

@@ -33,6 +33,15 @@ def test_parts_are_refused(y):
     assert st == L.RA_EINVAL and "overlaps dy" in err
 
 
+@pytest.mark.parametrize("sb,ss,fits", [(512, 256, False), (255, 4096, False), (256, 512, True), (256 * 10, 256, True),
+                                        (256 * 9, 256, False), (300, 512, False), (512, 1024, True)])
+def test_entries_inside_each_other(sb, ss, fits):
+    if fits and torch.cuda.is_available():
+        pytest.skip("made-up addresses that would be launched")
+    st, err = _norm(x=_t(0x100, 1 << 14), y=_t(HERE, sb, ss))
+    assert ("batch entries of y overlap" in err) == (not fits), err
+
+
 def test_products_are_never_in_place():
     x = _t(HERE, 40 * 256)
     for y in (x, _t(HERE + 512, 40 * 256)):
@@ -51,11 +60,24 @@ def test_random_slices():
         batch, rows, width = rng.choice((1, 2, 3)), rng.choice((1, 2, 5)), rng.choice((8, 24))
         ss = rng.choice((width, 2 * width, 3 * width + 8))
         sb = rng.choice((ss * rows, 2 * ss * rows, 3 * ss * rows + 16))
+        if rng.random() < 0.2:  # entries inside each other
+            sb, ss = ss, batch * ss
         kw = dict(batch=batch, rows=rows, width=width)
-        x = _t(HERE, sb, ss)
+        x = _t(HERE, sb * rng.choice((1, 1, 1, 2)), ss)
         y = _t(HERE + 2 * rng.choice((width, ss, ss * rows, 1, 8)) * rng.randint(-4, 4), sb, ss)
-        want = _overlaps(y, x, batch, rows, width, width) and y.data != x.data
+        in_place = y.data == x.data and (batch == 1 or x.stride_b == sb)
+        want = _overlaps(y, x, batch, rows, width, width) and not in_place
         st, err = _norm(x=x, y=y, **kw)
         assert (st == L.RA_EINVAL and "overlaps x" in err) == want, (batch, rows, width, sb, ss, y.data - HERE)
         seen[want] += 1
     assert min(seen) > 200
+
+
+def test_many_entries_take_no_time():
+    """65535 entries inside each other: columns of one buffer, and entries at two strides (refused)."""
+    n = 65535
+    x = _t(HERE, 512, n * 512)
+    assert _norm(x=x, y=_t(HERE + 2, 512, n * 512), batch=n, rows=4)[0] == L.RA_EINVAL
+    assert _norm(x=x, y=_t(HERE + 2, 1024, n * 512), batch=n, rows=4)[0] == L.RA_EINVAL
+    if not torch.cuda.is_available():
+        assert _norm(x=x, y=_t(HERE + 512, 512, n * 512), batch=n, rows=4)[0] not in (L.RA_OK, L.RA_EINVAL)  # to the launch
