@@ -298,14 +298,15 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearParams p) {
 #pragma unroll
     for (int g = 0; g < 4; ++g)
       add[i][g] = *reinterpret_cast<const f32x4*>(bias + wn * NB * 32 + 32 * i + 8 * g + 4 * half);
-  // 8 rows of `mine` a round: lane / 8 of them, chunk lane % 8 of its row, `per_chunk` outputs from n on
-  const auto put = [&](int j, int64_t n_first, auto* y, int per_chunk) {
+  // 8 rows of `mine` a round: lane / 8 of them, chunk lane % 8 of its row's `chunks`, `per_chunk` outputs from n on
+  const auto put = [&](int j, int64_t n_first, auto* y, int per_chunk, int chunks) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int row = 8 * q + lane / 8;
       const u32x4 v = *reinterpret_cast<const u32x4*>(mine + 128 * row + 16 * (lane % 8));
-      const int64_t m = m0 + (wm * MB + j) * 32 + row, n = n_first + per_chunk * ((lane % 8) ^ swizzle<8>(row));
-      if (m >= p.M || n >= p.N) continue;
+      const int chunk = (lane % 8) ^ swizzle<8>(row);
+      const int64_t m = m0 + (wm * MB + j) * 32 + row, n = n_first + per_chunk * chunk;
+      if (m >= p.M || n >= p.N || chunk >= chunks) continue;
       int64_t at = m * p.y.ss;
       if (p.rows < p.M) {  // rows of several batch entries that are not evenly spaced
         const uint32_t b = (uint32_t)m / (uint32_t)p.rows;
@@ -326,7 +327,6 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearParams p) {
       }
     }
   };
-  static_assert(NB % 2 == 0, "rows of 64 outputs");
 #pragma unroll
   for (int j = 0; j < MB; ++j) {
     if (p.f32) {
@@ -339,13 +339,14 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearParams p) {
           for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * g + e] + add[i][g][e];
           *reinterpret_cast<f32x4*>(mine + 128 * r + 16 * ((2 * g + half) ^ swizzle<8>(r))) = v;
         }
-        put(j, nw + 32 * i, static_cast<float*>(const_cast<void*>(p.y.p)), 4);
+        put(j, nw + 32 * i, static_cast<float*>(const_cast<void*>(p.y.p)), 4, 8);
       }
     } else {
 #pragma unroll
-      for (int pair = 0; pair < NB / 2; ++pair) {
+      for (int pair = 0; pair < (NB + 1) / 2; ++pair) {  // 64 outputs, or the 32 that are left
+        const int blocks = NB - 2 * pair < 2 ? 1 : 2;
 #pragma unroll
-        for (int o = 0; o < 2; ++o)
+        for (int o = 0; o < blocks; ++o)
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             const int i = 2 * pair + o;
@@ -356,7 +357,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearParams p) {
             *reinterpret_cast<u32x2*>(mine + 128 * r + 16 * ((4 * o + g) ^ swizzle<8>(r)) + 8 * half) =
                 u32x2{h[0] | h[1] << 16, h[2] | h[3] << 16};
           }
-        put(j, nw + 64 * pair, static_cast<uint16_t*>(const_cast<void*>(p.y.p)), 8);
+        put(j, nw + 64 * pair, static_cast<uint16_t*>(const_cast<void*>(p.y.p)), 8, 4 * blocks);
       }
     }
   }
@@ -741,7 +742,7 @@ int64_t few_bytes(int x_kind, int64_t M, int32_t K) {
 #define RA_LINEAR_TILES(KX, KW)                                                \
   template __global__ void linear_kernel<KX, KW, 256, 256, 2, 4>(LinearParams); \
   template __global__ void linear_kernel<KX, KW, 128, 128, 2, 2>(LinearParams); \
-  template __global__ void linear_kernel<KX, KW, 64, 64, 2, 1>(LinearParams);
+  template __global__ void linear_kernel<KX, KW, 64, 64, 2, 2>(LinearParams);
 RA_LINEAR_TILES(FP4, FP4)
 RA_LINEAR_TILES(FP4, FP8)
 RA_LINEAR_TILES(FP8, FP4)
@@ -788,14 +789,15 @@ hipError_t run_few(const LinearParams& p, hipStream_t stream) {
 // CUs' second place empty takes less. Measured, in us, 256 against 128: 16384 x 2048 -> 8192 in 4 bits 166 / 197, in 8
 // and 4 241 / 277; 4352 x 4096 -> 12288 131 / 145; 2048 x 2048 -> 6144 in 8 and 4 26 / 30; 4352 x 2048 -> 4096 in 4 bits
 // 38 / 31, in 8 and 4 54 / 45; 1024 x 2048 -> 4096 25 / 12. (256 x 128 and 128 x 256 on 8 wavefronts lie between.)
-// Tiles of 64 x 64 on 2 wavefronts where no CU has more than three: less work a stage, and more CUs read the weights. 64
-// against 128, 8 and 4 bits: 61 x 1536 -> 4608 7.1 / 10.5, 131 x 1536 -> 1152 6.1 / 8.9, 64 x 8192 -> 2048 21 / 32, 512 x
-// 2048 -> 4096 9.5 / 11.2, 768 rows of that 10.7 / 11.8, 896 13.2 / 12.0.
+// Tiles of 64 x 64 on 4 wavefronts where no CU has more than three: less work a stage, and more CUs read the weights. 64
+// against 128, 8 and 4 bits: 61 x 1536 -> 4608 (8 bits on both sides) 6.6 / 10.5, 131 x 1536 -> 1152 5.5 / 8.9, 64 x 8192 ->
+// 2048 20 / 32, 512 x 2048 -> 4096 8.6 / 11.2, 768 rows of that 11.3 / 11.8, 896 17 / 12. (On 2 wavefronts 7.1, 6.1, 21,
+// 9.4, 10.9.)
 template <int KX, int KW>
 hipError_t run_linear(const LinearParams& p, hipStream_t stream) {
   const double cus = std::max(1, attn_bf16_slots(128, kAttnBf16BM).cus);
   const auto tiles = [&](int64_t t) { return (double)(((p.M + t - 1) / t) * ((p.N + t - 1) / t)); };
-  if (tiles(64) <= 3 * cus) return run_tiles<KX, KW, 64, 64, 2, 1>(p, stream);
+  if (tiles(64) <= 3 * cus) return run_tiles<KX, KW, 64, 64, 2, 2>(p, stream);
   const double small = tiles(128) / (2 * cus), part = small - std::floor(small);
   const double small_us = std::floor(small) + (part > 0 ? 0.6 + 0.4 * part : 0.0);
   if (1.45 * std::ceil(tiles(256) / cus) < small_us) return run_tiles<KX, KW, 256, 256, 2, 4>(p, stream);
