@@ -89,8 +89,8 @@ struct Operand {
   }
 };
 
-// The scale bytes of its rows go to LDS for two stages at a time: 16 bytes a row (of which stages of 128 elements use the
-// first 8), 64 rows an instruction. Rows of scales start at whole words (the host has others copied).
+// The scale bytes of its rows go to LDS 16 bytes a row, of which a stage uses 4 or 8, 64 rows an instruction. Rows of
+// scales start at whole words (the host has others copied).
 struct ScaleRows {
   __amdgpu_buffer_rsrc_t rs;
   uint32_t voff;
@@ -108,11 +108,15 @@ struct ScaleRows {
   }
 };
 
-// Every wavefront's loads into LDS have arrived and its reads are done. (The barrier alone waits for the loads that this
-// wavefront reads itself, where the compiler sees such reads.)
-__device__ __forceinline__ void all_arrived() {
-  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
-  __syncthreads();
+// Every wavefront's loads into LDS but its last LEFT have arrived, and its reads and writes there are done. (The barrier
+// with its fence is not used: the fence may wait for every load, or for none that this wavefront does not read itself.)
+template <int LEFT>
+__device__ __forceinline__ void arrived() {
+  static_assert(LEFT < 64, "a counter of 6 bits");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070 | (LEFT & 15) | (LEFT >> 4) << 14);  // vmcnt(LEFT) lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
 }
 
 template <int KIND>
@@ -149,8 +153,8 @@ __device__ __forceinline__ void tile_at(int tile, const LinearParams& p, int& tm
   tm = g * GROUP_M + in - tn * rows;
 }
 
-// BM rows x BN outputs a workgroup of WM x WN wavefronts.
-template <int KX, int KW, int BM, int BN, int WM, int WN>
+// BM rows x BN outputs a workgroup of WM x WN wavefronts; DEPTH stages in LDS, of which all but one are on their way.
+template <int KX, int KW, int BM, int BN, int WM, int WN, int DEPTH>
 __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearParams p) {
   constexpr int KD = kDepth<KX, KW>, NW = WM * WN;
   constexpr int MB = BM / WM / 32, NB = BN / WN / 32;  // blocks of 32 of a wavefront
@@ -159,10 +163,16 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearParams p) {
   constexpr bool SCALED = KX != B16;
   constexpr int ND = KD / 128;  // scale words of a row and stage
   constexpr int NS = (BM / 64 + BN / 64 + NW - 1) / NW;  // scale loads of a wavefront
-  // separate arrays, so that a stage's loads are not waited for before the other stage's reads
-  __shared__ __attribute__((aligned(1024))) uint8_t x0[BM * X::RB], x1[BM * X::RB],
-      w0[BN * W::RB > 4096 * NW ? BN * W::RB : 4096 * NW], w1[BN * W::RB];
-  __shared__ __attribute__((aligned(1024))) uint8_t scales[SCALED ? 2 * 1024 * NW * NS : 16];
+  // Scale bytes are loaded for two stages at a time; with more stages in LDS, where their place would be another's, with
+  // every stage (8192^3 in 8 bits 438 us in pairs, 487 without).
+  constexpr bool PAIRS = DEPTH == 2;
+  constexpr int LOADS = X::NI + W::NI + (SCALED ? NS : 0);  // of a wavefront and stage, without pairs
+  static_assert(DEPTH == 2 || DEPTH == 4, "stages");
+  // separate arrays, so that a stage's loads are not waited for before another stage's reads
+  constexpr int XB = BM * X::RB, WB = BN * W::RB, EB = SCALED ? 1024 * NW * NS : 16;
+  constexpr int XB2 = DEPTH > 2 ? XB : 16, WB2 = DEPTH > 2 ? WB : 16, EB2 = DEPTH > 2 ? EB : 16;
+  __shared__ __attribute__((aligned(1024))) uint8_t x0[XB], x1[XB], x2[XB2], x3[XB2], w0[WB > 4096 * NW ? WB : 4096 * NW],
+      w1[WB], w2[WB2], w3[WB2], e0[PAIRS ? 2 * EB : EB], e1[EB2], e2[EB2], e3[EB2];
   __shared__ __attribute__((aligned(16))) float bias[BN];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -203,15 +213,15 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearParams p) {
   int next = 0, loaded = 0;  // the stage that is loaded next, within its part and of all
   const uint8_t* xbase = p.x + m0 * p.x_stride;
   // Without branches: across one the compiler moves matrix instructions behind the next barrier.
-  const auto load = [&](uint8_t* xl, uint8_t* wl, bool even) {
+  const auto load = [&](uint8_t* xl, uint8_t* wl, uint8_t* el, bool even) {
     const bool any = loaded < stages;
     xo.load(xl, next * X::RB, any);
     wo.load(wl, next * W::RB, any);
     if constexpr (SCALED) {
-      if (even) {
+      if constexpr (PAIRS) el = e0 + (next & 2 ? EB : 0);
+      if (!PAIRS || even) {
 #pragma unroll
-        for (int i = 0; i < NS; ++i)
-          so[i].load(scales + ((next & 2) * 512 * NW + 1024 * wave) * NS + 1024 * i, any ? next * (KD / 32) : 0);
+        for (int i = 0; i < NS; ++i) so[i].load(el + 1024 * (wave * NS + i), any ? next * (KD / 32) : 0);
       }
     }
     ++loaded;
@@ -225,13 +235,15 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearParams p) {
   // where this lane's operands and scales lie
   const uint32_t xat = (wm * MB * 32 + r) * X::RB + 16 * (half ^ swizzle<X::NC>(r));
   const uint32_t wat = (wn * NB * 32 + r) * W::RB + 16 * (half ^ swizzle<W::NC>(r));
-  const uint8_t* const xsat = scales + 16 * (wm * MB * 32 + r);
-  const uint8_t* const wsat = scales + 16 * (BM + wn * NB * 32 + r);
-  // Loads the next stage once this one's scale words have been read, and forms this one's products.
-  const auto stage = [&](const uint8_t* xl, const uint8_t* wl, uint8_t* xn, uint8_t* wn_, int s, bool even) {
+  const int xeat = 16 * (wm * MB * 32 + r), weat = 16 * (BM + wn * NB * 32 + r);
+  // Once stage s is there and every wavefront is done with the stage before it: loads stage s + DEPTH - 1 in that one's
+  // place, with stage s's scale words read ahead of that, and forms the products of stage s.
+  const auto stage = [&](const uint8_t* xl, const uint8_t* wl, const uint8_t* el, uint8_t* xn, uint8_t* wn_, uint8_t* en,
+                         int s, bool even) {
+    arrived<(DEPTH - 2) * LOADS>();
     uint32_t xe[MB][ND], we[NB][ND];
     if constexpr (SCALED) {
-      const int at = (s & 2) * 512 * NW * NS + (even ? 0 : 4 * ND);
+      if constexpr (PAIRS) el = e0 + (s & 2 ? EB : 0) + (even ? 0 : 4 * ND);
 #pragma unroll
       for (int d = 0; d < ND; ++d) {
         // bytes past the end of K meet zero codes, but 255 would make NaN of them
@@ -239,13 +251,13 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearParams p) {
         const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
 #pragma unroll
         for (int b = 0; b < MB; ++b)
-          xe[b][d] = (*reinterpret_cast<const uint32_t*>(xsat + at + 512 * b + 4 * d) & keep) >> (8 * half);
+          xe[b][d] = (*reinterpret_cast<const uint32_t*>(el + xeat + 512 * b + 4 * d) & keep) >> (8 * half);
 #pragma unroll
         for (int b = 0; b < NB; ++b)
-          we[b][d] = (*reinterpret_cast<const uint32_t*>(wsat + at + 512 * b + 4 * d) & keep) >> (8 * half);
+          we[b][d] = (*reinterpret_cast<const uint32_t*>(el + weat + 512 * b + 4 * d) & keep) >> (8 * half);
       }
     }
-    load(xn, wn_, !even);
+    load(xn, wn_, en, !even);
 #pragma unroll
     for (int t = 0; t < (SCALED ? 2 * ND : KD / 16); ++t) {
       i32x8 xv[MB], wv[NB];
@@ -271,17 +283,29 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearParams p) {
     }
   };
 
-  load(x0, w0, true);
   int s = 0;
-  for (; s + 1 < stages; s += 2) {
-    all_arrived();  // stage s is there, and every wavefront is done with the stage before it
-    stage(x0, w0, x1, w1, s, true);
-    all_arrived();
-    stage(x1, w1, x0, w0, s + 1, false);
-  }
-  if (s < stages) {
-    all_arrived();
-    stage(x0, w0, x1, w1, s, true);
+  load(x0, w0, e0, true);
+  if constexpr (DEPTH == 2) {
+    for (; s + 1 < stages; s += 2) {
+      stage(x0, w0, e0, x1, w1, e1, s, true);
+      stage(x1, w1, e1, x0, w0, e0, s + 1, false);
+    }
+    if (s < stages) stage(x0, w0, e0, x1, w1, e1, s, true);
+  } else {
+    __builtin_amdgcn_sched_barrier(0);  // in the order in which they are waited for
+    load(x1, w1, e1, false);
+    __builtin_amdgcn_sched_barrier(0);
+    load(x2, w2, e2, true);
+    __builtin_amdgcn_sched_barrier(0);
+    for (; s + 3 < stages; s += 4) {
+      stage(x0, w0, e0, x3, w3, e3, s, true);
+      stage(x1, w1, e1, x0, w0, e0, s + 1, false);
+      stage(x2, w2, e2, x1, w1, e1, s + 2, true);
+      stage(x3, w3, e3, x2, w2, e2, s + 3, false);
+    }
+    if (s < stages) stage(x0, w0, e0, x3, w3, e3, s, true);
+    if (s + 1 < stages) stage(x1, w1, e1, x0, w0, e0, s + 1, false);
+    if (s + 2 < stages) stage(x2, w2, e2, x1, w1, e1, s + 2, true);
   }
 
   // A lane's column of a block is a row of y, its registers 4 g .. 4 g + 3 outputs 8 g + 4 half .. + 3: written as they
@@ -289,7 +313,7 @@ __global__ __launch_bounds__(64 * WM * WN) void linear_kernel(LinearParams p) {
   // LDS (16-byte chunks swizzled as above) and stores whole lines, past the caches: left there, they push out the tiles
   // that others share, and the kernel ends with writing them back (4096 x 512 -> 2048 10.0 us, past them 8.9; 16384 x
   // 2048 -> 8192 in 8 and 4 bits 238, 233).
-  all_arrived();
+  arrived<0>();
   uint8_t* const mine = w0 + 4096 * wave;
   const int64_t nw = n0 + wn * NB * 32;
   f32x4 add[NB][4];
@@ -739,10 +763,11 @@ int64_t few_bytes(int x_kind, int64_t M, int32_t K) {
 }
 
 // Explicit: reached only through a launcher's kernel pointer, the host pass would leave their launch stubs out.
-#define RA_LINEAR_TILES(KX, KW)                                                \
-  template __global__ void linear_kernel<KX, KW, 256, 256, 2, 4>(LinearParams); \
-  template __global__ void linear_kernel<KX, KW, 128, 128, 2, 2>(LinearParams); \
-  template __global__ void linear_kernel<KX, KW, 64, 64, 2, 2>(LinearParams);
+#define RA_LINEAR_TILES(KX, KW)                                                    \
+  template __global__ void linear_kernel<KX, KW, 256, 256, 2, 4, 2>(LinearParams); \
+  template __global__ void linear_kernel<KX, KW, 128, 128, 2, 2, 2>(LinearParams); \
+  template __global__ void linear_kernel<KX, KW, 64, 64, 2, 2, 2>(LinearParams);   \
+  template __global__ void linear_kernel<KX, KW, 64, 64, 2, 2, 4>(LinearParams);
 RA_LINEAR_TILES(FP4, FP4)
 RA_LINEAR_TILES(FP4, FP8)
 RA_LINEAR_TILES(FP8, FP4)
@@ -763,12 +788,13 @@ RA_LINEAR_FEW(FP8, FP8)
 #undef RA_LINEAR_FEW
 #undef RA_LINEAR_FEW_OF
 
-template <int KX, int KW, int BM, int BN, int WM, int WN>
+template <int KX, int KW, int BM, int BN, int WM, int WN, int DEPTH>
 hipError_t run_tiles(LinearParams p, hipStream_t stream) {
   p.tiles_m = (int32_t)((p.M + BM - 1) / BM);
   p.tiles_n = (int32_t)((p.N + BN - 1) / BN);
   const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
-  return launch_kernel(linear_kernel<KX, KW, BM, BN, WM, WN>, dim3((unsigned)tiles), dim3(64 * WM * WN), 0, stream, p);
+  return launch_kernel(linear_kernel<KX, KW, BM, BN, WM, WN, DEPTH>, dim3((unsigned)tiles), dim3(64 * WM * WN), 0, stream,
+                       p);
 }
 
 template <int KX, int KW, int LDS>
@@ -792,16 +818,19 @@ hipError_t run_few(const LinearParams& p, hipStream_t stream) {
 // Tiles of 64 x 64 on 4 wavefronts where no CU has more than three: less work a stage, and more CUs read the weights. 64
 // against 128, 8 and 4 bits: 61 x 1536 -> 4608 (8 bits on both sides) 6.6 / 10.5, 131 x 1536 -> 1152 5.5 / 8.9, 64 x 8192 ->
 // 2048 20 / 32, 512 x 2048 -> 4096 8.6 / 11.2, 768 rows of that 11.3 / 11.8, 896 17 / 12. (On 2 wavefronts 7.1, 6.1, 21,
-// 9.4, 10.9.)
+// 9.4, 10.9.) With at most one a CU, four stages in LDS hide the weights' way from memory: cold weights, four against two, 61
+// x 1536 -> 4608 8.2 / 11.7, 64 x 8192 -> 2048 26 / 33, 40 x 4096 -> 4096 14.3 / 18.0; with more a CU their place in LDS
+// costs more: 256 x 2048 -> 6144 12.4 / 11.7, 512 x 2048 -> 4096 in 4 bits 12.0 / 9.2.
 template <int KX, int KW>
 hipError_t run_linear(const LinearParams& p, hipStream_t stream) {
   const double cus = std::max(1, attn_bf16_slots(128, kAttnBf16BM).cus);
   const auto tiles = [&](int64_t t) { return (double)(((p.M + t - 1) / t) * ((p.N + t - 1) / t)); };
-  if (tiles(64) <= 3 * cus) return run_tiles<KX, KW, 64, 64, 2, 2>(p, stream);
+  if (tiles(64) <= cus) return run_tiles<KX, KW, 64, 64, 2, 2, 4>(p, stream);
+  if (tiles(64) <= 3 * cus) return run_tiles<KX, KW, 64, 64, 2, 2, 2>(p, stream);
   const double small = tiles(128) / (2 * cus), part = small - std::floor(small);
   const double small_us = std::floor(small) + (part > 0 ? 0.6 + 0.4 * part : 0.0);
-  if (1.45 * std::ceil(tiles(256) / cus) < small_us) return run_tiles<KX, KW, 256, 256, 2, 4>(p, stream);
-  return run_tiles<KX, KW, 128, 128, 2, 2>(p, stream);
+  if (1.45 * std::ceil(tiles(256) / cus) < small_us) return run_tiles<KX, KW, 256, 256, 2, 4, 2>(p, stream);
+  return run_tiles<KX, KW, 128, 128, 2, 2, 2>(p, stream);
 }
 
 }  // namespace

@@ -13,9 +13,9 @@ from test_gpu_norm import _case, _check_grads, _check_y as _check_norm
 pytestmark = pytest.mark.gpu
 
 
-# tiles of 64, of 128 (more than three of 64 a CU) and of 256; rows and outputs that end inside a tile; K of one stage, of an
+# tiles of 64 in four stages and (more than one a CU) in two, of 128 (more than three of 64 a CU) and of 256; rows and outputs that end inside a tile; K of one stage, of an
 # odd and an even number, and ending inside one
-TILES = [(1, 63, 32, 65), (2, 65, 416, 127), (1, 1801, 160, 1795), (3, 601, 288, 1800), (1, 2300, 96, 3839), (2, 1153, 352, 3848)]
+TILES = [(1, 63, 32, 65), (2, 65, 416, 127), (1, 1100, 352, 1101), (3, 400, 1056, 1200), (1, 1801, 160, 1795), (3, 601, 288, 1800), (1, 2300, 96, 3839), (2, 1153, 352, 3848)]
 
 
 @pytest.mark.parametrize("fmt,wfmt", PAIRS)
@@ -36,7 +36,7 @@ def test_tiles(B, S, K, N, fmt, wfmt):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("S,K,N", [(1801, 1824, 33), (2300, 3840, 136), (1153, 96, 1795)])
+@pytest.mark.parametrize("S,K,N", [(1801, 1824, 33), (2300, 3840, 136), (1153, 96, 1795), (1100, 1120, 264)])
 def test_gradient_tiles(S, K, N, dtype):
     rng = np.random.default_rng(S + K + N)
     w, wp = _weights(rng, N, K, "mxfp4")
