@@ -488,8 +488,8 @@ struct RowsIn {
 // A workgroup forms 32 outputs of up to 32 rows, which it keeps in LDS whole; its wavefronts take chunks of K in turn, and
 // their sums are joined in order. Bound by the weights' bytes, which go from memory to registers two chunks ahead; a
 // row costs every workgroup its turn into LDS (about 0.1 ns an element). Measured: 1 row x 4096 -> 24576 in 8 and 4 bits
-// 12.9 us (4.1 TB/s; 17.4 with 64 outputs a workgroup), x 1536 -> 4608 3.9; 32 rows of that 9.0 (tiles, and the rounding
-// in a launch of its own: 11.2).
+// 12.9 us (4.1 TB/s; 17.4 with 64 outputs a workgroup; 16.7 with weights that the last-level cache does not hold), x 1536
+// -> 4608 3.9; 32 rows of that 9.0.
 template <int KX, int KW, int LDS, int XP>
 __global__ __launch_bounds__(64 * FEW_WAVES) void linear_few_kernel(LinearParams p) {
   constexpr int KC = KW == FP4 ? 256 : 128, STEPS = KC / 64, ND = KC / 128;
@@ -836,10 +836,10 @@ hipError_t run_linear(const LinearParams& p, hipStream_t stream) {
 }  // namespace
 
 // Few rows go to the kernel that reads the weights once and turns the rows in every workgroup, at about 0.1 ns an element
-// and round of workgroups; tiles take a launch for the rounding and walk K in stages. Measured, in us, few against tiles
-// (rounding included), 8 and 4 bits: 1 row x 512 -> 512 3.3 / 6.2, x 4096 -> 24576 13.1 / 20; 16 rows x 1536 -> 4608 6.3 /
-// 10.9, x 4096 -> 4096 12.0 / 18.9, x 4096 -> 24576 35 / 22 (tiles are taken); 32 rows x 1536 -> 4608 9.0 / 11.2, x 4096
-// -> 4096 19.2 / 19.3.
+// and round of workgroups; tiles take a launch for the rounding and walk K in stages. Measured with cold weights, in us, few
+// against tiles (rounding included), 8 and 4 bits: 1 row x 512 -> 512 3.1 / 5.4, x 4096 -> 24576 16.7 / 26; 16 rows x 1536
+// -> 4608 7.2 / 9.9, x 4096 -> 4096 13.5 / 15.8, x 4096 -> 24576 40 / 28 (tiles are taken), 24 rows x 4096 -> 4096 17.0 /
+// 16.7; 32 rows x 1536 -> 4608 10.0 / 10.3, x 2048 -> 8192 12.3 / 11.5.
 bool linear_is_few(int x_kind, int64_t M, int32_t N, int32_t K) {
   if (x_kind == B16 || M > FEW_ROWS || few_bytes(x_kind, M, K) > FEW_MORE_LDS) return false;
   return (double)M * K * std::max(1.0, N / 8192.0) < 24000.0 + 31.0 * K;
