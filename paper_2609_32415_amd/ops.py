@@ -961,30 +961,36 @@ def layer_norm_grad(dy, x, stats, weight=None, bias=None, *, scale=None, eps=1e-
 
 
 def _norm_grad(desc, pdt, dy, x, stats, weight, bias, scale, wanted, shapes, workspace=None):
-    dev, shape, dt, where = torch._C._cuda_getDevice(), x.shape, x.dtype, x.device
-    C, B = shape[-1], shape[0] if len(shape) == 3 else 1
-    w_x, *w_params = wanted
-    dx = torch.empty_like(x, memory_format=_DENSE) if w_x else None
-    sums = [None if not w else torch.empty_like(t, memory_format=_DENSE) if t is not None and t.shape == s else
-            torch.empty(s, dtype=pdt, device=where)
-            for w, t, s in zip(w_params, (weight, bias, scale, scale), ((C,), (C,), *shapes))]
-    nbytes = 0
+    dev, shape, dt = torch._C._cuda_getDevice(), x.shape, x.dtype
+    (S, C), B = shape[-2:], shape[0] if len(shape) == 3 else 1
+    w_params = wanted[1:]
+    sums, at, ws, nbytes = (None,) * 4, (0,) * 4, 0, 0
     if True in w_params:
+        sums = [None if not w else torch.empty_like(t, memory_format=_DENSE) if t is not None and t.shape == s else
+                torch.empty(s, dtype=pdt, device=x.device)
+                for w, t, s in zip(w_params, (weight, bias, scale, scale), ((C,), (C,), *shapes))]
+        at = [0 if t is None else t.data_ptr() for t in sums]
         if workspace is None:
-            workspace = torch.empty(L.refadapt_layer_norm_grad_workspace_size_packed(desc), dtype=torch.uint8,
-                                    device=where)
-        elif workspace.get_device() != dev:
-            _elsewhere("workspace", workspace, dev)
-        nbytes = _nbytes(workspace)
-    elif dx is None:
+            nbytes = L.refadapt_layer_norm_grad_workspace_size_packed(desc)
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+        else:
+            if workspace.get_device() != dev:
+                _elsewhere("workspace", workspace, dev)
+            nbytes = _nbytes(workspace)
+        ws = workspace.data_ptr()
+    elif not wanted[0]:
         return (None,) * 5
+    dx, to = None, _NO_TENSOR
+    if wanted[0]:
+        dx = torch.empty_like(x, memory_format=_DENSE)
+        to = dx.data_ptr(), S * C, 0, C
     sc, sc_stride = (0, 0) if scale is None else _row_words(
         "scale", scale, pdt, (C,) if len(shape) == 2 and scale.dim() == 1 else (B, C), dev)
     args = L.NORM_GRAD_ARGS_PACK.pack(
-        *_rows("dy", dy, dt, shape, dev), *_rows("x", x, dt, shape, dev), *_rows("dx", dx, dt, shape, dev),
-        stats.data_ptr(), _row_words("weight", weight, pdt, (C,), dev)[0], _row_words("bias", bias, pdt, (C,), dev)[0],
-        sc, sc_stride, *[0 if t is None else t.data_ptr() for t in sums], workspace.data_ptr() if nbytes else 0, nbytes)
-    if nbytes or x.numel():
+        *_rows("dy", dy, dt, shape, dev), *_rows("x", x, dt, shape, dev), *to, stats.data_ptr(),
+        0 if weight is None else _row_words("weight", weight, pdt, (C,), dev)[0],
+        0 if bias is None else _row_words("bias", bias, pdt, (C,), dev)[0], sc, sc_stride, *at, ws, nbytes)
+    if nbytes or S * B:
         L.refadapt_layer_norm_grad_packed(desc, args, _stream())
     return dx, *sums
 
