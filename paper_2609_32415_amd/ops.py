@@ -4,6 +4,8 @@ Each function checks devices, dtypes and layouts, allocates outputs with
 torch (caching allocator) when the caller does not pass them, and calls the
 C entry point of the same role on ``torch.cuda.current_stream()``. No torch
 compute op runs on these paths; a tensor that is not on a GPU is an error.
+What a call writes into a caller's tensors counts as a change in place, as
+with torch's own operations.
 """
 
 from __future__ import annotations
@@ -33,6 +35,12 @@ _NO_TENSOR = (0, 0, 0, 0)
 def _stream():
     # the current stream of the current device, without building a torch.cuda.Stream
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
+def _written(*tensors):
+    """Counts the library's writes into tensors of the caller as changes in place, as torch counts its own: a recorded
+    call that saved one of them refuses its backward pass then. (Tensors made in inference mode have no count.)"""
+    torch.autograd.graph.increment_version([t for t in tensors if t is not None and not t.is_inference()])
 
 
 def _on_gpu(name, t):
@@ -210,6 +218,7 @@ def joint_attn(
         0 if clock_probe is None else _probe_ptr(clock_probe),
     )
     L.refadapt_joint_attn_packed(L.DESC_PACK.pack(*desc), args, _stream())
+    _written(o_tgt, o_ref if ref_queries else None, mass_t, lse_t, mrq_t, smass_t)
     return AttnOut(o_tgt, o_ref if ref_queries else None, mass_t, lse_t, mrq_t, smass_t)
 
 
@@ -251,6 +260,7 @@ def q_change(q_cur, q_prev, eps=1e-8, out=None, workspace=None):
         _view("q_cur", q_cur, dt), _view("q_prev", q_prev, dt, q_cur.shape),
         float(eps), _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(),
     )
+    _written(out)
     return out
 
 
@@ -283,6 +293,7 @@ def gate(d_cur, mass_prev, theta, state, block, step, mode="product", decision_o
         B, H, n_tgt, int(block), int(step), _GATE[mode],
         _ptr(d_cur), _ptr(mass_prev), _ptr(theta), _ptr(state), _ptr(decision_out), _ptr(score_out), _stream(),
     )
+    _written(state, decision_out, score_out)
     return decision_out, score_out
 
 
@@ -329,6 +340,7 @@ def q_change_gate(q_cur, q_prev, mass_prev, theta, state, block, step, mode="pro
         int(block), int(step), _GATE[mode], _ptr(mass_prev), _ptr(theta), _ptr(state), _ptr(d_out),
         _ptr(decision_out), _ptr(score_out), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(),
     )
+    _written(state, d_out, decision_out, score_out)
     return d_out, decision_out, score_out
 
 
@@ -365,6 +377,7 @@ def q_change_gate_noalloc(q_cur, q_prev, mass_prev, theta, state, block, step, m
         int(block), int(step), _GATE[mode], _ptr(mass_prev), _ptr(theta), _ptr(state), _ptr(d_out),
         _ptr(decision_out), _ptr(score_out), _stream(),
     )
+    _written(state, d_out, decision_out, score_out)
     return d_out, decision_out, score_out
 
 
@@ -389,6 +402,7 @@ def cache_commit(k_ref, v_ref, k_cache, v_cache, decision=None, age=None, step=0
         _view("q_cache", q_cache, dt, k_ref.shape),
         _ptr(decision), _ptr(age), int(step), _stream(),
     )
+    _written(k_cache, v_cache, q_cache, age)
 
 
 # ---- diagnostics sidecar (read-only probes of the controlled path)
@@ -430,6 +444,7 @@ def kv_drift(k_cur, k_base, v_cur, v_base, eps=1e-8, d_k=None, d_v=None, e_kv=No
         _view("v_cur", v_cur, dt, k_cur.shape), _view("v_base", v_base, dt, k_cur.shape), float(eps),
         _ptr(d_k), _ptr(d_v), _ptr(e_kv), _ptr(workspace), _nbytes(workspace), _stream(),
     )
+    _written(d_k, d_v, e_kv)
     return d_k, d_v, e_kv
 
 
@@ -460,6 +475,7 @@ def drift_log_ratio(z_ref_cur, z_ref_prev, z_tgt_cur, z_tgt_prev, eps=1e-8, d_re
         _view("z_tgt_prev", z_tgt_prev, dt, (B, H, n_tgt, D)), float(eps), _ptr(d_ref), _ptr(d_tgt), _ptr(rho),
         _ptr(workspace), _nbytes(workspace), _stream(),
     )
+    _written(d_ref, d_tgt, rho)
     return d_ref, d_tgt, rho
 
 
@@ -482,6 +498,7 @@ def output_impact(o_stale, o_fresh, eps=1e-8, out=None, workspace=None):
         B, H, n, D, _DTYPES[dt], _view("o_stale", o_stale, dt), _view("o_fresh", o_fresh, dt, o_stale.shape),
         float(eps), _ptr(out), _ptr(workspace), _nbytes(workspace), _stream(),
     )
+    _written(out)
     return out
 
 
@@ -494,6 +511,7 @@ def mass_mean(mass, complement=False, out=None):
     B, H, n = mass.shape
     out = _f32_out("out", out, (B, H), mass.device)
     L.refadapt_mass_mean(B, H, n, _ptr(mass), int(bool(complement)), _ptr(out), _stream())
+    _written(out)
     return out
 
 
@@ -507,6 +525,7 @@ def adjacent_mass_change(mass_log, out=None):
     bh = mass_log[0, 0].numel()
     out = _f32_out("out", out, (nb,), mass_log.device)
     L.refadapt_adjacent_mass_change(T, nb, bh, _ptr(mass_log), _ptr(out), _stream())
+    _written(out)
     return out
 
 
@@ -648,6 +667,7 @@ def _rope(q, k, pos, freq, axis, pairing, inverse, q_out=None, k_out=None):
                                  _POS[pos.dtype], pst[0] if len(ps) == 3 and ps[0] == B else 0, pst[-2],
                                  freq.data_ptr(), axis.data_ptr())
     L.refadapt_rope_packed(desc, args, _stream())
+    _written(q_out, k_out)
     return q_out if k is None else (q_out, k_out)
 
 
@@ -731,6 +751,7 @@ def mx_commit(k_ref, v_ref, k_mx, v_mx, decision=None, age=None, step=0, q_ref=N
         *_mx_words("v_mx", v_mx, fmt, shape, dev), *_mx_words("q_mx", q_mx, fmt, shape, dev),
         _int_word("decision", decision, dev), _int_word("age", age, dev), int(step))
     L.refadapt_mx_commit_packed(L.MX_DESC_PACK.pack(B, H, n_ref, D, _DTYPES[dt], _MX[fmt]), args, _stream())
+    _written(age, *(t for m in (k_mx, v_mx, q_mx) if m is not None for t in (m.codes, m.scales)))
 
 
 def mx_read(k_mx, v_mx=None, q_mx=None, dtype=torch.bfloat16, k_out=None, v_out=None, q_out=None):
@@ -753,6 +774,7 @@ def mx_read(k_mx, v_mx=None, q_mx=None, dtype=torch.bfloat16, k_out=None, v_out=
         *_words("q_out", q_out, dtype, shape, dev), *_mx_words("k_mx", k_mx, fmt, shape, dev),
         *_mx_words("v_mx", v_mx, fmt, shape, dev), *_mx_words("q_mx", q_mx, fmt, shape, dev), 0, 0, 0)
     L.refadapt_mx_read_packed(L.MX_DESC_PACK.pack(B, H, n, D, _DTYPES[dtype], _MX[fmt]), args, _stream())
+    _written(k_out, v_out, q_out)
     return tuple(o for o in (k_out, v_out, q_out) if o is not None)
 
 
@@ -811,6 +833,7 @@ def joint_attn_mx(q_tgt, k_tgt, v_tgt, *, k_mx, v_mx, q_mx=None, q_ref=None, k_r
     cache = L.MX_CACHE_PACK.pack(_MX[fmt], *_mx_words("k_mx", k_mx, fmt, shp_r, dev),
                                  *_mx_words("v_mx", v_mx, fmt, shp_r, dev), *_mx_words("q_mx", q_mx, fmt, shp_r, dev))
     L.refadapt_joint_attn_mx_packed(desc, args, cache, _stream())
+    _written(o_tgt, o_ref if ref_queries else None, mass_t, lse_t, mrq_t)
     return AttnOut(o_tgt, o_ref if ref_queries else None, mass_t, lse_t, mrq_t)
 
 
@@ -911,7 +934,10 @@ def layer_norm(x, weight=None, bias=None, *, scale=None, shift=None, eps=1e-6, o
         return _LayerNorm.apply(x, weight, bias, scale, shift, eps)
     if out is None:
         out = torch.empty_like(x, memory_format=_DENSE)
-    _norm(x, weight, bias, scale, shift, eps, y=out)
+        _norm(x, weight, bias, scale, shift, eps, y=out)
+    else:
+        _norm(x, weight, bias, scale, shift, eps, y=out)
+        _written(out)
     return out
 
 
@@ -1007,6 +1033,7 @@ def layer_norm_mx(x, fmt, weight=None, bias=None, *, scale=None, shift=None, eps
     elif out.fmt != fmt:
         raise ValueError(f"out: format {out.fmt} differs from {fmt}")
     _norm(x, weight, bias, scale, shift, eps, y_mx=out)
+    _written(out.codes, out.scales)
     return out
 
 
@@ -1089,6 +1116,7 @@ def _linear(x, w, bias, fmt, dt, sizes, lead, out=None, workspace=None):
     where = x.codes.device if mx else x.device
     if not where.type == "cuda":
         _on_gpu("x", x.codes if mx else x)
+    given = out
     if out is None:
         out = x.codes.new_empty((*lead, n_out), dtype=dt) if mx else x.new_empty((*lead, n_out))
     ws, held = _linear_workspace(L.refadapt_mx_linear_workspace_size_packed(desc, mx), workspace, where, dev)
@@ -1098,6 +1126,8 @@ def _linear(x, w, bias, fmt, dt, sizes, lead, out=None, workspace=None):
         *_mx_words("w", w, w.fmt, (1, 1, n_out, n_in), dev), _row_words("bias", bias, dt, (n_out,), dev)[0],
         *_rows("out", out, dt, (*lead, n_out), dev), *ws)
     L.refadapt_mx_linear_packed(desc, args, _stream())
+    if given is not None:
+        _written(given)
     return out
 
 
