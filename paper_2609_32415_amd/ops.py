@@ -15,6 +15,7 @@ from dataclasses import dataclass
 from typing import Optional
 
 import torch
+from torch.autograd import forward_ad as _forward
 
 from . import _lib as L
 
@@ -43,6 +44,12 @@ def _written(*tensors):
     torch.autograd.graph.increment_version([t for t in tensors if t is not None and not t.is_inference()])
 
 
+def _no_tangent(name, t):
+    """Forward-mode derivatives: a tensor's pointer would leave its tangent behind. (Asked at a dual level alone.)"""
+    if _forward.unpack_dual(t).tangent is not None:
+        raise ValueError(f"{name} carries a tangent: there are no forward-mode derivatives")
+
+
 def _on_gpu(name, t):
     if t is not None and not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor (the HIP library is the only implementation)")
@@ -54,6 +61,8 @@ def _quad(name, t, dtype, shape):
         return _NO_TENSOR
     if not t.is_cuda:
         _on_gpu(name, t)
+    if _forward._current_level >= 0:
+        _no_tangent(name, t)
     sh = t.shape
     if len(sh) != 4:
         raise ValueError(f"{name} must be [B, H, S, d], got {tuple(sh)}")
@@ -74,6 +83,8 @@ def _view(name, t, dtype=None, shape=None):
 
 
 def _ptr(t):
+    if t is not None and _forward._current_level >= 0:
+        _no_tangent("an input", t)
     return None if t is None else t.data_ptr()
 
 
@@ -548,6 +559,8 @@ def _words(name, t, dtype, shape, dev):
         return _NO_TENSOR
     if t.get_device() != dev:
         _elsewhere(name, t, dev)
+    if _forward._current_level >= 0:
+        _no_tangent(name, t)
     if t.shape != shape or t.dtype != dtype:
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} differs from {dtype} {tuple(shape)}")
     sb, sh, ss, sd = t.stride()
@@ -645,6 +658,9 @@ def _rope(q, k, pos, freq, axis, pairing, inverse, q_out=None, k_out=None):
     ps, pst = pos.shape, pos.stride()
     if pos.get_device() != dev:
         _elsewhere("pos", pos, dev)
+    if _forward._current_level >= 0:
+        _no_tangent("pos", pos)
+        _no_tangent("freq", freq)
     if pos.dtype not in _POS or len(ps) not in (2, 3) or pst[-1] != 1 and ps[-1] != 1:
         raise ValueError("pos must be int32 or float32 [S, axes] or [B, S, axes] with contiguous axes")
     if ps[-2] != S or len(ps) == 3 and ps[0] not in (1, B):
@@ -858,6 +874,8 @@ def _rows(name, t, dtype, shape, dev):
         return _NO_TENSOR
     if t.get_device() != dev:
         _elsewhere(name, t, dev)
+    if _forward._current_level >= 0:
+        _no_tangent(name, t)
     if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} differs from {dtype} {tuple(shape)}")
     st = t.stride()
@@ -880,6 +898,8 @@ def _row_words(name, t, dtype, shape, dev):
         return 0, 0
     if t.get_device() != dev:
         _elsewhere(name, t, dev)
+    if _forward._current_level >= 0:
+        _no_tangent(name, t)
     if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} differs from {dtype} {tuple(shape)}")
     if t.stride(-1) != 1 and shape[-1] != 1:
@@ -983,6 +1003,8 @@ def layer_norm_grad(dy, x, stats, weight=None, bias=None, *, scale=None, eps=1e-
         raise ValueError(f"stats must be contiguous float32 {(*shape[:-1], 2)}")
     if stats.get_device() != dev:
         _elsewhere("stats", stats, dev)
+    if _forward._current_level >= 0:
+        _no_tangent("stats", stats)
     return _norm_grad(desc, pdt, dy, x, stats, weight, bias, scale, wanted, ((B, C), (B, C)), workspace)
 
 
