@@ -105,6 +105,27 @@ class AttnOut:
     seg_mass: Optional[torch.Tensor] = None
 
 
+class _Underived(torch.autograd.Function):
+    """The results of an operator without gradients: a backward pass that reaches it ends with an error."""
+
+    @staticmethod
+    def forward(ctx, who, results, *inputs):
+        ctx.who = who
+        return tuple(t.detach() for t in results)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise NotImplementedError(f"{ctx.who} has no gradients: detach its inputs, or call it under torch.no_grad()")
+
+
+def _attn_out(who, inputs, *results):
+    """``results`` as an ``AttnOut``, tied to ``inputs`` where these require gradients."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs):
+        tied = iter(_Underived.apply(who, [t for t in results if t is not None], *inputs))
+        results = [t if t is None else next(tied) for t in results]
+    return AttnOut(*results)
+
+
 def joint_attn(
     q_tgt,
     k_tgt,
@@ -153,6 +174,10 @@ def joint_attn(
     ``seg_cache`` (one bool per segment) picks the cached K/V for a segment, else
     the fresh K/V. ``seg_mass`` (bool or preallocated fp32 ``[B, H, n_tgt, n_seg]``)
     returns each target query's mass per segment in ``AttnOut.seg_mass``.
+
+    There are no gradients: where they are recorded and an input requires them, so do the tensors of the
+    ``AttnOut``, and a backward pass that reaches them raises NotImplementedError. (Buffers given for them
+    stay as they are.)
     """
     B, H, n_tgt, D = q_tgt.shape
     dt = q_tgt.dtype
@@ -230,7 +255,8 @@ def joint_attn(
     )
     L.refadapt_joint_attn_packed(L.DESC_PACK.pack(*desc), args, _stream())
     _written(o_tgt, o_ref if ref_queries else None, mass_t, lse_t, mrq_t, smass_t)
-    return AttnOut(o_tgt, o_ref if ref_queries else None, mass_t, lse_t, mrq_t, smass_t)
+    return _attn_out("joint_attn", (q_tgt, k_tgt, v_tgt, q_ref, k_ref, v_ref, k_cache, v_cache, q_cache),
+                     o_tgt, o_ref if ref_queries else None, mass_t, lse_t, mrq_t, smass_t)
 
 
 def attn_workspace(q_tgt, n_ref, qset="target", kvsrc="fresh", n_seg_mass=0):
@@ -799,7 +825,7 @@ def joint_attn_mx(q_tgt, k_tgt, v_tgt, *, k_mx, v_mx, q_mx=None, q_ref=None, k_r
                   ref_mass_refq=False, workspace=None, clock_probe=None):
     """``joint_attn`` with ``kvsrc`` "cache" or "device" whose cached reference K, V (and queries, ``q_mx``) are
     ``MxTensor``s, through ``refadapt_joint_attn_mx``. ``workspace``: None allocates what the library asks for, a
-    uint8 device tensor is used as given (``attn_mx_workspace``). Returns an ``AttnOut``."""
+    uint8 device tensor is used as given (``attn_mx_workspace``). Returns an ``AttnOut``, without gradients as there."""
     shp_t, dt, dev, where = q_tgt.shape, q_tgt.dtype, torch._C._cuda_getDevice(), q_tgt.device
     B, H, n_tgt, D = shp_t
     if dt not in _DTYPES:
@@ -850,7 +876,8 @@ def joint_attn_mx(q_tgt, k_tgt, v_tgt, *, k_mx, v_mx, q_mx=None, q_ref=None, k_r
                                  *_mx_words("v_mx", v_mx, fmt, shp_r, dev), *_mx_words("q_mx", q_mx, fmt, shp_r, dev))
     L.refadapt_joint_attn_mx_packed(desc, args, cache, _stream())
     _written(o_tgt, o_ref if ref_queries else None, mass_t, lse_t, mrq_t)
-    return AttnOut(o_tgt, o_ref if ref_queries else None, mass_t, lse_t, mrq_t)
+    return _attn_out("joint_attn_mx", (q_tgt, k_tgt, v_tgt, q_ref, k_ref, v_ref),
+                     o_tgt, o_ref if ref_queries else None, mass_t, lse_t, mrq_t)
 
 
 def attn_mx_workspace(q_tgt, n_ref, fmt, qset="target", kvsrc="cache", q_cached=False):
