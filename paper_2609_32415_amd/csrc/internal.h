@@ -176,6 +176,17 @@ struct RopeParams {
 };
 hipError_t launch_rope(int dtype, bool half, int32_t head_dim, RopeParams p, hipStream_t stream);
 
+// S rows in chunks of rows_per, the last of them perhaps shorter: `count`, no more than `most` (which counts as 1 at
+// least). Sums of two row numbers do not fit in 32 bits.
+struct RowChunks {
+  int32_t rows_per, count;
+};
+inline RowChunks row_chunks(int32_t S, int64_t most) {
+  most = most < 1 ? 1 : most;
+  const int64_t per = S > most ? ((int64_t)S + most - 1) / most : 1;
+  return RowChunks{(int32_t)per, (int32_t)(((int64_t)S + per - 1) / per)};
+}
+
 // Layer norm of the rows of [B, S, C] (View strides sb and ss), and its gradients.
 constexpr int kNormMaxWidth = 16384;
 struct NormParams {

@@ -146,15 +146,16 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS, 4) void norm_kernel(
   constexpr int L = 64 * W;
   __shared__ float slots[2][2][W];
   const int b = blockIdx.y, C = p.C;
-  const int s0 = blockIdx.x * p.rows_per, s1 = min(p.S, s0 + p.rows_per);
+  const int s0 = blockIdx.x * p.rows_per, group = (int)threadIdx.x / L;
+  uint32_t s = s0 + group;                       // (of a row past the last: 2^31 and more)
+  int left = min(p.rows_per, p.S - s0) - group;  // rows of the chunk from s on
   const bool pf32 = p.param_f32;
   const Lane<L, VEC> ln{(int)(threadIdx.x % L), C};
   constexpr int esz = BF16 ? 2 : 4;
   const char* const x = static_cast<const char*>(p.x.p) + b * p.x.sb * esz;
-  int s = s0 + (int)threadIdx.x / L;
   Oct v[NP];
   RawOct<BF16> next[NP];
-  if (s < s1) {
+  if (left > 0) {
 #pragma unroll
     for (int k = 0; k < NP; ++k) next[k] = ln.template raw<BF16>(x + s * p.x.ss * esz, k);
   }
@@ -174,7 +175,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS, 4) void norm_kernel(
       add[k].f[i] = fmaf(a.f[i], 1.f + m.f[i], t.f[i]);
     }
   }
-  for (int turn = 0; s < s1; s += ROWS, turn ^= 1) {
+  for (int turn = 0; left > 0; left -= ROWS, s += ROWS, turn ^= 1) {
     float sum = 0.f;
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
@@ -182,7 +183,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS, 4) void norm_kernel(
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum += v[k].f[i];
     }
-    if (s + ROWS < s1) {
+    if (left > ROWS) {
 #pragma unroll
       for (int k = 0; k < NP; ++k) next[k] = ln.template raw<BF16>(x + (s + ROWS) * p.x.ss * esz, k);
     }
@@ -242,7 +243,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS) void norm_grad_kerne
   __shared__ float slots[2][2][W];
   const int group = threadIdx.x / L;
   const int b = blockIdx.y, C = p.C;
-  const int s0 = blockIdx.x * p.rows_per, s1 = min(p.S, s0 + p.rows_per);
+  const int s0 = blockIdx.x * p.rows_per;
   const bool pf32 = p.param_f32;
   const Lane<L, VEC> ln{(int)(threadIdx.x % L), C};
   constexpr int esz = BF16 ? 2 : 4;
@@ -254,7 +255,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS) void norm_grad_kerne
   Oct ws[NP], P[NP], D[NP];
   RawOct<BF16> xn[NP], gn[NP];
   float2 stn = make_float2(0.f, 0.f);
-  const auto fetch = [&](int s) {
+  const auto fetch = [&](uint32_t s) {
     stn = st[s];
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
@@ -262,8 +263,9 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS) void norm_grad_kerne
       gn[k] = ln.template raw<BF16>(gb + s * p.dy.ss * esz, k);
     }
   };
-  int s = s0 + group;
-  if (s < s1) fetch(s);
+  uint32_t s = s0 + group;
+  int left = min(p.rows_per, p.S - s0) - group;
+  if (left > 0) fetch(s);
 #pragma unroll
   for (int k = 0; k < NP; ++k) {
     const Oct w = ln.param(p.weight, pf32, k, 1.f), m = ln.param(sc, pf32, k, 0.f);
@@ -273,7 +275,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS) void norm_grad_kerne
       P[k].f[i] = D[k].f[i] = 0.f;
     }
   }
-  for (int turn = 0; s < s1; s += ROWS, turn ^= 1) {
+  for (int turn = 0; left > 0; left -= ROWS, s += ROWS, turn ^= 1) {
     Oct h[NP], e[NP];
     const float2 now = stn;
     float a0 = 0.f, a1 = 0.f;
@@ -291,7 +293,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS) void norm_grad_kerne
         a1 = fmaf(e[k].f[i], h[k].f[i], a1);
       }
     }
-    if (s + ROWS < s1) fetch(s + ROWS);
+    if (left > ROWS) fetch(s + ROWS);
     // both sums behind one barrier; the slots of the row before stay readable (two sets in turn)
 #pragma unroll
     for (int m = 32; m > 0; m >>= 1) {
@@ -455,9 +457,9 @@ hipError_t launch_norm(int dtype, NormParams p, hipStream_t stream) {
     // bf16, us, 512 / 1024 / 2048 / 4096 chunks: 4096 x 4096 16.8 / 14.1 / 15.6 / 19.6, 2048 x 8192 15.6 / 16.9 / 20.7 /
     // 20.7, 16384 x 2048 38.6 / 25.7 / 24.5 / 24.4, 16384 x 512 10.8 / 8.8 / 8.4 / 10.3.
     const int64_t most = W > 4 ? 512 : W == 4 && NP == 1 ? 2048 : 1024;
-    const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>(most / p.B, (p.S + rows - 1) / rows));
-    p.rows_per = (int32_t)((p.S + chunks - 1) / chunks);
-    const dim3 grid((unsigned)((p.S + p.rows_per - 1) / p.rows_per), (unsigned)p.B);
+    const RowChunks chunks = row_chunks(p.S, std::min<int64_t>(most / p.B, ((int64_t)p.S + rows - 1) / rows));
+    p.rows_per = chunks.rows_per;
+    const dim3 grid((unsigned)chunks.count, (unsigned)p.B);
     const auto run = [&](auto* kernel) { return launch_kernel(kernel, grid, dim3(threads), 0, stream, p); };
     if (dtype == 0) return p.vec ? run(norm_kernel<true, W, NP, true>) : run(norm_kernel<true, W, NP, false>);
     return p.vec ? run(norm_kernel<false, W, NP, true>) : run(norm_kernel<false, W, NP, false>);
@@ -473,9 +475,9 @@ int norm_grad_chunks(int32_t B, int32_t S, int32_t C) {
 }
 
 hipError_t launch_norm_grad(int dtype, NormGradParams p, hipStream_t stream) {
-  p.chunks = norm_grad_chunks(p.B, p.S, p.C);
-  p.rows_per = std::max(1, (p.S + p.chunks - 1) / p.chunks);
-  p.chunks = (p.S + p.rows_per - 1) / p.rows_per;  // 0 without rows: the sums are zeros
+  const RowChunks chunks = row_chunks(p.S, norm_grad_chunks(p.B, p.S, p.C));
+  p.rows_per = chunks.rows_per;
+  p.chunks = chunks.count;  // 0 without rows: the sums are zeros
   const hipError_t e = p.chunks == 0 ? hipSuccess : with_shape(p.C, [&](auto w, auto np) {
     constexpr int W = decltype(w)::value, NP = decltype(np)::value;
     constexpr int threads = W > 4 ? 64 * W : NORM_THREADS;
