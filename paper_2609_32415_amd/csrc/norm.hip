@@ -468,10 +468,13 @@ hipError_t launch_norm(int dtype, NormParams p, hipStream_t stream) {
 
 // A chunk's column sums cost a store and a load of 2 C values, a launch of few chunks leaves loads unhidden: 512 chunks, two
 // rows each at least, and 256 of wide rows. Measured with every gradient, 256 / 512 / 1024 chunks: 16384 x 2048 bf16
-// 66 / 51 / 57 us, 4096 x 4096 31 / 31 / 39, 2048 x 8192 30 / 39 / 57.
+// 66 / 51 / 57 us, 4096 x 4096 31 / 31 / 39, 2048 x 8192 30 / 39 / 57. Long entries have more of them: a chunk's fp32 sums
+// are off by up to a rounding a row, so it has 128 rows at most (2^20 chunks an entry: longer from 2^27 rows on).
+constexpr int64_t NORM_CHUNK_ROWS = 128, NORM_MOST_CHUNKS = int64_t(1) << 20;
 int norm_grad_chunks(int32_t B, int32_t S, int32_t C) {
   const int64_t most = std::max<int64_t>(1, (C > 4096 ? 256 : 512) / B);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(most, ((int64_t)S + 1) / 2));
+  const int64_t least = std::min(((int64_t)S + NORM_CHUNK_ROWS - 1) / NORM_CHUNK_ROWS, NORM_MOST_CHUNKS);
+  return (int)std::max<int64_t>({1, least, std::min<int64_t>(most, ((int64_t)S + 1) / 2)});
 }
 
 hipError_t launch_norm_grad(int dtype, NormGradParams p, hipStream_t stream) {
