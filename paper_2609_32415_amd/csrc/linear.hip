@@ -879,9 +879,13 @@ hipError_t launch_linear_transpose(int format, MxView w, int32_t N, int32_t K, i
                           : launch_kernel(linear_transpose_kernel<false>, grid, dim3(256), 0, stream, w, N, K, ld, o);
 }
 
+// Chunks that fill the CUs, of 16 rows at least, and of 512 at most: a thread adds up a quarter of a chunk's rows in fp32,
+// with up to a rounding each. (A launch has 65535 of them: longer chunks from 2^25 rows on.)
+constexpr int64_t SUM_CHUNK_ROWS = 512, SUM_MOST_CHUNKS = 65535;
 int column_sum_chunks(int64_t M, int32_t N) {
   const int64_t cols = (N + 511) / 512;
-  return (int)std::max<int64_t>(1, std::min<int64_t>((1024 + cols - 1) / cols, (M + 15) / 16));
+  const int64_t least = std::min((M + SUM_CHUNK_ROWS - 1) / SUM_CHUNK_ROWS, SUM_MOST_CHUNKS);
+  return (int)std::max<int64_t>({1, least, std::min<int64_t>((1024 + cols - 1) / cols, (M + 15) / 16)});
 }
 
 hipError_t launch_column_sum(int dtype, View g, int32_t rows, int64_t M, int32_t N, float* part, void* out,

@@ -2,8 +2,8 @@
 
 Every row is the same, with mean 0 and deviation 1 given as its statistics, so that h is x itself. The sums run in fp32
 over chunks of 128 rows at most, which leaves a rounding a row and one of the product, and in fp64 from there on, with
-one rounding of the result: 130 of 2^-24 of the sum of the terms' sizes. (Sums of equal terms: in one chunk of 16384 rows
-they would be off by up to 2700.)"""
+one rounding of the result: 130 of 2^-24 of the sum of the terms' sizes. (Sums of equal terms: in one chunk of 16384
+rows they would be off by up to 2700.)"""
 
 import pytest
 import torch
