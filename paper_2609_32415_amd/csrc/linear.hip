@@ -753,7 +753,7 @@ __global__ __launch_bounds__(256) void column_sum_final_kernel(const float* part
   if (f32) {
     static_cast<float*>(out)[c] = (float)sum;
   } else {
-    static_cast<uint16_t*>(out)[c] = __builtin_bit_cast(uint16_t, (__bf16)(float)sum);
+    static_cast<uint16_t*>(out)[c] = bf16_bits(sum);
   }
 }
 

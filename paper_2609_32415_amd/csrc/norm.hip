@@ -101,8 +101,6 @@ struct Lane {
   __device__ __forceinline__ void store(char* p, const Oct& o, int k) const;
 };
 
-__device__ __forceinline__ uint16_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
-
 template <int L, bool VEC>
 template <bool BF16>
 __device__ __forceinline__ void Lane<L, VEC>::store(char* p, const Oct& o, int k) const {
@@ -367,7 +365,7 @@ __device__ __forceinline__ void put_param(void* p, bool f32, int64_t i, double v
   if (f32) {
     static_cast<float*>(p)[i] = (float)v;
   } else {
-    static_cast<uint16_t*>(p)[i] = bf16_bits((float)v);
+    static_cast<uint16_t*>(p)[i] = bf16_bits(v);
   }
 }
 
