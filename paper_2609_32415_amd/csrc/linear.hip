@@ -776,8 +776,7 @@ RA_LINEAR_TILES(B16, B16)
 #undef RA_LINEAR_TILES
 #define RA_LINEAR_FEW_OF(KX, KW, LDS)                                             \
   template __global__ void linear_few_kernel<KX, KW, LDS, X_CODES>(LinearParams); \
-  template __global__ void linear_few_kernel<KX, KW, LDS, X_BF16>(LinearParams);  \
-  template __global__ void linear_few_kernel<KX, KW, LDS, X_F32>(LinearParams);
+  template __global__ void linear_few_kernel<KX, KW, LDS, X_BF16>(LinearParams);
 #define RA_LINEAR_FEW(KX, KW)        \
   RA_LINEAR_FEW_OF(KX, KW, FEW_LDS) \
   RA_LINEAR_FEW_OF(KX, KW, FEW_MORE_LDS)
@@ -785,6 +784,8 @@ RA_LINEAR_FEW(FP4, FP4)
 RA_LINEAR_FEW(FP4, FP8)
 RA_LINEAR_FEW(FP8, FP4)
 RA_LINEAR_FEW(FP8, FP8)
+template __global__ void linear_few_kernel<FP4, FP4, FEW_LDS, X_F32>(LinearParams);
+template __global__ void linear_few_kernel<FP4, FP4, FEW_MORE_LDS, X_F32>(LinearParams);
 #undef RA_LINEAR_FEW
 #undef RA_LINEAR_FEW_OF
 
@@ -802,7 +803,9 @@ hipError_t run_few(const LinearParams& p, hipStream_t stream) {
   const dim3 grid((unsigned)((p.N + 31) / 32));
   const auto run = [&](auto* kernel) { return launch_kernel(kernel, grid, dim3(64 * FEW_WAVES), 0, stream, p); };
   if (p.x_plain.p == nullptr) return run(linear_few_kernel<KX, KW, LDS, X_CODES>);
-  return p.x_f32 ? run(linear_few_kernel<KX, KW, LDS, X_F32>) : run(linear_few_kernel<KX, KW, LDS, X_BF16>);
+  if constexpr (KX == FP4 && KW == FP4)  // fp32 rows with an e4m3 side are products of values
+    if (p.x_f32) return run(linear_few_kernel<KX, KW, LDS, X_F32>);
+  return run(linear_few_kernel<KX, KW, LDS, X_BF16>);
 }
 template <int KX, int KW>
 hipError_t run_few(const LinearParams& p, hipStream_t stream) {
