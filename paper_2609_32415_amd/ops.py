@@ -1137,6 +1137,8 @@ def mx_linear(x, w, bias=None, *, fmt=None, dtype=None, out=None, workspace=None
     if isinstance(x, MxTensor):
         if bias is not None and torch.is_grad_enabled() and bias.requires_grad:
             raise ValueError("codes carry no gradients: give mx_linear plain rows, or use torch.no_grad()")
+        if out is not None and torch.is_grad_enabled() and out.requires_grad:
+            raise ValueError("out cannot be given where a tensor requires grad")
         B, one, S, K = x.shape
         if one != 1:
             raise ValueError(f"x must be an MxTensor [B, 1, S, n_in], got {tuple(x.shape)}")
