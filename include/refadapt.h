@@ -541,7 +541,7 @@ typedef struct {
  *   dx = r * (e - mean(e) - h * mean(e * h))
  *   dweight = sum of dy * (1 + scale) * h, dbias = sum of dy * (1 + scale)   (all rows)
  *   dscale[b] = sum of dy * (h * weight + bias), dshift[b] = sum of dy       (rows of b)
- * Sums are fp32 over a chunk of rows (128 at most; longer from 2^27 rows an entry on)
+ * Sums are fp32 over a chunk of rows (512 at most; longer from 2^30 rows an entry on)
  * and fp64 over the chunks, in a fixed order
  * (results are bitwise reproducible), rounded once to param_dtype. dx may be dy or x
  * itself. Without rows the sums are zeros. A scale shared over the batch

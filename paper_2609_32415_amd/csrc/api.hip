@@ -1011,7 +1011,7 @@ size_t refadapt_layer_norm_grad_workspace_size(const ra_norm_desc* desc) {
   if (check_norm_desc("layer_norm_grad_workspace_size", desc) != RA_OK) return 0;
   const size_t B = desc->batch, C = desc->width;
   return (B > 1 ? padded(B * 2 * C * sizeof(double)) : 0) +
-         B * norm_grad_chunks(desc->batch, desc->rows, desc->width) * 2 * C * sizeof(float);
+         B * norm_grad_chunks(desc->batch, desc->rows, desc->width, true) * 2 * C * sizeof(float);
 }
 
 ra_status refadapt_layer_norm_grad(const ra_norm_desc* desc, const ra_norm_grad_args* args, void* stream) {

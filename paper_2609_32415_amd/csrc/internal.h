@@ -214,7 +214,7 @@ struct NormGradParams {
   int32_t B, S, C;
   bool param_f32, vec;
 };
-int norm_grad_chunks(int32_t B, int32_t S, int32_t C);
+int norm_grad_chunks(int32_t B, int32_t S, int32_t C, bool sums);  // sums: of the parameters' gradients
 hipError_t launch_norm_grad(int dtype, NormGradParams p, hipStream_t stream);
 
 // y [M, N] = x [M, K] w [N, K]^T + bias over codes (kinds MX_FP4, MX_FP8) with scale bytes, or over bf16 values (kind 2).

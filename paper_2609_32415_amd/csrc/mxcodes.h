@@ -45,8 +45,8 @@ struct RawOct {
 
 // bf16 bits of x, rounded to nearest even.
 __device__ __forceinline__ uint16_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
-// The same of an fp64 value, in one rounding: by way of fp32 cut towards zero, whose last bit is set where something was
-// cut off (a nearest fp32 value may lie halfway between two bf16 values where x does not).
+// The same of an fp64 value, in one rounding: by way of fp32 cut towards zero, whose last bit is set where something
+// was cut off (a nearest fp32 value may lie halfway between two bf16 values where x does not).
 __device__ __forceinline__ uint16_t bf16_bits(double x) {
   const float f = (float)x;
   uint32_t u = __float_as_uint(f);

@@ -144,16 +144,16 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS, 4) void norm_kernel(
   constexpr int L = 64 * W;
   __shared__ float slots[2][2][W];
   const int b = blockIdx.y, C = p.C;
-  const int s0 = blockIdx.x * p.rows_per, group = (int)threadIdx.x / L;
-  uint32_t s = s0 + group;                       // (of a row past the last: 2^31 and more)
-  int left = min(p.rows_per, p.S - s0) - group;  // rows of the chunk from s on
+  const int s0 = blockIdx.x * p.rows_per;
+  const uint32_t s1 = s0 + min(p.rows_per, p.S - s0);  // unsigned: a row past the last may pass 2^31
   const bool pf32 = p.param_f32;
   const Lane<L, VEC> ln{(int)(threadIdx.x % L), C};
   constexpr int esz = BF16 ? 2 : 4;
   const char* const x = static_cast<const char*>(p.x.p) + b * p.x.sb * esz;
+  uint32_t s = s0 + threadIdx.x / L;
   Oct v[NP];
   RawOct<BF16> next[NP];
-  if (left > 0) {
+  if (s < s1) {
 #pragma unroll
     for (int k = 0; k < NP; ++k) next[k] = ln.template raw<BF16>(x + s * p.x.ss * esz, k);
   }
@@ -173,7 +173,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS, 4) void norm_kernel(
       add[k].f[i] = fmaf(a.f[i], 1.f + m.f[i], t.f[i]);
     }
   }
-  for (int turn = 0; left > 0; left -= ROWS, s += ROWS, turn ^= 1) {
+  for (int turn = 0; s < s1; s += ROWS, turn ^= 1) {
     float sum = 0.f;
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
@@ -181,7 +181,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS, 4) void norm_kernel(
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum += v[k].f[i];
     }
-    if (left > ROWS) {
+    if (s + ROWS < s1) {
 #pragma unroll
       for (int k = 0; k < NP; ++k) next[k] = ln.template raw<BF16>(x + (s + ROWS) * p.x.ss * esz, k);
     }
@@ -239,9 +239,10 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS) void norm_grad_kerne
   constexpr int ROWS = W >= 4 ? 1 : NORM_THREADS / 64 / W;
   constexpr int L = 64 * W;
   __shared__ float slots[2][2][W];
-  const int group = threadIdx.x / L;
+  const int group = ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / L) : 0;  // scalar, and the row with it
   const int b = blockIdx.y, C = p.C;
   const int s0 = blockIdx.x * p.rows_per;
+  const uint32_t s1 = s0 + min(p.rows_per, p.S - s0);
   const bool pf32 = p.param_f32;
   const Lane<L, VEC> ln{(int)(threadIdx.x % L), C};
   constexpr int esz = BF16 ? 2 : 4;
@@ -262,8 +263,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS) void norm_grad_kerne
     }
   };
   uint32_t s = s0 + group;
-  int left = min(p.rows_per, p.S - s0) - group;
-  if (left > 0) fetch(s);
+  if (s < s1) fetch(s);
 #pragma unroll
   for (int k = 0; k < NP; ++k) {
     const Oct w = ln.param(p.weight, pf32, k, 1.f), m = ln.param(sc, pf32, k, 0.f);
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS) void norm_grad_kerne
       P[k].f[i] = D[k].f[i] = 0.f;
     }
   }
-  for (int turn = 0; left > 0; left -= ROWS, s += ROWS, turn ^= 1) {
+  for (int turn = 0; s < s1; s += ROWS, turn ^= 1) {
     Oct h[NP], e[NP];
     const float2 now = stn;
     float a0 = 0.f, a1 = 0.f;
@@ -291,7 +291,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS) void norm_grad_kerne
         a1 = fmaf(e[k].f[i], h[k].f[i], a1);
       }
     }
-    if (left > ROWS) fetch(s + ROWS);
+    if (s + ROWS < s1) fetch(s + ROWS);
     // both sums behind one barrier; the slots of the row before stay readable (two sets in turn)
 #pragma unroll
     for (int m = 32; m > 0; m >>= 1) {
@@ -467,16 +467,18 @@ hipError_t launch_norm(int dtype, NormParams p, hipStream_t stream) {
 // A chunk's column sums cost a store and a load of 2 C values, a launch of few chunks leaves loads unhidden: 512 chunks, two
 // rows each at least, and 256 of wide rows. Measured with every gradient, 256 / 512 / 1024 chunks: 16384 x 2048 bf16
 // 66 / 51 / 57 us, 4096 x 4096 31 / 31 / 39, 2048 x 8192 30 / 39 / 57. Long entries have more of them: a chunk's fp32 sums
-// are off by up to a rounding a row, so it has 128 rows at most (2^20 chunks an entry: longer from 2^27 rows on).
-constexpr int64_t NORM_CHUNK_ROWS = 128, NORM_MOST_CHUNKS = int64_t(1) << 20;
-int norm_grad_chunks(int32_t B, int32_t S, int32_t C) {
+// are off by up to a rounding a row, so it has 512 rows at most (2^21 chunks an entry: longer from 2^30 rows on). Chunks of
+// 128 cost 16 x 16384 x 2048 bf16 6% (671 us for 630).
+constexpr int64_t NORM_CHUNK_ROWS = 512, NORM_MOST_CHUNKS = int64_t(1) << 21;
+int norm_grad_chunks(int32_t B, int32_t S, int32_t C, bool sums) {
   const int64_t most = std::max<int64_t>(1, (C > 4096 ? 256 : 512) / B);
-  const int64_t least = std::min(((int64_t)S + NORM_CHUNK_ROWS - 1) / NORM_CHUNK_ROWS, NORM_MOST_CHUNKS);
+  const int64_t least =
+      sums ? std::min(((int64_t)S + NORM_CHUNK_ROWS - 1) / NORM_CHUNK_ROWS, NORM_MOST_CHUNKS) : int64_t(1);
   return (int)std::max<int64_t>({1, least, std::min<int64_t>(most, ((int64_t)S + 1) / 2)});
 }
 
 hipError_t launch_norm_grad(int dtype, NormGradParams p, hipStream_t stream) {
-  const RowChunks chunks = row_chunks(p.S, norm_grad_chunks(p.B, p.S, p.C));
+  const RowChunks chunks = row_chunks(p.S, norm_grad_chunks(p.B, p.S, p.C, p.part != nullptr));
   p.rows_per = chunks.rows_per;
   p.chunks = chunks.count;  // 0 without rows: the sums are zeros
   const hipError_t e = p.chunks == 0 ? hipSuccess : with_shape(p.C, [&](auto w, auto np) {

@@ -1,9 +1,10 @@
 """The layer norm's parameter gradients over many rows of many batch entries: their error does not grow with the rows.
 
 Every row is the same, with mean 0 and deviation 1 given as its statistics, so that h is x itself. The sums run in fp32
-over chunks of 128 rows at most, which leaves a rounding a row and one of the product, and in fp64 from there on, with
-one rounding of the result: 130 of 2^-24 of the sum of the terms' sizes. (Sums of equal terms: in one chunk of 16384
-rows they would be off by up to 2700.)"""
+over chunks of 512 rows at most, which leaves a rounding a row and one of the product, and in fp64 from there on, with
+one rounding of the result: 514 of 2^-24 of the sum of the terms' sizes. Up to 1024 columns four wavefronts share a
+chunk's rows, and their sums take three more: 133. (Sums of equal terms: in one chunk of 16384 rows they would be off by
+up to 2700, and by up to 170 of 1024.)"""
 
 import pytest
 import torch
@@ -25,4 +26,4 @@ def test_sums(B, S, C):
     got = ops.layer_norm_grad(spread(dy), spread(x), stats, wanted=(False, True, True, True, True))[1:]
     P, D = (dy.double() * x.double()) * S, dy.double() * S
     for t, exact in zip(got, (P * B, D * B, P.expand(B, C), D.expand(B, C))):
-        assert float(((t.double() - exact).abs() / exact).max()) <= 130 * U
+        assert float(((t.double() - exact).abs() / exact).max()) <= (133 if C <= 1024 else 514) * U
