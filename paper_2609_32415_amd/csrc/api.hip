@@ -847,8 +847,8 @@ ra_status check_rows(const char* who, const char* name, const ra_tensor& t, int 
   if (t.data == nullptr) return fail(RA_EINVAL, "%s: null %s", who, name);
   if (t.stride_b < 0 || t.stride_s < 0) return fail(RA_EINVAL, "%s: negative stride of %s", who, name);
   if (rows > 1 && t.stride_s < width)
-    return fail(RA_EINVAL, "%s: row stride %lld of %s is smaller than its %d elements", who, (long long)t.stride_s, name,
-                width);
+    return fail(RA_EINVAL, "%s: row stride %lld of %s is smaller than its %d elements", who, (long long)t.stride_s,
+                name, width);
   if (reinterpret_cast<uintptr_t>(t.data) % (dtype == RA_BF16 ? 2 : 4) != 0)
     return fail(RA_EUNSUPPORTED, "%s: %s is not aligned to its elements", who, name);
   return RA_OK;
@@ -856,8 +856,8 @@ ra_status check_rows(const char* who, const char* name, const ra_tensor& t, int 
 
 int64_t floor_div(int64_t a, int64_t b) { return a / b - (a % b < 0 ? 1 : 0); }
 
-// Whether rows of wy elements, the first of them d elements behind that of rows of wx elements, share elements with those.
-// Rows at other strides do where the ranges meet.
+// Whether rows of wy elements, the first of them d elements behind that of rows of wx elements, share elements with
+// those. Rows at other strides do where the ranges meet.
 bool entries_overlap(int64_t d, int32_t wy, int64_t y_s, int32_t wx, int64_t x_s, int32_t rows) {
   if (d + (rows - 1) * y_s + wy <= 0 || d >= (rows - 1) * x_s + wx) return false;
   if (y_s != x_s) return true;
@@ -866,10 +866,12 @@ bool entries_overlap(int64_t d, int32_t wy, int64_t y_s, int32_t wx, int64_t x_s
 }
 
 // Whether rows y of wy elements share elements with rows x of wx of the same type. Slices of one buffer, at the same
-// strides, whose rows or entries lie between each other's do not; rows at other strides do where their entries' ranges meet.
+// strides, whose rows or entries lie between each other's do not; rows at other strides do where their entries' ranges
+// meet.
 bool rows_overlap(const ra_tensor& y, int32_t wy, const ra_tensor& x, int32_t wx, int dtype, int32_t batch,
                   int32_t rows) {
-  const int64_t apart = (reinterpret_cast<intptr_t>(y.data) - reinterpret_cast<intptr_t>(x.data)) / (dtype == RA_BF16 ? 2 : 4);
+  const int64_t apart =
+      (reinterpret_cast<intptr_t>(y.data) - reinterpret_cast<intptr_t>(x.data)) / (dtype == RA_BF16 ? 2 : 4);
   const int64_t y_b = batch > 1 ? y.stride_b : 0, x_b = batch > 1 ? x.stride_b : 0;
   const int64_t y_s = rows > 1 ? y.stride_s : wy + wx, x_s = rows > 1 ? x.stride_s : y_s;
   const int64_t span_y = (rows - 1) * y_s + wy, span_x = (rows - 1) * x_s + wx;
@@ -1124,7 +1126,8 @@ bool linear_by_values(const ra_linear_desc& d) {
 bool linear_takes_plain(const ra_linear_desc& d) {
   return !linear_by_values(d) && linear_is_few(d.x_format, (int64_t)d.batch * d.rows, d.n_out, d.n_in);
 }
-// Scale rows that do not start at whole words are copied: where a row is not in whole words, room for that is asked for.
+// Scale rows that do not start at whole words are copied: where a row is not in whole words, room for that is asked
+// for.
 bool in_words(const ra_mx_tensor& t, int64_t row) {
   return (reinterpret_cast<uintptr_t>(t.scales) & 3) == 0 && (row & 3) == 0;
 }

@@ -217,7 +217,8 @@ struct NormGradParams {
 int norm_grad_chunks(int32_t B, int32_t S, int32_t C, bool sums);  // sums: of the parameters' gradients
 hipError_t launch_norm_grad(int dtype, NormGradParams p, hipStream_t stream);
 
-// y [M, N] = x [M, K] w [N, K]^T + bias over codes (kinds MX_FP4, MX_FP8) with scale bytes, or over bf16 values (kind 2).
+// y [M, N] = x [M, K] w [N, K]^T + bias over codes (kinds MX_FP4, MX_FP8) with scale bytes, or over bf16 values (kind
+// 2).
 constexpr int kLinearBf16 = 2;
 constexpr int64_t kLinearMaxStride = int64_t(1) << 22;  // bytes of a row: 256 rows stay within 32-bit offsets
 struct LinearParams {

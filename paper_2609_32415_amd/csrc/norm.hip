@@ -1,4 +1,5 @@
-// Layer norm of hidden rows with an affine map and the modulation of diffusion transformers, and its gradients (gfx950).
+// Layer norm of hidden rows with an affine map and the modulation of diffusion transformers, and its gradients
+// (gfx950).
 //
 // Of a row x of C elements with mean m and r = 1 / sqrt(mean((x - m)^2) + eps): h = (x - m) r, n = h w + b,
 // y = n (1 + s) + t, with w, b of the block and s, t of the row's batch entry. With e = g (1 + s) w the gradient
@@ -10,10 +11,10 @@
 // of row chunks fp64; results are rounded once. Sums run in a fixed order: outputs repeat bit for bit.
 //
 // Bound by memory: a row stays in registers between its passes, and each workgroup has the next one on its way. A large
-// copy moves 5.1 TB/s; measured in bf16, replayed from a graph: 4096 x 4096 with its modulation 14.2 us (4.7 TB/s), 16384 x
-// 2048 with every parameter 24.5 (5.5 TB/s; the rows partly in the last-level cache; 29 without); dx alone there 41.5 (4.8
-// TB/s), with the four sums 51. Rows in whole 16-byte units have kernels of their own (VEC): one kernel for both takes 16.1
-// and 28.6 us.
+// copy moves 5.1 TB/s; measured in bf16, replayed from a graph: 4096 x 4096 with its modulation 14.2 us (4.7 TB/s),
+// 16384 x 2048 with every parameter 24.5 (5.5 TB/s; the rows partly in the last-level cache; 29 without); dx alone
+// there 41.5 (4.8 TB/s), with the four sums 51. Rows in whole 16-byte units have kernels of their own (VEC): one kernel
+// for both takes 16.1 and 28.6 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -47,9 +48,9 @@ __device__ __forceinline__ float row_sum(float v, float* slot) {
 // A row's elements at any alignment of theirs: the hardware takes wide loads and stores there too.
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
 
-// The elements of a row that a lane holds, 8 a piece: piece lane + L k of the row's. With VEC rows are in whole 16-byte units;
-// without, they lie at any alignment and their last piece may be a part (2 x 1009 x 1001 fp32: 8.6 us; element by element
-// 10.3).
+// The elements of a row that a lane holds, 8 a piece: piece lane + L k of the row's. With VEC rows are in whole 16-byte
+// units; without, they lie at any alignment and their last piece may be a part (2 x 1009 x 1001 fp32: 8.6 us; element
+// by element 10.3).
 template <int L, bool VEC>
 struct Lane {
   int lane, C;
@@ -115,8 +116,9 @@ __device__ __forceinline__ void Lane<L, VEC>::store(char* p, const Oct& o, int k
       else
         w[i / 4][i % 4] = __float_as_uint(o.f[i]);
     }
-    if constexpr (BF16 && VEC) {  // past the caches (gradient of 16384 x 2048 46.5 us, past them 44.7); fp32 rows are sums
-      __builtin_nontemporal_store(w[0], reinterpret_cast<u32x4*>(p));  // too, which are read next
+    if constexpr (BF16 && VEC) {
+      // past the caches (gradient of 16384 x 2048 46.5 us, past them 44.7); fp32 rows are sums too, which are read next
+      __builtin_nontemporal_store(w[0], reinterpret_cast<u32x4*>(p));
     } else {
       reinterpret_cast<u32x4_any*>(p)[0] = w[0];
       if constexpr (!BF16) reinterpret_cast<u32x4_any*>(p)[1] = w[1];
@@ -134,9 +136,9 @@ __device__ __forceinline__ void Lane<L, VEC>::store(char* p, const Oct& o, int k
   }
 }
 
-// blockIdx.y: batch entry, x: chunk of its rows. W wavefronts work on a row, with W = 1 each wavefront of the workgroup on
-// rows of its own; NP pieces a lane. The parameters, folded to y = h p + q, stay in registers over the chunk, and the next
-// row is on its way while one is worked on. y goes out as it is or, with a format, as codes of the values
+// blockIdx.y: batch entry, x: chunk of its rows. W wavefronts work on a row, with W = 1 each wavefront of the workgroup
+// on rows of its own; NP pieces a lane. The parameters, folded to y = h p + q, stay in registers over the chunk, and
+// the next row is on its way while one is worked on. y goes out as it is or, with a format, as codes of the values
 // rounded to the rows' type (the bits that quantising y itself gives).
 template <bool BF16, int W, int NP, bool VEC>
 __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS, 4) void norm_kernel(NormParams p) {
@@ -233,7 +235,9 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS, 4) void norm_kernel(
   }
 }
 
-// The same chunks. With W = 1 the workgroup's wavefronts join their column sums in shared memory.
+// The same chunks. With W = 1 the workgroup's wavefronts join their column sums in shared memory. Rows above 8192
+// elements take 1024 threads of 128 registers, which do not hold P, D and the row: 8 to 35 values a lane go to scratch
+// and back (2048 x 16384, every gradient: bf16 61 us, fp32 143; the bytes alone take 39 and 79).
 template <bool BF16, int W, int NP, bool VEC>
 __global__ __launch_bounds__(W > 4 ? 64 * W : NORM_THREADS) void norm_grad_kernel(NormGradParams p) {
   constexpr int ROWS = W >= 4 ? 1 : NORM_THREADS / 64 / W;
@@ -369,8 +373,9 @@ __device__ __forceinline__ void put_param(void* p, bool f32, int64_t i, double v
   }
 }
 
-// Joins the chunks' column sums of batch entry blockIdx.y: FIN_COLS columns a workgroup, its groups of threads take chunks
-// in turn (2048 columns of 512 chunks 7.4 us; 10.8 with 32 columns, 8.6 with 8). With several entries the terms of dw and db go to `entry` [B][2][C], which a second launch adds up.
+// Joins the chunks' column sums of batch entry blockIdx.y: FIN_COLS columns a workgroup, its groups of threads take
+// chunks in turn (2048 columns of 512 chunks 7.4 us; 10.8 with 32 columns, 8.6 with 8). With several entries the terms
+// of dw and db go to `entry` [B][2][C], which a second launch adds up.
 constexpr int FIN_COLS = 16, FIN_GROUPS = 64, FIN_UNROLL = 4;
 __global__ __launch_bounds__(FIN_COLS * FIN_GROUPS) void norm_grad_final_kernel(NormGradParams p) {
   __shared__ double held[2][FIN_GROUPS][FIN_COLS];
@@ -452,8 +457,8 @@ hipError_t launch_norm(int dtype, NormParams p, hipStream_t stream) {
     constexpr int W = decltype(w)::value, NP = decltype(np)::value;
     constexpr int rows = W >= 4 ? 1 : NORM_THREADS / 64 / W, threads = W > 4 ? 64 * W : NORM_THREADS;
     // Workgroups that are at work at once, about: the parameters are read once a chunk and the next row is on its way.
-    // bf16, us, 512 / 1024 / 2048 / 4096 chunks: 4096 x 4096 16.8 / 14.1 / 15.6 / 19.6, 2048 x 8192 15.6 / 16.9 / 20.7 /
-    // 20.7, 16384 x 2048 38.6 / 25.7 / 24.5 / 24.4, 16384 x 512 10.8 / 8.8 / 8.4 / 10.3.
+    // bf16, us, 512 / 1024 / 2048 / 4096 chunks: 4096 x 4096 16.8 / 14.1 / 15.6 / 19.6, 2048 x 8192 15.6 / 16.9 / 20.7
+    // / 20.7, 16384 x 2048 38.6 / 25.7 / 24.5 / 24.4, 16384 x 512 10.8 / 8.8 / 8.4 / 10.3.
     const int64_t most = W > 4 ? 512 : W == 4 && NP == 1 ? 2048 : 1024;
     const RowChunks chunks = row_chunks(p.S, std::min<int64_t>(most / p.B, ((int64_t)p.S + rows - 1) / rows));
     p.rows_per = chunks.rows_per;
@@ -464,11 +469,11 @@ hipError_t launch_norm(int dtype, NormParams p, hipStream_t stream) {
   });
 }
 
-// A chunk's column sums cost a store and a load of 2 C values, a launch of few chunks leaves loads unhidden: 512 chunks, two
-// rows each at least, and 256 of wide rows. Measured with every gradient, 256 / 512 / 1024 chunks: 16384 x 2048 bf16
-// 66 / 51 / 57 us, 4096 x 4096 31 / 31 / 39, 2048 x 8192 30 / 39 / 57. Long entries have more of them: a chunk's fp32 sums
-// are off by up to a rounding a row, so it has 512 rows at most (2^21 chunks an entry: longer from 2^30 rows on). Chunks of
-// 128 cost 16 x 16384 x 2048 bf16 6% (671 us for 630).
+// A chunk's column sums cost a store and a load of 2 C values, a launch of few chunks leaves loads unhidden: 512
+// chunks, two rows each at least, and 256 of wide rows. Measured with every gradient, 256 / 512 / 1024 chunks: 16384 x
+// 2048 bf16 66 / 51 / 57 us, 4096 x 4096 31 / 31 / 39, 2048 x 8192 30 / 39 / 57. Long entries have more of them: a
+// chunk's fp32 sums are off by up to a rounding a row, so it has 512 rows at most (2^21 chunks an entry: longer from
+// 2^30 rows on). Chunks of 128 cost 16 x 16384 x 2048 bf16 6% (671 us for 630).
 constexpr int64_t NORM_CHUNK_ROWS = 512, NORM_MOST_CHUNKS = int64_t(1) << 21;
 int norm_grad_chunks(int32_t B, int32_t S, int32_t C, bool sums) {
   const int64_t most = std::max<int64_t>(1, (C > 4096 ? 256 : 512) / B);
