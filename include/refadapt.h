@@ -513,7 +513,9 @@ typedef struct {
  * in fp32, rounded once to dtype; with y_mx those rounded rows become codes as
  * refadapt_mx_commit makes them (bit for bit). y may be x itself (same data and
  * strides, batch entries apart); otherwise what is written overlaps nothing else.
- * A row with a NaN or an infinity is NaN throughout and touches no other row.
+ * A row with a NaN or an infinity is NaN throughout and touches no other row. So is one
+ * whose sum passes fp32's range; where only the squares of its differences add up past
+ * it, h is 0.
  * Errors: RA_EINVAL (null desc, args or tensors, both of y and y_mx, sizes, dtypes,
  * eps, negative or overlapping strides, y over a part of x, x broadcast over the batch
  * and normalised in place), RA_EUNSUPPORTED (width above 16384, or not a multiple of 32 with y_mx,
@@ -579,10 +581,11 @@ typedef struct {
  *   y = Q(x) w^T + bias
  * with Q(x) the values of x as refadapt_mx_commit rounds it to x_format (of x_mx: its
  * values) and w the values of the weights. Sums are fp32, rounded once to dtype. Of
- * RA_BF16 results with an RA_MXFP8 side each 64 products are added by a matrix
+ * RA_BF16 results with an RA_MXFP8 side products are added in eights by a matrix
  * instruction that keeps about 13 bits below the largest of them (an error of at most
  * 2^-10 of the sum of their magnitudes, about 2e-5 of the result for normal data);
- * RA_F32 results and those of two RA_MXFP4 sides are exact to fp32 roundings. Codes
+ * RA_F32 results and those of two RA_MXFP4 sides are exact to fp32 roundings (RA_F32
+ * with an RA_MXFP8 side: of scale bytes that a commit writes). Codes
  * under scale byte 255 are NaN. Results are deterministic. Scale rows that are not in
  * whole 4-byte words are read as the aligned words that hold them.
  * The workspace needs no initialisation and must not be used by another call that runs
@@ -609,9 +612,11 @@ typedef struct {
  *
  *   dx = dy w            (the rounding of x passes gradients on as they are)
  *   dbias = sum over the rows of dy
- * with w the values of the weights, which have no gradient of their own. Products and
- * sums are exact to fp32 roundings (fp32 dy enters as three bf16 terms), rounded once
- * to dtype, and deterministic. Where dtype is RA_BF16 and n_out a multiple of 8, rows
+ * with w the values of the weights (under scale bytes that a commit writes), which have
+ * no gradient of their own. Products and sums are exact to fp32 roundings, rounded once
+ * to dtype, and deterministic. fp32 dy enters as three bf16 terms, exact from 2^-110 in
+ * size on; of smaller values the bits below 2^-133 are left out. dbias is summed in fp32
+ * over up to 512 rows (2048 from 2^25 rows on) and in fp64 over the rest. Where dtype is RA_BF16 and n_out a multiple of 8, rows
  * of dy lie in whole 16-byte units and evenly over the batch. Without rows dbias is
  * zeros. desc->x_format is not read beyond its check.
  * Errors: as refadapt_mx_linear; RA_EINVAL (no gradient wanted, dx over dy).

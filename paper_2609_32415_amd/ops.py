@@ -963,7 +963,7 @@ def _norm(x, weight, bias, scale, shift, eps, y=None, y_mx=None, stats=None):
 
 
 def layer_norm(x, weight=None, bias=None, *, scale=None, shift=None, eps=1e-6, out=None):
-    """Layer norm of rows ``x`` [B, S, C] or [S, C], through ``refadapt_layer_norm``:
+    """Layer norm of rows ``x`` [B, S, C] (B at least 1) or [S, C], through ``refadapt_layer_norm``:
     (h * weight + bias) * (1 + scale) + shift with h the normalised rows.
 
     ``weight``, ``bias`` [C] and the modulation ``scale``, ``shift`` [B, C] (for [S, C] rows [C] too; rows of a larger
@@ -1125,8 +1125,8 @@ def _linear_workspace(nbytes, workspace, where, dev):
 def mx_linear(x, w, bias=None, *, fmt=None, dtype=None, out=None, workspace=None):
     """The projection Q(x) w^T + bias through ``refadapt_mx_linear``.
 
-    ``x``: rows [B, S, n_in] or [S, n_in] in whole 16-byte units, rounded to codes of ``fmt`` (default: ``w``'s) on the
-    way, or an ``MxTensor`` [B, 1, S, n_in] (``layer_norm_mx``), whose result is [B, S, n_out] of ``dtype`` (default:
+    ``x``: rows [B, S, n_in] (B at least 1) or [S, n_in] in whole 16-byte units, rounded to codes of ``fmt`` (default:
+    ``w``'s) on the way, or an ``MxTensor`` [B, 1, S, n_in] (``layer_norm_mx``), whose result is [B, S, n_out] of ``dtype`` (default:
     bias's, or bfloat16).
     ``w``: an ``MxTensor`` [1, 1, n_out, n_in] (``mx_weight``), or rows of one. ``bias`` [n_out] is of the result's
     dtype. ``out`` may be any rows with contiguous elements, a slice of a larger tensor too.
