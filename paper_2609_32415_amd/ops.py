@@ -1126,8 +1126,8 @@ def mx_linear(x, w, bias=None, *, fmt=None, dtype=None, out=None, workspace=None
     """The projection Q(x) w^T + bias through ``refadapt_mx_linear``.
 
     ``x``: rows [B, S, n_in] (B at least 1) or [S, n_in] in whole 16-byte units, rounded to codes of ``fmt`` (default:
-    ``w``'s) on the way, or an ``MxTensor`` [B, 1, S, n_in] (``layer_norm_mx``), whose result is [B, S, n_out] of ``dtype`` (default:
-    bias's, or bfloat16).
+    ``w``'s) on the way, or an ``MxTensor`` [B, 1, S, n_in] (``layer_norm_mx``), whose result is [B, S, n_out] of
+    ``dtype`` (default: bias's, or bfloat16).
     ``w``: an ``MxTensor`` [1, 1, n_out, n_in] (``mx_weight``), or rows of one. ``bias`` [n_out] is of the result's
     dtype. ``out`` may be any rows with contiguous elements, a slice of a larger tensor too.
 
