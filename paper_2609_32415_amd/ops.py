@@ -38,16 +38,16 @@ def _stream():
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
-def _written(*tensors):
-    """Counts the library's writes into tensors of the caller as changes in place, as torch counts its own: a recorded
-    call that saved one of them refuses its backward pass then. (Tensors made in inference mode have no count.)"""
-    torch.autograd.graph.increment_version([t for t in tensors if t is not None and not t.is_inference()])
+# Counts the library's writes into tensors of the caller as changes in place, as torch counts its own: a recorded call
+# that saved one of them refuses its backward pass then.
+_written = torch.autograd.graph.increment_version
 
 
-def _no_tangent(name, t):
+def _no_tangents(**tensors):
     """Forward-mode derivatives: a tensor's pointer would leave its tangent behind. (Asked at a dual level alone.)"""
-    if _forward.unpack_dual(t).tangent is not None:
-        raise ValueError(f"{name} carries a tangent: there are no forward-mode derivatives")
+    for name, t in tensors.items():
+        if t is not None and _forward.unpack_dual(t).tangent is not None:
+            raise ValueError(f"{name} carries a tangent: there are no forward-mode derivatives")
 
 
 def _on_gpu(name, t):
@@ -61,8 +61,6 @@ def _quad(name, t, dtype, shape):
         return _NO_TENSOR
     if not t.is_cuda:
         _on_gpu(name, t)
-    if _forward._current_level >= 0:
-        _no_tangent(name, t)
     sh = t.shape
     if len(sh) != 4:
         raise ValueError(f"{name} must be [B, H, S, d], got {tuple(sh)}")
@@ -79,12 +77,12 @@ def _quad(name, t, dtype, shape):
 
 
 def _view(name, t, dtype=None, shape=None):
+    if _forward._current_level >= 0:
+        _no_tangents(**{name: t})
     return L.ra_tensor(*_quad(name, t, dtype, shape))
 
 
 def _ptr(t):
-    if t is not None and _forward._current_level >= 0:
-        _no_tangent("an input", t)
     return None if t is None else t.data_ptr()
 
 
@@ -119,9 +117,11 @@ class _Underived(torch.autograd.Function):
 
 
 def _attn_out(who, inputs, *results):
-    """``results`` as an ``AttnOut``, tied to ``inputs`` where these require gradients."""
+    """``results``, written, as an ``AttnOut``, tied to ``inputs`` where these require gradients."""
+    written = [t for t in results if t is not None]
+    _written(written)
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs):
-        tied = iter(_Underived.apply(who, [t for t in results if t is not None], *inputs))
+        tied = iter(_Underived.apply(who, written, *inputs))
         results = [t if t is None else next(tied) for t in results]
     return AttnOut(*results)
 
@@ -179,6 +179,9 @@ def joint_attn(
     ``AttnOut``, and a backward pass that reaches them raises NotImplementedError. (Buffers given for them
     stay as they are.)
     """
+    if _forward._current_level >= 0:
+        _no_tangents(q_tgt=q_tgt, k_tgt=k_tgt, v_tgt=v_tgt, q_ref=q_ref, k_ref=k_ref, v_ref=v_ref, k_cache=k_cache,
+                     v_cache=v_cache, q_cache=q_cache)
     B, H, n_tgt, D = q_tgt.shape
     dt = q_tgt.dtype
     if dt not in _DTYPES:
@@ -254,7 +257,6 @@ def joint_attn(
         0 if clock_probe is None else _probe_ptr(clock_probe),
     )
     L.refadapt_joint_attn_packed(L.DESC_PACK.pack(*desc), args, _stream())
-    _written(o_tgt, o_ref if ref_queries else None, mass_t, lse_t, mrq_t, smass_t)
     return _attn_out("joint_attn", (q_tgt, k_tgt, v_tgt, q_ref, k_ref, v_ref, k_cache, v_cache, q_cache),
                      o_tgt, o_ref if ref_queries else None, mass_t, lse_t, mrq_t, smass_t)
 
@@ -308,6 +310,8 @@ def new_gate_state(device, delta_max=0):
 
 def gate(d_cur, mass_prev, theta, state, block, step, mode="product", decision_out=None, score_out=None):
     """One block's decision through ``refadapt_gate``; returns (decision int32[1], scores fp32[3])."""
+    if _forward._current_level >= 0:
+        _no_tangents(d_cur=d_cur, mass_prev=mass_prev, theta=theta)
     B, H = d_cur.shape
     n_tgt = mass_prev.shape[-1]
     dev = d_cur.device
@@ -330,7 +334,7 @@ def gate(d_cur, mass_prev, theta, state, block, step, mode="product", decision_o
         B, H, n_tgt, int(block), int(step), _GATE[mode],
         _ptr(d_cur), _ptr(mass_prev), _ptr(theta), _ptr(state), _ptr(decision_out), _ptr(score_out), _stream(),
     )
-    _written(state, decision_out, score_out)
+    _written((state, decision_out, score_out))
     return decision_out, score_out
 
 
@@ -345,6 +349,8 @@ def q_change_gate(q_cur, q_prev, mass_prev, theta, state, block, step, mode="pro
                   decision_out=None, score_out=None, workspace=None):
     """Q-change and gate fused through ``refadapt_q_change_gate``;
     returns (d [B, H], decision int32[1], scores fp32[3])."""
+    if _forward._current_level >= 0:
+        _no_tangents(mass_prev=mass_prev, theta=theta)
     B, H, n, D = q_cur.shape
     dt = q_cur.dtype
     if dt not in _DTYPES:
@@ -377,7 +383,7 @@ def q_change_gate(q_cur, q_prev, mass_prev, theta, state, block, step, mode="pro
         int(block), int(step), _GATE[mode], _ptr(mass_prev), _ptr(theta), _ptr(state), _ptr(d_out),
         _ptr(decision_out), _ptr(score_out), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(),
     )
-    _written(state, d_out, decision_out, score_out)
+    _written((state, d_out, decision_out, score_out))
     return d_out, decision_out, score_out
 
 
@@ -386,6 +392,8 @@ def q_change_gate_noalloc(q_cur, q_prev, mass_prev, theta, state, block, step, m
     """``q_change_gate`` through ``refadapt_q_change_gate_noalloc``: no workspace, the library's
     fixed device scratch holds the partial sums (for callers that cannot allocate; calls that
     overlap on one device race). Outputs must be passed in to allocate nothing here either."""
+    if _forward._current_level >= 0:
+        _no_tangents(mass_prev=mass_prev, theta=theta)
     B, H, n, D = q_cur.shape
     dt = q_cur.dtype
     if dt not in _DTYPES:
@@ -414,7 +422,7 @@ def q_change_gate_noalloc(q_cur, q_prev, mass_prev, theta, state, block, step, m
         int(block), int(step), _GATE[mode], _ptr(mass_prev), _ptr(theta), _ptr(state), _ptr(d_out),
         _ptr(decision_out), _ptr(score_out), _stream(),
     )
-    _written(state, d_out, decision_out, score_out)
+    _written((state, d_out, decision_out, score_out))
     return d_out, decision_out, score_out
 
 
@@ -439,7 +447,7 @@ def cache_commit(k_ref, v_ref, k_cache, v_cache, decision=None, age=None, step=0
         _view("q_cache", q_cache, dt, k_ref.shape),
         _ptr(decision), _ptr(age), int(step), _stream(),
     )
-    _written(k_cache, v_cache, q_cache, age)
+    _written([t for t in (k_cache, v_cache, q_cache, age) if t is not None])
 
 
 # ---- diagnostics sidecar (read-only probes of the controlled path)
@@ -481,7 +489,7 @@ def kv_drift(k_cur, k_base, v_cur, v_base, eps=1e-8, d_k=None, d_v=None, e_kv=No
         _view("v_cur", v_cur, dt, k_cur.shape), _view("v_base", v_base, dt, k_cur.shape), float(eps),
         _ptr(d_k), _ptr(d_v), _ptr(e_kv), _ptr(workspace), _nbytes(workspace), _stream(),
     )
-    _written(d_k, d_v, e_kv)
+    _written((d_k, d_v, e_kv))
     return d_k, d_v, e_kv
 
 
@@ -512,7 +520,7 @@ def drift_log_ratio(z_ref_cur, z_ref_prev, z_tgt_cur, z_tgt_prev, eps=1e-8, d_re
         _view("z_tgt_prev", z_tgt_prev, dt, (B, H, n_tgt, D)), float(eps), _ptr(d_ref), _ptr(d_tgt), _ptr(rho),
         _ptr(workspace), _nbytes(workspace), _stream(),
     )
-    _written(d_ref, d_tgt, rho)
+    _written((d_ref, d_tgt, rho))
     return d_ref, d_tgt, rho
 
 
@@ -542,6 +550,8 @@ def output_impact(o_stale, o_fresh, eps=1e-8, out=None, workspace=None):
 def mass_mean(mass, complement=False, out=None):
     """Per-(b, h) mean over rows of a [B, H, n] per-query mass (or of 1 - mass) through
     ``refadapt_mass_mean``."""
+    if _forward._current_level >= 0:
+        _no_tangents(mass=mass)
     _on_gpu("mass", mass)
     if mass.dim() != 3 or mass.dtype != torch.float32 or not mass.is_contiguous():
         raise ValueError("mass must be a contiguous float32 [B, H, n] tensor")
@@ -555,6 +565,8 @@ def mass_mean(mass, complement=False, out=None):
 def adjacent_mass_change(mass_log, out=None):
     """Per block, 100 / (T - 1) * sum_t |Mbar_t - Mbar_{t-1}| (percentage points) from a
     [T, n_blocks, ...] log of per-head mass means, through ``refadapt_adjacent_mass_change``."""
+    if _forward._current_level >= 0:
+        _no_tangents(mass_log=mass_log)
     _on_gpu("mass_log", mass_log)
     if mass_log.dim() < 2 or mass_log.dtype != torch.float32 or not mass_log.is_contiguous():
         raise ValueError("mass_log must be a contiguous float32 [T, n_blocks, ...] tensor")
@@ -585,8 +597,6 @@ def _words(name, t, dtype, shape, dev):
         return _NO_TENSOR
     if t.get_device() != dev:
         _elsewhere(name, t, dev)
-    if _forward._current_level >= 0:
-        _no_tangent(name, t)
     if t.shape != shape or t.dtype != dtype:
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} differs from {dtype} {tuple(shape)}")
     sb, sh, ss, sd = t.stride()
@@ -675,6 +685,8 @@ def _readable(t):
 
 
 def _rope(q, k, pos, freq, axis, pairing, inverse, q_out=None, k_out=None):
+    if _forward._current_level >= 0:
+        _no_tangents(q=q, k=k, pos=pos, freq=freq)
     shape, dt, dev = q.shape, q.dtype, torch._C._cuda_getDevice()
     B, H, S, D = shape
     if dt not in _DTYPES:
@@ -684,9 +696,6 @@ def _rope(q, k, pos, freq, axis, pairing, inverse, q_out=None, k_out=None):
     ps, pst = pos.shape, pos.stride()
     if pos.get_device() != dev:
         _elsewhere("pos", pos, dev)
-    if _forward._current_level >= 0:
-        _no_tangent("pos", pos)
-        _no_tangent("freq", freq)
     if pos.dtype not in _POS or len(ps) not in (2, 3) or pst[-1] != 1 and ps[-1] != 1:
         raise ValueError("pos must be int32 or float32 [S, axes] or [B, S, axes] with contiguous axes")
     if ps[-2] != S or len(ps) == 3 and ps[0] not in (1, B):
@@ -695,6 +704,7 @@ def _rope(q, k, pos, freq, axis, pairing, inverse, q_out=None, k_out=None):
     for name, t, want in (("freq", freq, torch.float64), ("axis", axis, torch.int32)):
         if t.is_cuda or t.dtype != want or t.shape != (n,) or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous {want} host tensor, one entry a pair")
+    given = [t for t in (q_out, k_out) if t is not None]
     if q_out is None:
         q_out = torch.empty_like(q)
     if k is None:
@@ -709,7 +719,8 @@ def _rope(q, k, pos, freq, axis, pairing, inverse, q_out=None, k_out=None):
                                  _POS[pos.dtype], pst[0] if len(ps) == 3 and ps[0] == B else 0, pst[-2],
                                  freq.data_ptr(), axis.data_ptr())
     L.refadapt_rope_packed(desc, args, _stream())
-    _written(q_out, k_out)
+    if given:
+        _written(given)
     return q_out if k is None else (q_out, k_out)
 
 
@@ -779,6 +790,8 @@ def mx_commit(k_ref, v_ref, k_mx, v_mx, decision=None, age=None, step=0, q_ref=N
     """``cache_commit`` into a quantised cache, through ``refadapt_mx_commit``: rounds the fresh reference K, V (and Q
     when ``q_ref``/``q_mx`` are given) into the ``MxTensor``s when ``decision`` is COMPUTE (or None); with ``v_ref``
     and ``v_mx`` None only K. One launch takes every pair."""
+    if _forward._current_level >= 0:
+        _no_tangents(k_ref=k_ref, v_ref=v_ref, q_ref=q_ref)
     shape, dt, dev, fmt = k_ref.shape, k_ref.dtype, torch._C._cuda_getDevice(), _mx_format(k_mx)
     B, H, n_ref, D = shape
     if dt not in _DTYPES:
@@ -793,7 +806,13 @@ def mx_commit(k_ref, v_ref, k_mx, v_mx, decision=None, age=None, step=0, q_ref=N
         *_mx_words("v_mx", v_mx, fmt, shape, dev), *_mx_words("q_mx", q_mx, fmt, shape, dev),
         _int_word("decision", decision, dev), _int_word("age", age, dev), int(step))
     L.refadapt_mx_commit_packed(L.MX_DESC_PACK.pack(B, H, n_ref, D, _DTYPES[dt], _MX[fmt]), args, _stream())
-    _written(age, *(t for m in (k_mx, v_mx, q_mx) if m is not None for t in (m.codes, m.scales)))
+    written = [k_mx.codes, k_mx.scales]
+    for m in (v_mx, q_mx):
+        if m is not None:
+            written += m.codes, m.scales
+    if age is not None:
+        written.append(age)
+    _written(written)
 
 
 def mx_read(k_mx, v_mx=None, q_mx=None, dtype=torch.bfloat16, k_out=None, v_out=None, q_out=None):
@@ -816,8 +835,9 @@ def mx_read(k_mx, v_mx=None, q_mx=None, dtype=torch.bfloat16, k_out=None, v_out=
         *_words("q_out", q_out, dtype, shape, dev), *_mx_words("k_mx", k_mx, fmt, shape, dev),
         *_mx_words("v_mx", v_mx, fmt, shape, dev), *_mx_words("q_mx", q_mx, fmt, shape, dev), 0, 0, 0)
     L.refadapt_mx_read_packed(L.MX_DESC_PACK.pack(B, H, n, D, _DTYPES[dtype], _MX[fmt]), args, _stream())
-    _written(k_out, v_out, q_out)
-    return tuple(o for o in (k_out, v_out, q_out) if o is not None)
+    out = tuple(o for o in (k_out, v_out, q_out) if o is not None)
+    _written(out)
+    return out
 
 
 def joint_attn_mx(q_tgt, k_tgt, v_tgt, *, k_mx, v_mx, q_mx=None, q_ref=None, k_ref=None, v_ref=None, qset="target",
@@ -826,6 +846,8 @@ def joint_attn_mx(q_tgt, k_tgt, v_tgt, *, k_mx, v_mx, q_mx=None, q_ref=None, k_r
     """``joint_attn`` with ``kvsrc`` "cache" or "device" whose cached reference K, V (and queries, ``q_mx``) are
     ``MxTensor``s, through ``refadapt_joint_attn_mx``. ``workspace``: None allocates what the library asks for, a
     uint8 device tensor is used as given (``attn_mx_workspace``). Returns an ``AttnOut``, without gradients as there."""
+    if _forward._current_level >= 0:
+        _no_tangents(q_tgt=q_tgt, k_tgt=k_tgt, v_tgt=v_tgt, q_ref=q_ref, k_ref=k_ref, v_ref=v_ref)
     shp_t, dt, dev, where = q_tgt.shape, q_tgt.dtype, torch._C._cuda_getDevice(), q_tgt.device
     B, H, n_tgt, D = shp_t
     if dt not in _DTYPES:
@@ -875,7 +897,6 @@ def joint_attn_mx(q_tgt, k_tgt, v_tgt, *, k_mx, v_mx, q_mx=None, q_ref=None, k_r
     cache = L.MX_CACHE_PACK.pack(_MX[fmt], *_mx_words("k_mx", k_mx, fmt, shp_r, dev),
                                  *_mx_words("v_mx", v_mx, fmt, shp_r, dev), *_mx_words("q_mx", q_mx, fmt, shp_r, dev))
     L.refadapt_joint_attn_mx_packed(desc, args, cache, _stream())
-    _written(o_tgt, o_ref if ref_queries else None, mass_t, lse_t, mrq_t)
     return _attn_out("joint_attn_mx", (q_tgt, k_tgt, v_tgt, q_ref, k_ref, v_ref),
                      o_tgt, o_ref if ref_queries else None, mass_t, lse_t, mrq_t)
 
@@ -901,8 +922,6 @@ def _rows(name, t, dtype, shape, dev):
         return _NO_TENSOR
     if t.get_device() != dev:
         _elsewhere(name, t, dev)
-    if _forward._current_level >= 0:
-        _no_tangent(name, t)
     if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} differs from {dtype} {tuple(shape)}")
     st = t.stride()
@@ -925,8 +944,6 @@ def _row_words(name, t, dtype, shape, dev):
         return 0, 0
     if t.get_device() != dev:
         _elsewhere(name, t, dev)
-    if _forward._current_level >= 0:
-        _no_tangent(name, t)
     if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} differs from {dtype} {tuple(shape)}")
     if t.stride(-1) != 1 and shape[-1] != 1:
@@ -946,6 +963,8 @@ def _norm_desc(x, sizes, params, eps, fmt=0):
 
 
 def _norm(x, weight, bias, scale, shift, eps, y=None, y_mx=None, stats=None):
+    if _forward._current_level >= 0:
+        _no_tangents(x=x, weight=weight, bias=bias, scale=scale, shift=shift)
     dev, shape = torch._C._cuda_getDevice(), x.shape
     B, S, C = sizes = _batch_rows("x", shape)
     desc, pdt = _norm_desc(x, sizes, (weight, bias, scale, shift), eps, 0 if y_mx is None else _MX[y_mx.fmt])
@@ -1030,12 +1049,12 @@ def layer_norm_grad(dy, x, stats, weight=None, bias=None, *, scale=None, eps=1e-
         raise ValueError(f"stats must be contiguous float32 {(*shape[:-1], 2)}")
     if stats.get_device() != dev:
         _elsewhere("stats", stats, dev)
-    if _forward._current_level >= 0:
-        _no_tangent("stats", stats)
     return _norm_grad(desc, pdt, dy, x, stats, weight, bias, scale, wanted, ((B, C), (B, C)), workspace)
 
 
 def _norm_grad(desc, pdt, dy, x, stats, weight, bias, scale, wanted, shapes, workspace=None):
+    if _forward._current_level >= 0:
+        _no_tangents(dy=dy, x=x, stats=stats, weight=weight, bias=bias, scale=scale)
     dev, shape, dt = torch._C._cuda_getDevice(), x.shape, x.dtype
     (S, C), B = shape[-2:], shape[0] if len(shape) == 3 else 1
     w_params = wanted[1:]
@@ -1082,7 +1101,7 @@ def layer_norm_mx(x, fmt, weight=None, bias=None, *, scale=None, shift=None, eps
     elif out.fmt != fmt:
         raise ValueError(f"out: format {out.fmt} differs from {fmt}")
     _norm(x, weight, bias, scale, shift, eps, y_mx=out)
-    _written(out.codes, out.scales)
+    _written((out.codes, out.scales))
     return out
 
 
@@ -1158,12 +1177,13 @@ def mx_linear(x, w, bias=None, *, fmt=None, dtype=None, out=None, workspace=None
 
 
 def _linear(x, w, bias, fmt, dt, sizes, lead, out=None, workspace=None):
-    dev = torch._C._cuda_getDevice()
+    mx, dev = isinstance(x, MxTensor), torch._C._cuda_getDevice()
+    if _forward._current_level >= 0:
+        _no_tangents(x=None if mx else x, bias=bias)
     B, S, K = sizes
     desc, n_out, n_in = _linear_desc(B, S, w, dt, fmt)
     if K != n_in:
         raise ValueError(f"rows of {K} elements and weights of {n_in}")
-    mx = isinstance(x, MxTensor)
     where = x.codes.device if mx else x.device
     if not where.type == "cuda":
         _on_gpu("x", x.codes if mx else x)
@@ -1202,6 +1222,8 @@ class _MxLinear(torch.autograd.Function):
 def mx_linear_grad(dy, w, *, wanted=(True, True), workspace=None):
     """The gradients of ``mx_linear`` through ``refadapt_mx_linear_grad``: (dx, dbias) of ``dy`` [B, S, n_out] or
     [S, n_out], None where ``wanted`` says so."""
+    if _forward._current_level >= 0:
+        _no_tangents(dy=dy)
     dev, shape, dt = torch._C._cuda_getDevice(), dy.shape, dy.dtype
     B, S, N = _batch_rows("dy", shape)
     desc, n_out, n_in = _linear_desc(B, S, w, dt, w.fmt)

@@ -49,6 +49,10 @@ def _attn_tensors(**more):
     return dict({n: _t(1, 1, 4, 64) for n in ("q_tgt", "k_tgt", "v_tgt", "q_ref", "k_ref", "v_ref")}, **more)
 
 
+def _two():
+    return dict(q_cur=_t(1, 1, 4, 64), q_prev=_t(1, 1, 4, 64))
+
+
 CALLS = {
     "layer_norm": (ops.layer_norm, _norm_tensors()),
     "layer_norm_mx": (lambda **t: ops.layer_norm_mx(fmt="mxfp4", **t), _norm_tensors()),
@@ -60,9 +64,22 @@ CALLS = {
     "rope": (ops.rope, _rope_tensors()),
     "joint_attn": (ops.joint_attn, _attn_tensors(k_cache=_t(1, 1, 4, 64), v_cache=_t(1, 1, 4, 64))),
     "joint_attn_mx": (lambda **t: ops.joint_attn_mx(k_mx=_mx(), v_mx=_mx(), **t), _attn_tensors()),
-    "q_change": (lambda **t: ops.q_change(workspace=_t(64, dtype=U8), **t),
-                 dict(q_cur=_t(1, 1, 4, 64), q_prev=_t(1, 1, 4, 64))),
+    "q_change": (lambda **t: ops.q_change(workspace=_t(64, dtype=U8), **t), _two()),
     "mass_mean": (ops.mass_mean, dict(mass=_t(1, 2, 4, dtype=F32))),
+    "adjacent_mass_change": (ops.adjacent_mass_change, dict(mass_log=_t(3, 2, 1, dtype=F32))),
+    "gate": (lambda **t: ops.gate(state=_t(4, dtype=I32), block=0, step=0, **t),
+             dict(d_cur=_t(1, 1, dtype=F32), mass_prev=_t(1, 1, 4, dtype=F32), theta=_t(1, dtype=F32))),
+    "q_change_gate": (lambda **t: ops.q_change_gate(state=_t(4, dtype=I32), block=0, step=0, workspace=_t(64, dtype=U8),
+                                                    **t),
+                      dict(_two(), mass_prev=_t(1, 1, 4, dtype=F32), theta=_t(1, dtype=F32))),
+    "q_change_gate_noalloc": (lambda **t: ops.q_change_gate_noalloc(state=_t(4, dtype=I32), block=0, step=0, **t),
+                              dict(_two(), mass_prev=_t(1, 1, 4, dtype=F32), theta=_t(1, dtype=F32))),
+    "cache_commit": (lambda **t: ops.cache_commit(k_cache=_t(1, 1, 4, 64), v_cache=_t(1, 1, 4, 64), **t),
+                     dict(k_ref=_t(1, 1, 4, 64), v_ref=_t(1, 1, 4, 64))),
+    "kv_drift": (lambda **t: ops.kv_drift(workspace=_t(64, dtype=U8), **t),
+                 {n: _t(1, 1, 4, 64) for n in ("k_cur", "k_base", "v_cur", "v_base")}),
+    "output_impact": (lambda **t: ops.output_impact(workspace=_t(64, dtype=U8), **t),
+                      dict(o_stale=_t(1, 1, 4, 64), o_fresh=_t(1, 1, 4, 64))),
 }
 CASES = [(name, n) for name, (_, tensors) in CALLS.items() for n, t in tensors.items() if t.is_floating_point()]
 
