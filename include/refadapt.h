@@ -616,7 +616,7 @@ typedef struct {
  * no gradient of their own. Products and sums are exact to fp32 roundings, rounded once
  * to dtype, and deterministic. fp32 dy enters as three bf16 terms, exact from 2^-110 in
  * size on; of smaller values the bits below 2^-133 are left out. dbias is summed in fp32
- * over up to 512 rows (2048 from 2^25 rows on) and in fp64 over the rest. Where dtype is RA_BF16 and n_out a multiple of 8, rows
+ * over up to 512 rows (more from 2^25 rows on) and in fp64 over the rest. Where dtype is RA_BF16 and n_out a multiple of 8, rows
  * of dy lie in whole 16-byte units and evenly over the batch. Without rows dbias is
  * zeros. desc->x_format is not read beyond its check.
  * Errors: as refadapt_mx_linear; RA_EINVAL (no gradient wanted, dx over dy).
